@@ -8,7 +8,9 @@
  *   - P0 is an operator descriptor (rc_op_desc): one of five dense
  *     contractions with fused epilogues, the layer kinds of Sec. 4.1
  *     (attention, MoE, convolution, gated MLP) plus the fp32 contraction of
- *     the App. A example module;
+ *     the App. A example module; or one of the operators of the dense layers
+ *     in 8-bit integers (the matrix product with its scales, and the
+ *     quantisation of its rows, with or without a norm in front);
  *   - a program variant is a schedule (rc_schedule): one integer per knob;
  *   - a transformation (rc_transform) sets one knob, named after the
  *     transformation classes of App. A (TileSize, Parallel,
@@ -111,11 +113,53 @@ typedef enum rc_op_kind {
      * in[1] = w stored [K][R][S][C] (layout 1) or [R][S][C][K] (layout 0)
      * bf16; in[2] = bias [K] fp32; out[0] = y [N][P][Q][K] bf16 with
      * P = H + 2 pad - R + 1, Q = W + 2 pad - S + 1. */
-    RC_OP_CONV2D = 5
+    RC_OP_CONV2D = 5,
+    /* Root-mean-square norm of bf16 rows with an int8 output and a scale for
+     * each row; with RC_FLAG_RESIDUAL the residual's addition in front:
+     *   h = bf16(x + r)  (x without the flag),
+     *   y = h / sqrt(mean(h^2) + eps) * w,
+     *   scale = max |y| / 127,  q = y / scale rounded to the nearest integer
+     *   (halves to the even one), so that q * scale is y in 8 bits.
+     * q is the exactly rounded quotient (the norm's factor cancels from it),
+     * whatever the schedule.  A row of zeros has q 0 and scale 0; a row that
+     * holds a NaN or an infinity, or whose squares sum past fp32, has q 0 and
+     * scale NaN.
+     * dim = {T, Hd}; the descriptor's eps (1e-6 from rc_op_init) is finite
+     * and at least 2^-100.  in[0] = x [T][Hd] bf16; in[1] = w [Hd] bf16;
+     * in[2] = r [T][Hd] bf16 (RC_FLAG_RESIDUAL).  out[0] = q [T][Hd] int8;
+     * out[1] = scale [T] fp32; out[2] = h [T][Hd] bf16 (RC_FLAG_RESIDUAL),
+     * which may be the buffer of x or of r (no other overlap is allowed).
+     * Hd need not be a multiple of anything. */
+    RC_OP_RMSNORM_I8 = 6,
+    /* Rows of bf16 to int8 with a scale for each row, without a norm:
+     *   scale = max |x| / 127,  q = x / scale rounded as above
+     * (rows of zeros and rows with a NaN or an infinity as above).
+     * dim = {T, Hd}.  in[0] = x [T][Hd] bf16; out[0] = q [T][Hd] int8;
+     * out[1] = scale [T] fp32. */
+    RC_OP_QUANT_I8 = 7,
+    /* Matrix product in 8-bit integers with a scale for each row of A (token)
+     * and of the weight (channel), int32 sums, which are exact:
+     *   out[m][n] = (sum_k A[m][k] B[n][k]) * sa[m] * sb[n] (+ bias[n]),
+     * in bf16, or in fp32 with RC_FLAG_OUT_F32; bias with RC_FLAG_BIAS.
+     * With RC_FLAG_GATED (alone) two weights share A, and
+     *   out = bf16(SiLU(g) * u),  g and u the two products.
+     * dim = {M, N, K}, K at most 131071 (the sums of 128 * 128 stay in 32
+     * bits), N at most 2^30, M at most 2^31 - 1.  in[0] = A [M][K] int8;
+     * in[1] = sa [M] fp32; in[2] = B [N][K] int8; in[3] = sb [N] fp32;
+     * in[4] = bias [N] fp32 (RC_FLAG_BIAS), or in[4] = the up weight [N][K]
+     * int8 and in[5] = its scales [N] fp32 (RC_FLAG_GATED; in[2] and in[3]
+     * are the gate's).  out[0] = [M][N].  No size need be a multiple of
+     * anything.  Weights are stored [N][K] only: 16 consecutive k are what a
+     * lane of the matrix cores takes. */
+    RC_OP_GEMM_I8 = 8
 } rc_op_kind;
 
 #define RC_FLAG_CAUSAL 1   /* RC_OP_ATTENTION only */
 #define RC_FLAG_NO_ACT 2   /* RC_OP_CONV2D only: bias, no SiLU */
+#define RC_FLAG_RESIDUAL 4 /* RC_OP_RMSNORM_I8 only: h = bf16(x + r), stored */
+#define RC_FLAG_BIAS 8     /* RC_OP_GEMM_I8 only: + bias[n] */
+#define RC_FLAG_OUT_F32 16 /* RC_OP_GEMM_I8 only: fp32 output */
+#define RC_FLAG_GATED 32   /* RC_OP_GEMM_I8 only: SiLU(g) * u, two weights */
 #define RC_MAX_DIMS 8
 
 typedef struct rc_op_desc {
@@ -123,13 +167,14 @@ typedef struct rc_op_desc {
     int32_t kind;              /* rc_op_kind */
     int64_t dim[RC_MAX_DIMS];  /* meaning per kind, unused entries 0 */
     int32_t flags;
-    int32_t reserved;
+    float eps;                 /* RC_OP_RMSNORM_I8 only; may be set after rc_op_init */
 } rc_op_desc;
 
 /* Fill *d for `kind` with `ndims` dimensions.  Checks the kind, the number
  * of dimensions, that every dimension is positive (pad may be 0) and that
  * `flags` holds only flags defined for the kind; RC_ERR_INVALID_ARGUMENT
- * otherwise. */
+ * otherwise.  Sizes past the limits stated for the 8-bit kinds are
+ * RC_ERR_UNSUPPORTED. */
 rc_status rc_op_init(rc_op_desc *d, int32_t kind, const int64_t *dims, int32_t ndims,
                      int32_t flags);
 
@@ -141,8 +186,9 @@ rc_status rc_op_init(rc_op_desc *d, int32_t kind, const int64_t *dims, int32_t n
 double rc_op_flops(const rc_op_desc *d);
 double rc_op_bytes(const rc_op_desc *d);
 /* Published MI355X peak that bounds the operator: fp32 MFMA (157.3 TFLOP/s)
- * for RC_OP_GEMM_F32, bf16 MFMA (2516.6 TFLOP/s) otherwise, in FLOP/s;
- * and HBM bandwidth (8.0e12 B/s). */
+ * for RC_OP_GEMM_F32, int8 MFMA (5033.2 TOP/s) for RC_OP_GEMM_I8, bf16 MFMA
+ * (2516.6 TFLOP/s) otherwise, in FLOP/s; and HBM bandwidth (8.0e12 B/s).
+ * (The row kinds have no contraction: their FLOPs are 0.) */
 double rc_peak_flops(const rc_op_desc *d);
 double rc_peak_bytes_per_s(void);
 
@@ -179,6 +225,13 @@ rc_status rc_knob_values(const rc_op_desc *d, int32_t knob, int32_t *vals, int32
  * legal for every operator this library accepts, and it is the denominator
  * of reported speedups (Sec. 4.2). */
 rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out);
+
+/* A legal schedule for an 8-bit kind (RC_OP_RMSNORM_I8, RC_OP_QUANT_I8,
+ * RC_OP_GEMM_I8) at the descriptor's sizes, by rules on sizes: for a caller
+ * that has not searched, whose sizes change from call to call (the kernels of
+ * these kinds take sizes as arguments, so that plans of all sizes share a few
+ * code objects).  RC_ERR_UNSUPPORTED for the other kinds. */
+rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out);
 
 /* Legality check, host only.  Returns RC_OK or RC_ERR_ILLEGAL_SCHEDULE with
  * the first violated rule written to `why` (may be NULL).  Tiles may end
@@ -302,14 +355,18 @@ rc_status rc_describe(const rc_op_desc *d, const rc_schedule *s, rc_kernel_info 
 rc_status rc_kernel_defines(const rc_op_desc *d, const rc_schedule *s, int32_t i, char *buf,
                             size_t cap);
 
+/* (Operators with up to two outputs also take a block that ends after
+ * out[1], its struct_size saying so.) */
 typedef struct rc_args {
     uint32_t struct_size;
     const void *in[8];
-    void *out[2];
+    void *out[4];
 } rc_args;
 
 /* Enqueue one execution of the operator on `stream`.  Checks pointers
- * (non-NULL, 16-byte aligned) and the workspace size; never synchronises. */
+ * (non-NULL, 16-byte aligned) and the workspace size; never synchronises.
+ * The plan of an 8-bit kind is launched with the device current that it was
+ * created on (RC_ERR_INVALID_ARGUMENT otherwise). */
 rc_status rc_launch(const rc_plan *p, const rc_args *a, void *workspace, size_t ws_bytes,
                     void *stream);
 

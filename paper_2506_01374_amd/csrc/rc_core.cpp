@@ -123,6 +123,30 @@ static std::vector<KnobDef> attention_knobs() {
     };
 }
 
+static std::vector<KnobDef> rows_i8_knobs() {
+    return {
+        {"waves", "Parallel", {1, 2, 4, 8, 16}, 1},           // waves that share a row
+        {"rows", "Parallel", {1, 2, 4, 8}, 1},                // rows of a workgroup
+        {"vec", "Vectorize", {1, 2, 4, 8}, 1},                // bf16 per global load
+        // vectors a thread keeps between its two passes over a row (0: reads it again)
+        {"held", "ComputeLocation", {0, 1, 2, 4}, 0},
+    };
+}
+
+static std::vector<KnobDef> gemm_i8_knobs() {
+    return {
+        {"tile_m", "TileSize", {16, 32, 64, 128, 256}, 16},
+        {"tile_n", "TileSize", {16, 32, 64, 128, 256}, 16},   // output columns
+        {"tile_k", "TileSize", {64, 128, 256}, 64},
+        {"waves_m", "Parallel", {1, 2, 4}, 1},
+        {"waves_n", "Parallel", {1, 2, 4}, 1},
+        {"mfma", "TileSize", {16, 32}, 16},                   // MFMA instruction shape
+        {"stages", "ComputeLocation", {1}, 1},                // staging of the K tiles
+        {"order", "Parallel", {0, 1}, 0},                     // tile order: plain / XCD-grouped bands
+        {"occ", "Parallel", {1, 2}, 1},                       // waves per SIMD to budget registers for
+    };
+}
+
 const std::vector<KnobDef> &knobs_for(int32_t kind) {
     static const std::vector<KnobDef> empty;
     static const std::vector<KnobDef> g = gemm_f32_knobs();
@@ -130,12 +154,17 @@ const std::vector<KnobDef> &knobs_for(int32_t kind) {
     static const std::vector<KnobDef> m = mlp_knobs();
     static const std::vector<KnobDef> e = moe_knobs();
     static const std::vector<KnobDef> c = conv_knobs();
+    static const std::vector<KnobDef> ri = rows_i8_knobs();
+    static const std::vector<KnobDef> gi = gemm_i8_knobs();
     switch (kind) {
         case RC_OP_GEMM_F32: return g;
         case RC_OP_ATTENTION: return a;
         case RC_OP_GATED_MLP: return m;
         case RC_OP_MOE: return e;
         case RC_OP_CONV2D: return c;
+        case RC_OP_RMSNORM_I8:
+        case RC_OP_QUANT_I8: return ri;
+        case RC_OP_GEMM_I8: return gi;
         default: return empty;
     }
 }
@@ -154,6 +183,9 @@ static int expected_dims(int32_t kind) {
         case RC_OP_GATED_MLP: return 3;
         case RC_OP_MOE: return 5;
         case RC_OP_CONV2D: return 8;
+        case RC_OP_RMSNORM_I8:
+        case RC_OP_QUANT_I8: return 2;
+        case RC_OP_GEMM_I8: return 3;
         default: return -1;
     }
 }
@@ -344,7 +376,89 @@ static std::string check_bf16_block(const rc_op_desc *d, const rc_schedule *s,
     return "";
 }
 
+static int32_t allowed_flags(int32_t kind) {
+    switch (kind) {
+        case RC_OP_ATTENTION: return RC_FLAG_CAUSAL;
+        case RC_OP_CONV2D: return RC_FLAG_NO_ACT;
+        case RC_OP_RMSNORM_I8: return RC_FLAG_RESIDUAL;
+        case RC_OP_GEMM_I8: return RC_FLAG_BIAS | RC_FLAG_OUT_F32 | RC_FLAG_GATED;
+        default: return 0;
+    }
+}
+
+// What a descriptor of an 8-bit kind must keep to beyond positive
+// dimensions: "" or the first violated rule.  `size`: the rule is a limit of
+// the kernels, not a wrong argument.
+static std::string check_i8_desc(const rc_op_desc *d, bool *size) {
+    *size = false;
+    const int64_t *D = d->dim;
+    switch (d->kind) {
+        case RC_OP_RMSNORM_I8:
+            // (squares below fp32's normal range are nothing next to it)
+            if (!(d->eps >= 0x1p-100f) || !std::isfinite(d->eps)) return "eps must be finite and at least 2^-100";
+            // fall through: the same row sizes
+        case RC_OP_QUANT_I8:
+            *size = true;
+            if (D[0] > INT32_MAX) return fmt("%lld rows exceed the grid's 2^31 - 1", (long long)D[0]);
+            if (D[1] > (1LL << 30)) return fmt("rows of %lld elements exceed the 32-bit column indices", (long long)D[1]);
+            return "";
+        case RC_OP_GEMM_I8:
+            if ((d->flags & RC_FLAG_GATED) && (d->flags & (RC_FLAG_BIAS | RC_FLAG_OUT_F32)))
+                return "the gated form takes no bias and stores bf16";
+            *size = true;
+            if (D[2] > 131071) return fmt("K = %lld: sums of more than 131071 products can exceed int32", (long long)D[2]);
+            if (D[0] > INT32_MAX) return fmt("M = %lld exceeds 2^31 - 1", (long long)D[0]);
+            if (D[1] > (1LL << 30)) return fmt("N = %lld exceeds 2^30", (long long)D[1]);
+            return "";
+    }
+    return "";
+}
+
+static std::string check_rows_i8(const rc_op_desc *d, const rc_schedule *s) {
+    const int w = kv(d, s, "waves"), r = kv(d, s, "rows"), vec = kv(d, s, "vec"), held = kv(d, s, "held");
+    const int64_t T = d->dim[0], C = d->dim[1];
+    if (w * r > 16) return fmt("waves x rows = %d exceeds 16 waves per workgroup", w * r);
+    if (redundant_tile(d, "rows", r, T)) return fmt("rows %d: rows %d already cover T = %lld", r, r / 2, (long long)T);
+    if (redundant_tile(d, "vec", vec, C)) return fmt("vec %d: vec %d already covers a row of %lld", vec, vec / 2, (long long)C);
+    const int64_t step = 64LL * w * vec;     // elements of one vector of every thread of a row
+    if (w > 1 && step / 2 >= C) return fmt("waves %d: half of them already cover a row of %lld", w, (long long)C);
+    if (held > 0 && step * held < C)
+        return fmt("%d vectors of %d in each of %d threads do not hold a row of %lld", held, vec, 64 * w, (long long)C);
+    if (held > 1 && step * (held / 2) >= C) return fmt("held %d: %d vectors already hold a row of %lld", held, held / 2, (long long)C);
+    return "";
+}
+
+static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
+    const int nb = (d->flags & RC_FLAG_GATED) ? 2 : 1;
+    const int tm = kv(d, s, "tile_m"), tno = kv(d, s, "tile_n"), tn = nb * tno, tk = kv(d, s, "tile_k");
+    const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), mf = kv(d, s, "mfma");
+    const int occ = kv(d, s, "occ");
+    const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
+    const int nt = 64 * wm * wn;
+    if (tm % wm || (tm / wm) % mf) return fmt("tile_m/waves_m = %d/%d is not a multiple of the %dx%d MFMA", tm, wm, mf, mf);
+    if (tno % wn || (tno / wn) % mf) return fmt("tile_n/waves_n = %d/%d is not a multiple of the %dx%d MFMA", tno, wn, mf, mf);
+    // tiles may end over every extent, but one twice the extent adds only empty work
+    if (redundant_tile(d, "tile_m", tm, M)) return fmt("tile_m %d: tile_m %d already covers M = %lld", tm, tm / 2, (long long)M);
+    if (redundant_tile(d, "tile_n", tno, N)) return fmt("tile_n %d: tile_n %d already covers N = %lld", tno, tno / 2, (long long)N);
+    if (redundant_tile(d, "tile_k", tk, K)) return fmt("tile_k %d: tile_k %d already covers K = %lld", tk, tk / 2, (long long)K);
+    if (((M + tm - 1) / tm) * ((N + tno - 1) / tno) > INT32_MAX) return "the tiles exceed the grid's 2^31 - 1";
+    const int64_t acc = (int64_t)tm * tn / nt;
+    if (acc > 256) return fmt("%lld accumulators per lane exceed 256", (long long)acc);
+    if (occ > 1 && acc > 512 / occ - 32) return fmt("%lld accumulators leave no registers at %d waves/SIMD", (long long)acc, occ);
+    // register staging of the next tile next to the accumulators
+    const int64_t stage_bytes = (int64_t)(tm + tn) * tk;
+    const int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 4;
+    if (regs > 384) return fmt("%lld accumulator and staging registers per lane exceed 384", (long long)regs);
+    const int64_t lds = 2 * stage_bytes;
+    const int64_t wgs = occ > 1 ? (occ * 4 + wm * wn - 1) / (wm * wn) : 1;
+    if (wgs * lds > LDS_LIMIT) return fmt("%lld workgroups of %lld B LDS do not fit a CU", (long long)wgs, (long long)lds);
+    return "";
+}
+
 std::string check_schedule(const rc_op_desc *d, const rc_schedule *s) {
+    bool size = false;
+    std::string bad = check_i8_desc(d, &size);
+    if (!bad.empty()) return bad;
     const auto &kt = knobs_for(d->kind);
     if (s->struct_size < sizeof(rc_schedule)) return "schedule struct_size too small";
     if (s->nknobs != (int32_t)kt.size()) return fmt("schedule has %d knobs, operator has %d",
@@ -552,8 +666,49 @@ std::string check_schedule(const rc_op_desc *d, const rc_schedule *s) {
             if (R * S > 32) return fmt("%lld filter taps exceed the 32-bit tap mask", (long long)(R * S));
             return check_bf16_block(d, s, PLAIN, N * P * Q, K, R * S * C, 1, "conv", true);
         }
+        case RC_OP_RMSNORM_I8:
+        case RC_OP_QUANT_I8: return check_rows_i8(d, s);
+        case RC_OP_GEMM_I8: return check_gemm_i8(d, s);
     }
     return "unknown operator kind";
+}
+
+static void set_knob(const rc_op_desc *d, rc_schedule *s, const char *name, int32_t v) {
+    s->knob[knob_index(d->kind, name)] = v;
+}
+
+// Rows to int8: a row in registers, 16-byte loads, two vectors a thread.
+static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
+    const int64_t T = d->dim[0], C = d->dim[1];
+    int vec = 8;
+    while (vec > 1 && vec / 2 >= C) vec /= 2;
+    int waves = 1, held = 1;
+    while (64LL * waves * vec * held < C && waves < 4) waves *= 2;
+    while (64LL * waves * vec * held < C && held < 2) held *= 2;
+    while (64LL * waves * vec * held < C && waves < 16) waves *= 2;
+    while (64LL * waves * vec * held < C && held < 4) held *= 2;
+    if (64LL * waves * vec * held < C) held = 0;
+    int rows = 1;
+    while (rows * waves < 4 && rows < T) rows *= 2;
+    set_knob(d, s, "vec", vec);
+    set_knob(d, s, "waves", waves);
+    set_knob(d, s, "held", held);
+    set_knob(d, s, "rows", rows);
+}
+
+// The largest of a few tiles that still gives every CU one.
+static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
+    const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
+    static const int tiles[][4] = {{128, 128, 2, 2}, {64, 64, 2, 2}, {32, 32, 2, 2}, {16, 16, 1, 1}};
+    for (const int *t : tiles) {
+        set_knob(d, s, "tile_m", t[0]);
+        set_knob(d, s, "tile_n", t[1]);
+        set_knob(d, s, "waves_m", t[2]);
+        set_knob(d, s, "waves_n", t[3]);
+        if (((M + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) >= 256 && check_schedule(d, s).empty()) break;
+    }
+    set_knob(d, s, "tile_k", K > 64 ? 128 : 64);
+    set_knob(d, s, "order", 1);
 }
 
 }  // namespace rc
@@ -591,11 +746,14 @@ rc_status rc_op_init(rc_op_desc *d, int32_t kind, const int64_t *dims, int32_t n
     t.kind = kind;
     for (int i = 0; i < nd; ++i) t.dim[i] = dims[i];
     t.flags = flags;
+    t.eps = kind == RC_OP_RMSNORM_I8 ? 1e-6f : 0.f;
     if (!desc_ok(&t)) return fail(RC_ERR_INVALID_ARGUMENT, "dimensions must be positive");
-    const int32_t allowed = kind == RC_OP_ATTENTION ? RC_FLAG_CAUSAL : kind == RC_OP_CONV2D ? RC_FLAG_NO_ACT : 0;
-    if (flags & ~allowed) return fail(RC_ERR_INVALID_ARGUMENT, fmt("flags 0x%x not defined for kind %d", flags, kind));
+    if (flags & ~allowed_flags(kind)) return fail(RC_ERR_INVALID_ARGUMENT, fmt("flags 0x%x not defined for kind %d", flags, kind));
     if (kind == RC_OP_MOE && t.dim[4] > t.dim[2])
         return fail(RC_ERR_INVALID_ARGUMENT, "topk exceeds the number of experts");
+    bool size = false;
+    const std::string bad = check_i8_desc(&t, &size);
+    if (!bad.empty()) return fail(size ? RC_ERR_UNSUPPORTED : RC_ERR_INVALID_ARGUMENT, bad);
     *d = t;
     clear_error();
     return RC_OK;
@@ -617,6 +775,9 @@ double rc_op_flops(const rc_op_desc *d) {
             double P = D[1] + 2 * D[7] - D[5] + 1, Q = D[2] + 2 * D[7] - D[6] + 1;
             return 2.0 * D[0] * P * Q * D[4] * D[5] * D[6] * D[3];
         }
+        case RC_OP_RMSNORM_I8:
+        case RC_OP_QUANT_I8: return 0.0;     // no contraction
+        case RC_OP_GEMM_I8: return ((d->flags & RC_FLAG_GATED) ? 4.0 : 2.0) * D[0] * D[1] * D[2];
     }
     return -1.0;
 }
@@ -635,13 +796,22 @@ double rc_op_bytes(const rc_op_desc *d) {
             return 2.0 * D[0] * D[1] * D[2] * D[3] + 2.0 * D[4] * D[5] * D[6] * D[3] + 4.0 * D[4] +
                    2.0 * D[0] * P * Q * D[4];
         }
+        case RC_OP_RMSNORM_I8:
+            return ((d->flags & RC_FLAG_RESIDUAL) ? 7.0 : 3.0) * D[0] * D[1] + 2.0 * D[1] + 4.0 * D[0];
+        case RC_OP_QUANT_I8: return 3.0 * D[0] * D[1] + 4.0 * D[0];
+        case RC_OP_GEMM_I8: {
+            const double nb = (d->flags & RC_FLAG_GATED) ? 2.0 : 1.0;
+            return (double)D[0] * D[2] + 4.0 * D[0] + nb * ((double)D[1] * D[2] + 4.0 * D[1]) +
+                   ((d->flags & RC_FLAG_BIAS) ? 4.0 * D[1] : 0.0) +
+                   ((d->flags & RC_FLAG_OUT_F32) ? 4.0 : 2.0) * D[0] * D[1];
+        }
     }
     return -1.0;
 }
 
 double rc_peak_flops(const rc_op_desc *d) {
     if (!desc_ok(d)) return -1.0;
-    return d->kind == RC_OP_GEMM_F32 ? 157.3e12 : 2516.6e12;
+    return d->kind == RC_OP_GEMM_F32 ? 157.3e12 : d->kind == RC_OP_GEMM_I8 ? 5033.2e12 : 2516.6e12;
 }
 
 double rc_peak_bytes_per_s(void) { return 8.0e12; }
@@ -683,6 +853,26 @@ rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out) {
     for (size_t i = 0; i < k.size(); ++i) s.knob[i] = k[i].def;
     std::string why = check_schedule(d, &s);
     if (!why.empty()) return fail(RC_ERR_UNSUPPORTED, "operator shape admits no default schedule: " + why);
+    *out = s;
+    return RC_OK;
+}
+
+rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) {
+    if (!desc_ok(d) || !out) return fail(RC_ERR_INVALID_ARGUMENT, "bad descriptor");
+    rc_schedule s;
+    std::memset(&s, 0, sizeof s);
+    s.struct_size = sizeof s;
+    const auto &k = knobs_for(d->kind);
+    s.nknobs = (int32_t)k.size();
+    for (size_t i = 0; i < k.size(); ++i) s.knob[i] = k[i].def;
+    if (d->kind == RC_OP_RMSNORM_I8 || d->kind == RC_OP_QUANT_I8)
+        suggest_rows_i8(d, &s);
+    else if (d->kind == RC_OP_GEMM_I8)
+        suggest_gemm_i8(d, &s);
+    else
+        return fail(RC_ERR_UNSUPPORTED, "schedules of this kind are found by search, not suggested");
+    std::string why = check_schedule(d, &s);
+    if (!why.empty()) return fail(RC_ERR_UNSUPPORTED, "no schedule to suggest: " + why);
     *out = s;
     return RC_OK;
 }

@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <fstream>
@@ -64,6 +65,20 @@ struct AttnArgs {
     const void *Q, *K, *V;
     void *O;
     void *P;   // partial states of query tiles cut into several work items
+};
+
+struct RowsI8Args {
+    const void *x, *w, *r;
+    void *q, *scale, *h;
+    long long rows;
+    int cols;
+    float eps;
+};
+struct GemmI8Args {
+    const void *A, *B0, *B1, *sa, *sb0, *sb1, *bias;
+    void *C;
+    long long M;
+    int N, K;
 };
 
 // A kernel's by-value argument block (fixed storage: launching allocates
@@ -442,6 +457,7 @@ struct rc_plan {
     std::vector<Kern> kerns;
     size_t workspace = 0;
     int dominant = 0;
+    int device = -1;          // the kernels' modules are loaded on it
     // named parts of the workspace: name -> (byte offset, bytes)
     std::map<std::string, std::pair<size_t, size_t>> parts;
 };
@@ -828,6 +844,52 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             p.dominant = 0;
             break;
         }
+        case RC_OP_RMSNORM_I8:
+        case RC_OP_QUANT_I8: {
+            const bool norm = d->kind == RC_OP_RMSNORM_I8, res = norm && (d->flags & RC_FLAG_RESIDUAL);
+            const int w = kv(d, s, "waves"), r = kv(d, s, "rows");
+            Kern k;
+            k.src = Source{SRC_rows_i8, "rc_rows_i8",
+                           def("WAVES", w) + def("ROWS", r) + def("VEC", kv(d, s, "vec")) +
+                               def("HELD", kv(d, s, "held")) + def("NORM", norm) + def("RES", res)};
+            k.grid = dim3((unsigned)((D[0] + r - 1) / r), 1, 1);
+            k.block = dim3(64 * w * r, 1, 1);
+            const long long rows = D[0];
+            const int cols = (int)D[1];
+            const float eps = d->eps;
+            k.bind = [=](const rc_args *a, char *, ArgBlob &b) {
+                put(b, RowsI8Args{a->in[0], norm ? a->in[1] : nullptr, res ? a->in[2] : nullptr, a->out[0], a->out[1],
+                                  res ? a->out[2] : nullptr, rows, cols, eps});
+            };
+            p.kerns.push_back(k);
+            p.dominant = 0;
+            break;
+        }
+        case RC_OP_GEMM_I8: {
+            const bool gated = d->flags & RC_FLAG_GATED, bias = d->flags & RC_FLAG_BIAS;
+            const int tm = kv(d, s, "tile_m"), tn = kv(d, s, "tile_n");
+            const int nt = 64 * kv(d, s, "waves_m") * kv(d, s, "waves_n");
+            Kern k;
+            // sizes are arguments: plans of all sizes share the code object
+            k.src = Source{SRC_gemm_i8, "rc_gemm_i8",
+                           def("TM", tm) + def("TN", gated ? 2 * tn : tn) + def("TK", kv(d, s, "tile_k")) +
+                               def("WM", kv(d, s, "waves_m")) + def("WN", kv(d, s, "waves_n")) +
+                               def("MF", kv(d, s, "mfma")) + def("STAGES", kv(d, s, "stages")) +
+                               def("ORDER", kv(d, s, "order")) + def("OCC", kv(d, s, "occ")) + def("BIAS", bias) +
+                               def("F32", (d->flags & RC_FLAG_OUT_F32) != 0) + def("GATED", gated)};
+            k.grid = dim3((unsigned)(((D[0] + tm - 1) / tm) * ((D[1] + tn - 1) / tn)), 1, 1);
+            k.block = dim3(nt, 1, 1);
+            k.flops = rc_op_flops(d);
+            const long long M = D[0];
+            const int N = (int)D[1], K = (int)D[2];
+            k.bind = [=](const rc_args *a, char *, ArgBlob &b) {
+                put(b, GemmI8Args{a->in[0], a->in[2], gated ? a->in[4] : nullptr, a->in[1], a->in[3],
+                                  gated ? a->in[5] : nullptr, bias ? a->in[4] : nullptr, a->out[0], M, N, K});
+            };
+            p.kerns.push_back(k);
+            p.dominant = 0;
+            break;
+        }
         default: return fail(RC_ERR_UNSUPPORTED, "unknown operator kind");
     }
     for (auto &k : p.kerns) {
@@ -841,15 +903,26 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
     return RC_OK;
 }
 
-int n_inputs(int kind) {
-    switch (kind) {
+int n_inputs(const rc_op_desc &d) {
+    switch (d.kind) {
         case RC_OP_GEMM_F32: return 2;
         case RC_OP_ATTENTION: return 3;
         case RC_OP_GATED_MLP: return 4;
         case RC_OP_MOE: return 6;
         case RC_OP_CONV2D: return 3;
+        case RC_OP_RMSNORM_I8: return (d.flags & RC_FLAG_RESIDUAL) ? 3 : 2;
+        case RC_OP_QUANT_I8: return 1;
+        case RC_OP_GEMM_I8: return (d.flags & RC_FLAG_GATED) ? 6 : (d.flags & RC_FLAG_BIAS) ? 5 : 4;
     }
     return 0;
+}
+
+int n_outputs(const rc_op_desc &d) {
+    switch (d.kind) {
+        case RC_OP_RMSNORM_I8: return (d.flags & RC_FLAG_RESIDUAL) ? 3 : 2;
+        case RC_OP_QUANT_I8: return 2;
+    }
+    return 1;
 }
 
 rc_status hip_fail(hipError_t e, const char *what) {
@@ -1005,6 +1078,7 @@ rc_status rc_plan_create(const rc_op_desc *d, const rc_schedule *s, rc_plan **ou
     p->sched = *s;
     rc_status r = describe(d, s, *p);
     if (r != RC_OK) return r;
+    if (hipGetDevice(&p->device) != hipSuccess) p->device = -1;
     for (auto &k : p->kerns) {
         std::vector<char> code;
         std::string key;
@@ -1082,14 +1156,29 @@ rc_status rc_time_release(void) {
 }
 
 static rc_status check_args(const rc_plan *p, const rc_args *a, void *ws, size_t ws_bytes) {
-    if (!p || !a || a->struct_size < sizeof(rc_args)) return fail(RC_ERR_INVALID_ARGUMENT, "null plan or args");
-    int ni = n_inputs(p->desc.kind);
+    if (!p || !a) return fail(RC_ERR_INVALID_ARGUMENT, "null plan or args");
+    const int no = n_outputs(p->desc);
+    // a block without out[2] and out[3] serves operators that have none
+    const size_t least = no > 2 ? sizeof(rc_args) : offsetof(rc_args, out) + 2 * sizeof(void *);
+    if (a->struct_size < least) return fail(RC_ERR_INVALID_ARGUMENT, "rc_args struct_size too small");
+    int ni = n_inputs(p->desc);
     for (int i = 0; i < ni; ++i) {
         if (!a->in[i]) return fail(RC_ERR_INVALID_ARGUMENT, "input " + std::to_string(i) + " is NULL");
         if ((uintptr_t)a->in[i] & 15) return fail(RC_ERR_MISALIGNED, "input " + std::to_string(i) + " is not 16-byte aligned");
     }
-    if (!a->out[0]) return fail(RC_ERR_INVALID_ARGUMENT, "output is NULL");
-    if ((uintptr_t)a->out[0] & 15) return fail(RC_ERR_MISALIGNED, "output is not 16-byte aligned");
+    auto name = [no](int i) { return no > 1 ? "output " + std::to_string(i) : std::string("output"); };
+    for (int i = 0; i < no; ++i) {
+        if (!a->out[i]) return fail(RC_ERR_INVALID_ARGUMENT, name(i) + " is NULL");
+        if ((uintptr_t)a->out[i] & 15) return fail(RC_ERR_MISALIGNED, name(i) + " is not 16-byte aligned");
+    }
+    if (p->desc.kind >= RC_OP_RMSNORM_I8) {
+        int dev = -1;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+        if (dev != p->device)
+            return fail(RC_ERR_INVALID_ARGUMENT, "the plan is of device " + std::to_string(p->device) +
+                                                     ", the current device is " + std::to_string(dev));
+    }
     if (p->workspace) {
         if (!ws || ws_bytes < p->workspace)
             return fail(RC_ERR_INVALID_ARGUMENT, "workspace of " + std::to_string(p->workspace) + " bytes required");

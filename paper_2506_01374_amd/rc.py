@@ -23,8 +23,10 @@ STATUS = {0: "RC_OK", 1: "RC_ERR_INVALID_ARGUMENT", 2: "RC_ERR_ILLEGAL_SCHEDULE"
  RC_ERR_OUT_OF_MEMORY, RC_ERR_MISALIGNED, RC_ERR_BUDGET) = range(1, 9)
 
 RC_OP_GEMM_F32, RC_OP_ATTENTION, RC_OP_GATED_MLP, RC_OP_MOE, RC_OP_CONV2D = 1, 2, 3, 4, 5
+RC_OP_RMSNORM_I8, RC_OP_QUANT_I8, RC_OP_GEMM_I8 = 6, 7, 8
 RC_FLAG_CAUSAL = 1
 RC_FLAG_NO_ACT = 2
+RC_FLAG_RESIDUAL, RC_FLAG_BIAS, RC_FLAG_OUT_F32, RC_FLAG_GATED = 4, 8, 16, 32
 RC_POLICY_RANDOM, RC_POLICY_UCT, RC_POLICY_EXHAUSTIVE = 0, 1, 2
 MAX_DIMS, MAX_KNOBS = 8, 32
 
@@ -32,7 +34,7 @@ MAX_DIMS, MAX_KNOBS = 8, 32
 class rc_op_desc(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("kind", ctypes.c_int32),
                 ("dim", ctypes.c_int64 * MAX_DIMS), ("flags", ctypes.c_int32),
-                ("reserved", ctypes.c_int32)]
+                ("eps", ctypes.c_float)]
 
 
 class rc_schedule(ctypes.Structure):
@@ -53,7 +55,7 @@ class rc_kernel_info(ctypes.Structure):
 
 class rc_args(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("in_", ctypes.c_void_p * 8),
-                ("out", ctypes.c_void_p * 2)]
+                ("out", ctypes.c_void_p * 4)]
 
 
 class rc_time_opts(ctypes.Structure):
@@ -108,6 +110,7 @@ _SIGS = [
                                       ctypes.POINTER(ctypes.c_int32), ctypes.c_int32,
                                       ctypes.POINTER(ctypes.c_int32)]),
     ("rc_default_schedule", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule)]),
+    ("rc_suggest_schedule", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule)]),
     ("rc_validate", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule),
                                    ctypes.c_char_p, ctypes.c_size_t]),
     ("rc_apply", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule),
@@ -224,13 +227,21 @@ def _check(st: int, where: str) -> None:
 # ---------------------------------------------------------------------------
 
 class Op:
-    """An operator descriptor (the input program P0)."""
+    """An operator descriptor (the input program P0).  ``eps`` is the
+    RC_OP_RMSNORM_I8 descriptor's (None: rc_op_init's default)."""
 
-    def __init__(self, kind: int, dims: Sequence[int], flags: int = 0):
+    def __init__(self, kind: int, dims: Sequence[int], flags: int = 0, eps: Optional[float] = None):
         self.desc = rc_op_desc()
         arr = (ctypes.c_int64 * len(dims))(*dims)
         _check(lib().rc_op_init(ctypes.byref(self.desc), kind, arr, len(dims), flags), "rc_op_init")
         self.kind, self.dims, self.flags = kind, tuple(int(d) for d in dims), flags
+        if eps is not None:
+            if kind != RC_OP_RMSNORM_I8:
+                raise ValueError("eps is a parameter of RC_OP_RMSNORM_I8 only")
+            self.desc.eps = eps
+            if not (math.isfinite(self.desc.eps) and self.desc.eps >= 2.0 ** -100):
+                raise ValueError("eps must be finite and at least 2^-100")
+        self.eps = self.desc.eps
 
     @property
     def ref(self):
@@ -271,6 +282,12 @@ class Op:
     def default(self) -> "Schedule":
         s = rc_schedule()
         _check(lib().rc_default_schedule(self.ref, ctypes.byref(s)), "rc_default_schedule")
+        return Schedule(self, s)
+
+    def suggest(self) -> "Schedule":
+        """A legal schedule by rules on the sizes (the 8-bit kinds)."""
+        s = rc_schedule()
+        _check(lib().rc_suggest_schedule(self.ref, ctypes.byref(s)), "rc_suggest_schedule")
         return Schedule(self, s)
 
     def schedule(self, **knobs) -> "Schedule":
@@ -423,11 +440,11 @@ def _stream_ptr(stream) -> int:
     return int(torch.cuda.current_stream().cuda_stream)
 
 
-# rc_launch taking its rc_args block as bytes (struct_size, in[8], out[2]):
+# rc_launch taking its rc_args block as bytes (struct_size, in[8], out[4]):
 # packing them is cheaper than filling a ctypes structure field by field.
 # With the stream read as above, back-to-back launches of the fp32 GEMM 128 x
 # 128 x 128 take 4.3 us each instead of 6.9; the kernel itself takes 3.4.
-_ARGS_FORMAT = struct.Struct("@I8P2P")
+_ARGS_FORMAT = struct.Struct("@I8P4P")
 _launch_fn = None
 
 
@@ -447,7 +464,60 @@ def _pack_args(inputs: Iterable, output) -> bytes:
     if len(ptrs) > 8:
         raise IndexError("an operator takes at most 8 inputs")
     ptrs += [0] * (8 - len(ptrs))
-    return _ARGS_FORMAT.pack(_ARGS_FORMAT.size, *ptrs, _ptr(output), 0)
+    if isinstance(output, (tuple, list)):
+        ptrs += [_ptr(t) for t in output]
+        if len(ptrs) > 12:
+            raise IndexError("an operator has at most 4 outputs")
+        ptrs += [0] * (12 - len(ptrs))
+        return _ARGS_FORMAT.pack(_ARGS_FORMAT.size, *ptrs)
+    return _ARGS_FORMAT.pack(_ARGS_FORMAT.size, *ptrs, _ptr(output), 0, 0, 0)
+
+
+def _i8_tensors(op: Op):
+    """(name, dtype, shape) of the inputs and of the outputs of an 8-bit
+    operator, which Plan checks at each launch: a wrong type or size would
+    read or write past a buffer."""
+    import torch
+    bf16, f32, i8 = torch.bfloat16, torch.float32, torch.int8
+    if op.kind == RC_OP_GEMM_I8:
+        m, n, k = op.dims
+        ins = [("A", i8, (m, k)), ("sa", f32, (m,)), ("B", i8, (n, k)), ("sb", f32, (n,))]
+        if op.flags & RC_FLAG_BIAS:
+            ins.append(("bias", f32, (n,)))
+        if op.flags & RC_FLAG_GATED:
+            ins += [("up weight", i8, (n, k)), ("up scales", f32, (n,))]
+        return ins, [("out", f32 if op.flags & RC_FLAG_OUT_F32 else bf16, (m, n))]
+    t, c = op.dims
+    ins, outs = [("x", bf16, (t, c))], [("q", i8, (t, c)), ("scale", f32, (t,))]
+    if op.kind == RC_OP_RMSNORM_I8:
+        ins.append(("w", bf16, (c,)))
+        if op.flags & RC_FLAG_RESIDUAL:
+            ins.append(("r", bf16, (t, c)))
+            outs.append(("h", bf16, (t, c)))
+    return ins, outs
+
+
+def _check_tensors(tensors, device: int, inputs, output, workspace, stream):
+    """The inputs and outputs of an 8-bit operator as lists, checked against
+    ``tensors`` (of _i8_tensors) and the plan's device; ValueError otherwise."""
+    inputs = list(inputs)
+    output = list(output) if isinstance(output, (tuple, list)) else [output]
+    for what, got, want in (("inputs", inputs, tensors[0]), ("outputs", output, tensors[1])):
+        if len(got) != len(want):
+            raise ValueError(f"{what}: the operator has {len(want)} ({', '.join(w[0] for w in want)}), got {len(got)}")
+        for t, (name, dtype, shape) in zip(got, want):
+            if t is None or t.dtype != dtype or t.shape != shape:
+                is_ = "None" if t is None else f"{t.dtype} {tuple(t.shape)}"
+                raise ValueError(f"{name} must be {dtype} {shape}, got {is_}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            if t.get_device() != device:
+                raise ValueError(f"{name} is on {t.device}, the plan on cuda:{device}")
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError(f"the workspace is on {workspace.device}, the plan on cuda:{device}")
+    if stream is not None and stream.device.index != device:
+        raise ValueError(f"the stream is of {stream.device}, the plan on cuda:{device}")
+    return inputs, output
 
 
 class Plan:
@@ -463,6 +533,14 @@ class Plan:
         nk, dom = ctypes.c_int32(), ctypes.c_int32()
         _check(lib().rc_plan_kernels(h, ctypes.byref(nk), ctypes.byref(dom)), "rc_plan_kernels")
         self.nkernels, self.dominant = nk.value, dom.value
+        self._tensors = None
+        if op.kind >= RC_OP_RMSNORM_I8:
+            import torch
+            self._device = torch.cuda.current_device()
+            self._tensors = _i8_tensors(op)
+
+    def _checked(self, inputs, output, workspace, stream=None):
+        return _check_tensors(self._tensors, self._device, inputs, output, workspace, stream)
 
     def __del__(self):
         if getattr(self, "h", None) and _lib is not None:
@@ -494,13 +572,16 @@ class Plan:
         a.struct_size = ctypes.sizeof(rc_args)
         for i, t in enumerate(inputs):
             a.in_[i] = _ptr(t)
-        a.out[0] = _ptr(output)
+        for i, t in enumerate(output if isinstance(output, (tuple, list)) else (output,)):
+            a.out[i] = _ptr(t)
         return a
 
     class Prepared:
         """Argument block, workspace and stream of repeated launches, built once."""
 
         def __init__(self, plan, inputs, output, workspace, stream):
+            if plan._tensors:
+                inputs, output = plan._checked(inputs, output, workspace, stream)
             self.plan = plan
             self.args = plan._args(inputs, output)
             self.keep = (list(inputs), output, workspace)       # keep tensors alive
@@ -526,6 +607,10 @@ class Plan:
         return Plan.Prepared(self, inputs, output, workspace, stream)
 
     def launch(self, inputs, output, workspace=None, stream=None) -> None:
+        """rc_launch.  ``output``: a tensor, or a tuple of an operator's
+        several outputs.  Tensors of the 8-bit kinds are checked."""
+        if self._tensors:
+            inputs, output = self._checked(inputs, output, workspace, stream)
         wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
         st = (_launch_fn or _launch_bytes())(self.h, _pack_args(inputs, output), _ptr(workspace), wsz,
                                              _stream_ptr(stream))
@@ -534,12 +619,16 @@ class Plan:
 
     def launch_static(self, inputs, output, stream=None) -> None:
         """rc_launch_static: the workspace is the library's static array."""
+        if self._tensors:
+            inputs, output = self._checked(inputs, output, None, stream)
         a = self._args(inputs, output)
         _check(lib().rc_launch_static(self.h, ctypes.byref(a), _stream_ptr(stream)), "rc_launch_static")
 
     def launch_timed(self, inputs, output, events, workspace=None, stream=None) -> None:
         """events: list of nkernels + 1 torch.cuda.Event(enable_timing=True),
         each already created (recorded once), since torch creates events lazily."""
+        if self._tensors:
+            inputs, output = self._checked(inputs, output, workspace, stream)
         a = self._args(inputs, output)
         wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
         handles = [int(e.cuda_event) for e in events]
@@ -551,6 +640,8 @@ class Plan:
 
     def time(self, inputs, output, workspace=None, warmup=3, repeat=20, flush=True,
              stream=None) -> rc_timing:
+        if self._tensors:
+            inputs, output = self._checked(inputs, output, workspace, stream)
         a = self._args(inputs, output)
         o = rc_time_opts()
         lib().rc_time_opts_init(ctypes.byref(o))

@@ -1,0 +1,88 @@
+"""Sizes and schedules of the 8-bit integer operators' tests."""
+from __future__ import annotations
+
+import itertools
+
+from paper_2506_01374_amd import rc
+
+R, B, F, G = rc.RC_FLAG_RESIDUAL, rc.RC_FLAG_BIAS, rc.RC_FLAG_OUT_F32, rc.RC_FLAG_GATED
+
+# (rows, columns): single elements, rows around a vector, a wave's and a
+# workgroup's step, odd widths, more rows than a workgroup takes
+ROWS_DIMS = [(1, 1), (3, 2), (5, 7), (1, 8), (4, 9), (2, 63), (7, 64), (3, 65), (2, 511), (9, 512), (2, 513), (5, 1001),
+             (3, 2048), (2, 4097), (1, 14336), (2, 16385)]
+ROWS_TEXTS = ["", "vec=8", "vec=4,rows=2", "waves=2,vec=2", "vec=8,held=1", "vec=8,held=2", "waves=4,vec=8,held=2,rows=2",
+              "waves=4,vec=8,held=4", "waves=8,vec=8,held=4", "waves=16,vec=8,held=1", "waves=16,vec=8,held=4",
+              "vec=2,held=1,rows=4", "waves=16,vec=1", "waves=2,vec=8,rows=8"]
+
+
+def rows_jobs():
+    """(dims, schedule text) of every size with its legal schedules."""
+    jobs = []
+    for dims in ROWS_DIMS:
+        op = rc.Op(rc.RC_OP_QUANT_I8, dims)
+        texts = [t for t in ROWS_TEXTS if op.from_string(t).validate() == ""]
+        jobs += [(dims, t) for t in dict.fromkeys(texts + [str(op.suggest())])]
+    return jobs
+
+
+_TILE = "tile_m={},tile_n={},tile_k={},waves_m={},waves_n={},mfma={},stages={},order={},occ={}"
+GEMM_TEXTS = [_TILE.format(*t) for t in (
+    (16, 16, 64, 1, 1, 16, 1, 0, 1), (32, 64, 64, 2, 2, 16, 1, 1, 1), (64, 64, 128, 2, 2, 32, 1, 1, 2),
+    (128, 128, 128, 2, 4, 16, 1, 1, 1), (128, 64, 64, 4, 1, 32, 1, 0, 1), (256, 128, 64, 2, 4, 16, 1, 1, 1),
+    (64, 32, 256, 4, 2, 16, 1, 1, 1))]
+
+# (M, N, K): one of each, around 16 and the tiles, K around a chunk, an MFMA
+# step and the K tiles, rows that start on no alignment
+GEMM_DIMS = [(1, 1, 1), (1, 17, 16), (2, 3, 15), (15, 16, 17), (16, 100, 64), (17, 33, 65), (1, 260, 1000), (33, 64, 63),
+             (64, 129, 127), (65, 128, 128), (100, 61, 129), (130, 257, 256), (257, 130, 257), (300, 272, 400),
+             (128, 256, 1040)]
+
+
+def gemm_jobs(flags):
+    jobs = []
+    for dims in GEMM_DIMS:
+        op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
+        texts = [t for t in GEMM_TEXTS if op.from_string(t).validate() == ""]
+        jobs += [(dims, t) for t in dict.fromkeys(texts + [str(op.suggest())])]
+    return jobs
+
+
+def suggested(kind, flags, rows, cols, depths=(None,)):
+    """The different schedules suggested over a grid of sizes, each with a
+    size that it is suggested for."""
+    found = {}
+    for dims in itertools.product(rows, cols, depths):
+        op = rc.Op(kind, dims if dims[2] is not None else dims[:2], flags)
+        found.setdefault(str(op.suggest()), op)
+    return [(op, text) for text, op in found.items()]
+
+
+_STEPS = [1, 2, 4, 8, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512, 768, 1000, 1536, 2048, 4096, 8192]
+_WIDE = [1, 2, 3, 8, 16, 32, 64, 128, 200, 256, 512, 777, 1024, 1536, 2048, 4096, 6144, 8192, 14336, 16384, 28672, 65536, 131072]
+
+
+def suggested_jobs():
+    """(op, schedule text): every code object that a suggested schedule can
+    ask for (the kernels of these kinds take sizes as arguments)."""
+    jobs = []
+    for kind, flags in ((rc.RC_OP_QUANT_I8, 0), (rc.RC_OP_RMSNORM_I8, 0), (rc.RC_OP_RMSNORM_I8, R)):
+        jobs += suggested(kind, flags, _STEPS, _WIDE)
+    for flags in (0, B, F, B | F, G):
+        jobs += suggested(rc.RC_OP_GEMM_I8, flags, _STEPS, _WIDE, [1, 16, 64, 100, 128, 900, 1024, 4096, 4100, 14336, 131071])
+    return jobs
+
+
+def compile_jobs():
+    """(op, [schedules]) for ahead-of-time compilation."""
+    jobs = [(op, [op.from_string(t)]) for op, t in suggested_jobs()]
+    for dims, text in rows_jobs():
+        for kind, flags in ((rc.RC_OP_QUANT_I8, 0), (rc.RC_OP_RMSNORM_I8, 0), (rc.RC_OP_RMSNORM_I8, R)):
+            op = rc.Op(kind, dims, flags)
+            jobs.append((op, [op.from_string(text)]))
+    for flags in (0, B, F, B | F, G):
+        for dims, text in gemm_jobs(flags):
+            op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
+            jobs.append((op, [op.from_string(text)]))
+    # one job a code object: a schedule and the flags, whatever the sizes
+    return list({(op.kind, op.flags, str(s[0])): (op, s) for op, s in jobs}.values())
