@@ -320,7 +320,8 @@ rc_status rc_plan_kernel_flops(const rc_plan *p, int32_t kernel, double *flops);
  *     [2][T][tail columns], "down.tail.partials" fp32 [2][T][tail columns];
  *   unfused epilogues: "gate.f32", "up.f32" or "pre.f32" (fp32 [rows][cols]);
  *   RC_OP_ATTENTION with chunk > 0: "partials"; RC_OP_GEMM_F32 streaming
- *   stage with splits > 1: "splitk.partials".
+ *   stage with splits > 1: "splitk.partials"; RC_OP_GEMM_I8 with splits > 1:
+ *   "splitk.partials" int32 [splits][M][1, or 2 gated][N rounded up to 4].
  * RC_ERR_INVALID_ARGUMENT if the plan has no part of that name.  (The
  * routing preparation of the MoE layer of Sec. 4.1 is integer index work:
  * these parts let it be checked exactly.) */

@@ -140,10 +140,14 @@ static std::vector<KnobDef> gemm_i8_knobs() {
         {"tile_k", "TileSize", {64, 128, 256}, 64},
         {"waves_m", "Parallel", {1, 2, 4}, 1},
         {"waves_n", "Parallel", {1, 2, 4}, 1},
+        {"waves_k", "Parallel", {1, 2, 4, 8, 16}, 1},         // waves that share a tile's K
         {"mfma", "TileSize", {16, 32}, 16},                   // MFMA instruction shape
-        {"stages", "ComputeLocation", {1}, 1},                // staging of the K tiles
+        // staging of the K tiles: double buffer / direct-to-LDS ring / straight to registers
+        {"stages", "ComputeLocation", {1, 2, 3}, 1},
         {"order", "Parallel", {0, 1}, 0},                     // tile order: plain / XCD-grouped bands
         {"occ", "Parallel", {1, 2}, 1},                       // waves per SIMD to budget registers for
+        {"splits", "Parallel", {1, 2, 4, 8, 16}, 1},          // K splits across workgroups
+        {"tail", "Parallel", {0, 1}, 0},                      // half-height tiles in a last, partial round
     };
 }
 
@@ -238,6 +242,30 @@ int gemm_ring_stages(int tm, int tn, int tk, int nb, int waves, int occ) {
     const int64_t wgs = std::max<int64_t>(1, (occ * 4 + waves - 1) / waves);
     const int64_t lpt = std::max<int64_t>(1, sb / 1024 / waves);
     return (int)std::min<int64_t>(std::min<int64_t>(12, LDS_LIMIT / (wgs * sb)), 63 / lpt + 2);
+}
+
+// The same for the int8 ring (elements are bytes).
+int gemm_i8_ring_stages(int tm, int tn, int tk, int waves, int occ) {
+    const int64_t sb = (int64_t)(tm + tn) * tk;
+    const int64_t wgs = std::max<int64_t>(1, (occ * 4 + waves - 1) / waves);
+    const int64_t lpt = std::max<int64_t>(1, sb / 1024 / waves);
+    return (int)std::min<int64_t>(std::min<int64_t>(12, LDS_LIMIT / (wgs * sb)), 63 / lpt + 2);
+}
+
+// K of one split of an int8 product: whole K tiles, the last split's fewer.
+int64_t gemm_i8_split_k(int64_t K, int tk, int splits) {
+    const int64_t tiles = (K + tk - 1) / tk;
+    return splits > 1 ? (tiles + splits - 1) / splits * tk : K;
+}
+
+// Tiles of an int8 product's last, partial round of workgroups, if twice as
+// many of half the height still are one round (else 0): the round then takes
+// half its time.
+int64_t gemm_i8_tail_tiles(int64_t tiles, int tm, int tn, int tk, int waves, int occ) {
+    const int64_t lds = (int64_t)gemm_i8_ring_stages(tm, tn, tk, waves, occ) * (tm + tn) * tk;
+    const int64_t slots = 256 * std::max<int64_t>(1, std::min<int64_t>(LDS_LIMIT / lds, occ * 4 / waves));
+    const int64_t r = tiles % slots;
+    return tiles > slots && 2 * r <= slots ? r : 0;
 }
 
 // Column split of a GEMM block whose workgroups end in a partial round:
@@ -431,8 +459,8 @@ static std::string check_rows_i8(const rc_op_desc *d, const rc_schedule *s) {
 static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     const int nb = (d->flags & RC_FLAG_GATED) ? 2 : 1;
     const int tm = kv(d, s, "tile_m"), tno = kv(d, s, "tile_n"), tn = nb * tno, tk = kv(d, s, "tile_k");
-    const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), mf = kv(d, s, "mfma");
-    const int occ = kv(d, s, "occ");
+    const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), wk = kv(d, s, "waves_k"), mf = kv(d, s, "mfma");
+    const int st = kv(d, s, "stages"), occ = kv(d, s, "occ"), sp = kv(d, s, "splits"), tail = kv(d, s, "tail");
     const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
     const int nt = 64 * wm * wn;
     if (tm % wm || (tm / wm) % mf) return fmt("tile_m/waves_m = %d/%d is not a multiple of the %dx%d MFMA", tm, wm, mf, mf);
@@ -441,16 +469,54 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     if (redundant_tile(d, "tile_m", tm, M)) return fmt("tile_m %d: tile_m %d already covers M = %lld", tm, tm / 2, (long long)M);
     if (redundant_tile(d, "tile_n", tno, N)) return fmt("tile_n %d: tile_n %d already covers N = %lld", tno, tno / 2, (long long)N);
     if (redundant_tile(d, "tile_k", tk, K)) return fmt("tile_k %d: tile_k %d already covers K = %lld", tk, tk / 2, (long long)K);
-    if (((M + tm - 1) / tm) * ((N + tno - 1) / tno) > INT32_MAX) return "the tiles exceed the grid's 2^31 - 1";
+    if (sp * ((M + tm - 1) / tm) * ((N + tno - 1) / tno) > INT32_MAX) return "the tiles exceed the grid's 2^31 - 1";
     const int64_t acc = (int64_t)tm * tn / nt;
     if (acc > 256) return fmt("%lld accumulators per lane exceed 256", (long long)acc);
     if (occ > 1 && acc > 512 / occ - 32) return fmt("%lld accumulators leave no registers at %d waves/SIMD", (long long)acc, occ);
-    // register staging of the next tile next to the accumulators
+    if (sp > 1) {
+        if (st == 3) return "the streaming stage (3) splits K over waves (waves_k), not over workgroups";
+        if ((sp - 1) * gemm_i8_split_k(K, tk, sp) >= K)
+            return fmt("%d splits of K = %lld in tiles of %d leave one empty", sp, (long long)K, tk);
+        if ((M * ((N + 3) / 4) + 255) / 256 > INT32_MAX) return "the outputs exceed the joining launch's grid";
+    }
+    if (wk > 1 && st != 3) return "waves share a tile's K in the streaming stage (3) only";
     const int64_t stage_bytes = (int64_t)(tm + tn) * tk;
-    const int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 4;
-    if (regs > 384) return fmt("%lld accumulator and staging registers per lane exceed 384", (long long)regs);
-    const int64_t lds = 2 * stage_bytes;
-    const int64_t wgs = occ > 1 ? (occ * 4 + wm * wn - 1) / (wm * wn) : 1;
+    int64_t lds = 2 * stage_bytes;
+    int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 4;     // register staging of the next tile
+    int64_t waves = (int64_t)wm * wn;
+    if (st == 2) {
+        if (K % 16) return fmt("the direct-to-LDS ring moves 16 aligned bytes a lane: K = %lld is no multiple of 16", (long long)K);
+        if ((int64_t)tm * tk % (1024 * waves)) return fmt("A tile is not a whole number of 1 KiB wave-loads for %lld waves", (long long)waves);
+        if ((int64_t)tn * tk % (1024 * waves)) return fmt("B tile is not a whole number of 1 KiB wave-loads for %lld waves", (long long)waves);
+        const int ns = gemm_i8_ring_stages(tm, tn, tk, (int)waves, occ);
+        if (ns < 3) return fmt("the LDS holds %d ring stages of this tile (needs 3)", ns);
+        const int64_t last = K - (sp - 1) * gemm_i8_split_k(K, tk, sp);     // K of the last split
+        if ((tk / (mf == 16 ? 64 : 32)) % 2 && (last + tk - 1) / tk < ns - 1)
+            return fmt("a ring of %d stages with an odd number of MFMA steps a tile needs %d K tiles", ns, ns - 1);
+        lds = ns * stage_bytes;
+        // one set of A fragments, two of the weight's
+        regs = acc + 4 * (tm / wm / mf + 2 * (tn / wn / mf));
+    } else if (st == 3) {
+        if (wm != 1 || wn != 1 || mf != 16) return "the streaming stage takes one wave column of 16x16 MFMAs (waves_m 1, waves_n 1)";
+        if (tm > 64 || tn > 128) return fmt("the streaming stage takes at most 64 rows and 128 weight rows (%d, %d)", tm, tn);
+        if (wk > 1 && (int64_t)wk / 2 * tk >= K) return fmt("waves_k %d: half of them already take all of K = %lld", wk, (long long)K);
+        waves = wk;
+        lds = (int64_t)wk * (tm / 16) * (tn / 16) * 1024;
+        // two batches of fragments
+        regs = acc + 2 * (tk / 64) * (tm / 16 + tn / 16) * 4;
+    }
+    if (tail) {
+        if (st != 2 || sp != 1) return "half-height tail tiles need the ring (stages 2) and no K splits";
+        if ((tm / 2 / wm) % mf || tm / 2 % wm || (int64_t)tm / 2 * tk % (1024 * waves))
+            return fmt("tail: the half-height tile of %d rows does not split over the waves", tm / 2);
+        if (!gemm_i8_tail_tiles(((M + tm - 1) / tm) * ((N + tno - 1) / tno), tm, tn, tk, (int)waves, occ))
+            return "tail: no partial round of workgroups that half-height tiles shorten";
+    }
+    // registers of a lane: all waves of a workgroup are resident together
+    const int64_t per_simd = std::max<int64_t>(occ, (waves + 3) / 4);
+    if (regs + 24 > 512 / per_simd)
+        return fmt("%lld accumulator and operand registers per lane leave too few at %lld waves/SIMD", (long long)regs, (long long)per_simd);
+    const int64_t wgs = occ > 1 ? (occ * 4 + waves - 1) / waves : 1;
     if (wgs * lds > LDS_LIMIT) return fmt("%lld workgroups of %lld B LDS do not fit a CU", (long long)wgs, (long long)lds);
     return "";
 }
@@ -696,19 +762,29 @@ static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
     set_knob(d, s, "rows", rows);
 }
 
-// The largest of a few tiles that still gives every CU one.
 static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
+    auto set = [&](const char *name, int v) { set_knob(d, s, name, v); };
+    if (M <= 16) {
+        set("stages", 3);
+        set("tile_m", 16);
+        set("tile_n", 16);
+        set("tile_k", K >= 256 ? 256 : K > 64 ? 128 : 64);
+        int wk = 8;
+        while (wk > 1 && (int64_t)wk / 2 * (K >= 256 ? 256 : K > 64 ? 128 : 64) >= K) wk /= 2;
+        set("waves_k", wk);
+        return;
+    }
     static const int tiles[][4] = {{128, 128, 2, 2}, {64, 64, 2, 2}, {32, 32, 2, 2}, {16, 16, 1, 1}};
     for (const int *t : tiles) {
-        set_knob(d, s, "tile_m", t[0]);
-        set_knob(d, s, "tile_n", t[1]);
-        set_knob(d, s, "waves_m", t[2]);
-        set_knob(d, s, "waves_n", t[3]);
+        set("tile_m", t[0]);
+        set("tile_n", t[1]);
+        set("waves_m", t[2]);
+        set("waves_n", t[3]);
         if (((M + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) >= 256 && check_schedule(d, s).empty()) break;
     }
-    set_knob(d, s, "tile_k", K > 64 ? 128 : 64);
-    set_knob(d, s, "order", 1);
+    set("tile_k", K > 64 ? 128 : 64);
+    set("order", 1);
 }
 
 }  // namespace rc

@@ -31,6 +31,12 @@ int32_t kv(const rc_op_desc *d, const rc_schedule *s, const char *name);
 // Depth of the direct-to-LDS ring of bf16 GEMM stages 7.
 int gemm_ring_stages(int tm, int tn, int tk, int nb, int waves, int occ);
 
+// The same for the int8 product's ring (stages 2), the K of one of its splits,
+// and the tiles that it runs at half height.
+int gemm_i8_ring_stages(int tm, int tn, int tk, int waves, int occ);
+int64_t gemm_i8_split_k(int64_t K, int tk, int splits);
+int64_t gemm_i8_tail_tiles(int64_t tiles, int tm, int tn, int tk, int waves, int occ);
+
 // Column split of a GEMM block over two launches (the "tail" knob).
 bool gemm_tail_split(int tm, int tn, int tk, int nb, int waves, int occ, int st, int64_t M, int64_t N,
                      int64_t *main_cols, int64_t *tail_cols);

@@ -76,9 +76,9 @@ struct RowsI8Args {
 };
 struct GemmI8Args {
     const void *A, *B0, *B1, *sa, *sb0, *sb1, *bias;
-    void *C;
+    void *C, *P;
     long long M;
-    int N, K;
+    int N, K, KP, tail;
 };
 
 // A kernel's by-value argument block (fixed storage: launching allocates
@@ -867,33 +867,48 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
         }
         case RC_OP_GEMM_I8: {
             const bool gated = d->flags & RC_FLAG_GATED, bias = d->flags & RC_FLAG_BIAS;
-            const int tm = kv(d, s, "tile_m"), tn = kv(d, s, "tile_n");
-            const int nt = 64 * kv(d, s, "waves_m") * kv(d, s, "waves_n");
+            const int tm = kv(d, s, "tile_m"), tn = kv(d, s, "tile_n"), tk = kv(d, s, "tile_k");
+            const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), wk = kv(d, s, "waves_k");
+            const int st = kv(d, s, "stages"), sp = kv(d, s, "splits"), occ = kv(d, s, "occ");
+            const int tnw = gated ? 2 * tn : tn;              // weight rows of a tile
             Kern k;
             // sizes are arguments: plans of all sizes share the code object
             k.src = Source{SRC_gemm_i8, "rc_gemm_i8",
-                           def("TM", tm) + def("TN", gated ? 2 * tn : tn) + def("TK", kv(d, s, "tile_k")) +
-                               def("WM", kv(d, s, "waves_m")) + def("WN", kv(d, s, "waves_n")) +
-                               def("MF", kv(d, s, "mfma")) + def("STAGES", kv(d, s, "stages")) +
-                               def("ORDER", kv(d, s, "order")) + def("OCC", kv(d, s, "occ")) + def("BIAS", bias) +
-                               def("F32", (d->flags & RC_FLAG_OUT_F32) != 0) + def("GATED", gated)};
-            k.grid = dim3((unsigned)(((D[0] + tm - 1) / tm) * ((D[1] + tn - 1) / tn)), 1, 1);
-            k.block = dim3(nt, 1, 1);
+                           def("TM", tm) + def("TN", tnw) + def("TK", tk) + def("WM", wm) + def("WN", wn) +
+                               def("WK", wk) + def("MF", kv(d, s, "mfma")) + def("STAGES", st) +
+                               def("ORDER", kv(d, s, "order")) + def("OCC", occ) + def("SPLITS", sp) +
+                               def("TAIL", kv(d, s, "tail")) +
+                               def("BIAS", bias) + def("F32", (d->flags & RC_FLAG_OUT_F32) != 0) + def("GATED", gated)};
+            if (st == 2) k.src.defines += def("NSTAGE", gemm_i8_ring_stages(tm, tnw, tk, wm * wn, occ));
+            const int64_t tiles = ((D[0] + tm - 1) / tm) * ((D[1] + tn - 1) / tn);
+            const int tail = kv(d, s, "tail") ? (int)gemm_i8_tail_tiles(tiles, tm, tnw, tk, wm * wn, occ) : 0;
+            k.grid = dim3((unsigned)(tiles * sp + tail), 1, 1);
+            k.block = dim3(64 * wm * wn * wk, 1, 1);
             k.flops = rc_op_flops(d);
             const long long M = D[0];
-            const int N = (int)D[1], K = (int)D[2];
-            k.bind = [=](const rc_args *a, char *, ArgBlob &b) {
+            const int N = (int)D[1], K = (int)D[2], KP = (int)gemm_i8_split_k(K, tk, sp);
+            const size_t offP = sp > 1 ? ws.add((size_t)sp * M * (gated ? 2 : 1) * ((N + 3) / 4 * 4) * 4, "splitk.partials") : 0;
+            k.bind = [=](const rc_args *a, char *w, ArgBlob &b) {
                 put(b, GemmI8Args{a->in[0], a->in[2], gated ? a->in[4] : nullptr, a->in[1], a->in[3],
-                                  gated ? a->in[5] : nullptr, bias ? a->in[4] : nullptr, a->out[0], M, N, K});
+                                  gated ? a->in[5] : nullptr, bias ? a->in[4] : nullptr, a->out[0],
+                                  sp > 1 ? w + offP : nullptr, M, N, K, KP, tail});
             };
             p.kerns.push_back(k);
+            if (sp > 1) {
+                Kern kj = k;
+                kj.flops = 0;
+                kj.src.entry = "rc_gemm_i8_join";
+                kj.grid = dim3((unsigned)((M * ((N + 3) / 4) + 255) / 256), 1, 1);
+                kj.block = dim3(256, 1, 1);
+                p.kerns.push_back(kj);
+            }
             p.dominant = 0;
             break;
         }
         default: return fail(RC_ERR_UNSUPPORTED, "unknown operator kind");
     }
     for (auto &k : p.kerns) {
-        if (k.src.defines.find("#define NSTAGE ") != std::string::npos) k.src.fallback = def("RING_FREE", 1);
+        if (d->kind != RC_OP_GEMM_I8 && k.src.defines.find("#define NSTAGE ") != std::string::npos) k.src.fallback = def("RING_FREE", 1);
         // (only where it changes the source: a spilled variant is not compiled twice to the same code)
         if (k.src.defines.find("#define PINGPONG 1") != std::string::npos)
             k.src.fallback = "#undef PINGPONG\n" + def("PINGPONG", 0);

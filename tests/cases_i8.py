@@ -26,17 +26,40 @@ def rows_jobs():
     return jobs
 
 
-_TILE = "tile_m={},tile_n={},tile_k={},waves_m={},waves_n={},mfma={},stages={},order={},occ={}"
+_TILE = "tile_m={},tile_n={},tile_k={},waves_m={},waves_n={},waves_k={},mfma={},stages={},order={},occ={},splits={}"
 GEMM_TEXTS = [_TILE.format(*t) for t in (
-    (16, 16, 64, 1, 1, 16, 1, 0, 1), (32, 64, 64, 2, 2, 16, 1, 1, 1), (64, 64, 128, 2, 2, 32, 1, 1, 2),
-    (128, 128, 128, 2, 4, 16, 1, 1, 1), (128, 64, 64, 4, 1, 32, 1, 0, 1), (256, 128, 64, 2, 4, 16, 1, 1, 1),
-    (64, 32, 256, 4, 2, 16, 1, 1, 1))]
+    # double buffer
+    (16, 16, 64, 1, 1, 1, 16, 1, 0, 1, 1), (32, 64, 64, 2, 2, 1, 16, 1, 1, 1, 1), (64, 64, 128, 2, 2, 1, 32, 1, 1, 2, 1),
+    (128, 128, 128, 2, 4, 1, 16, 1, 1, 1, 1), (128, 64, 64, 4, 1, 1, 32, 1, 0, 1, 2), (256, 128, 64, 2, 4, 1, 16, 1, 1, 1, 1),
+    (64, 32, 256, 4, 2, 1, 16, 1, 1, 1, 1), (16, 16, 64, 1, 1, 1, 16, 1, 1, 1, 4),
+    # ring
+    (64, 64, 128, 2, 2, 1, 16, 2, 1, 1, 1), (128, 128, 128, 2, 2, 1, 16, 2, 1, 1, 2), (256, 128, 64, 4, 2, 1, 32, 2, 1, 1, 1),
+    (256, 256, 64, 2, 4, 1, 32, 2, 1, 1, 1), (32, 32, 128, 1, 1, 1, 16, 2, 0, 2, 4), (64, 128, 256, 2, 2, 1, 32, 2, 1, 1, 1),
+    (128, 128, 64, 2, 2, 1, 32, 2, 1, 2, 16), (256, 256, 64, 2, 4, 1, 16, 2, 1, 1, 1), (64, 64, 64, 2, 2, 1, 16, 2, 1, 1, 1),
+    (64, 64, 64, 2, 2, 1, 16, 2, 1, 1, 2),
+    # streaming
+    (16, 16, 64, 1, 1, 1, 16, 3, 0, 1, 1), (16, 16, 256, 1, 1, 8, 16, 3, 0, 1, 1), (16, 64, 128, 1, 1, 4, 16, 3, 1, 1, 1),
+    (32, 32, 128, 1, 1, 16, 16, 3, 0, 1, 1), (64, 32, 128, 1, 1, 2, 16, 3, 1, 1, 1), (64, 64, 64, 1, 1, 8, 16, 3, 0, 1, 1))]
 
 # (M, N, K): one of each, around 16 and the tiles, K around a chunk, an MFMA
 # step and the K tiles, rows that start on no alignment
 GEMM_DIMS = [(1, 1, 1), (1, 17, 16), (2, 3, 15), (15, 16, 17), (16, 100, 64), (17, 33, 65), (1, 260, 1000), (33, 64, 63),
              (64, 129, 127), (65, 128, 128), (100, 61, 129), (130, 257, 256), (257, 130, 257), (300, 272, 400),
-             (128, 256, 1040)]
+             (128, 256, 1040), (16, 64, 4096), (70, 96, 2064)]
+
+
+# a last, partial round of workgroups in half-height tiles: with a last row
+# tile that is whole, less than half and more than half, and K of one tile
+# and many
+TAIL_TEXT = "tile_m=32,tile_n=16,tile_k=128,waves_m=1,waves_n=1,mfma=16,stages=2,order=1,occ=1,tail=1"
+TAIL_WIDE = "tile_m=256,tile_n=128,tile_k=64,waves_m=2,waves_n=4,mfma=16,stages=2,order=1,occ=1,tail=1"
+TAIL_DIMS = [(32 * 10, 16 * 110, 128), (32 * 9 + 5, 16 * 140, 400), (32 * 9 + 20, 16 * 120 - 3, 1600), (32 * 20, 16 * 60, 80)]
+TAIL_WIDE_DIMS = [(256 * 5 + 140, 128 * 45, 512), (256 * 6 + 4, 128 * 40 + 10, 1040)]
+
+
+def tail_jobs(flags):
+    jobs = [(dims, TAIL_TEXT) for dims in TAIL_DIMS] + [(dims, TAIL_WIDE) for dims in TAIL_WIDE_DIMS]
+    return [(dims, text) for dims, text in jobs if rc.Op(rc.RC_OP_GEMM_I8, dims, flags).from_string(text).validate() == ""]
 
 
 def gemm_jobs(flags):
@@ -81,7 +104,7 @@ def compile_jobs():
             op = rc.Op(kind, dims, flags)
             jobs.append((op, [op.from_string(text)]))
     for flags in (0, B, F, B | F, G):
-        for dims, text in gemm_jobs(flags):
+        for dims, text in gemm_jobs(flags) + tail_jobs(flags):
             op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
             jobs.append((op, [op.from_string(text)]))
     # one job a code object: a schedule and the flags, whatever the sizes

@@ -261,6 +261,14 @@ def test_gemm(dims, flags):
         check_gemm(dims, flags, 7 * i + flags, text)
 
 
+@pytest.mark.parametrize("flags", [0, B | F, G])
+def test_gemm_with_half_height_tiles(flags):
+    jobs = cases_i8.tail_jobs(flags)
+    assert len(jobs) == len(cases_i8.TAIL_DIMS) + len(cases_i8.TAIL_WIDE_DIMS)
+    for i, (dims, text) in enumerate(jobs):
+        check_gemm(dims, flags, 300 + i, text)
+
+
 @pytest.mark.parametrize("dims", [(3, 40, 131071), (200, 200, 131056), (20, 70, 131071)])
 def test_sums_at_the_limit_of_int32(dims):
     # every product is 128 * 128: 131071 of them are 2^31 - 2^14
