@@ -38,6 +38,12 @@
 #define RPL ((16 / CPR) > 0 ? (16 / CPR) : 1)
 #define TNO (GATED ? TN / 2 : TN)                           // output columns of a tile
 #define WTO (GATED ? WTN / 2 : WTN)                         // of a wave
+// neighbouring output columns of a lane
+#if STAGES != 3 && (TN / WN) / (GATED + 1) % 32 == 0
+#define RUN 8
+#else
+#define RUN 4
+#endif
 
 typedef unsigned short bf16_t;
 typedef signed char i8;
@@ -121,44 +127,77 @@ __device__ __forceinline__ float silu(float x) {
     return x / (1.0f + __builtin_amdgcn_exp2f(-x * 1.4426950408889634f));
 }
 
-// Columns n .. n + 3 of row m from their sums (GATED: g, and u the second
-// weight's); `whole`: all four exist and rows start on four columns.
-__device__ __forceinline__ void finish(const GemmI8Args &a, long long m, int n, const int (&g)[4], const int (&u)[4], bool whole) {
-    const float sa = a.sa[m];
-    float v[4];
-    auto one = [&](int r) {
-        float y = (float)g[r] * (sa * a.sb0[n + r]);
+// R neighbouring columns' scales (and bias).
+template <int R> struct Cols {
+    float s[R];
 #if GATED
-        y = silu(y) * ((float)u[r] * (sa * a.sb1[n + r]));
+    float u[R];
 #endif
 #if BIAS
-        y += a.bias[n + r];
+    float b[R];
 #endif
-        return y;
-    };
-    const size_t at = (size_t)m * a.N + n;
-    if (whole) {
+    // of column n on; `in`: all R exist (columns past the last repeat it)
+    __device__ __forceinline__ void load(const GemmI8Args &a, int n, bool in) {
+        if (in) {
+            __builtin_memcpy(s, a.sb0 + n, sizeof s);
+#if GATED
+            __builtin_memcpy(u, a.sb1 + n, sizeof u);
+#endif
+#if BIAS
+            __builtin_memcpy(b, a.bias + n, sizeof b);
+#endif
+        } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = one(r);
-#if F32
-        *(f32x4 *)((float *)a.C + at) = f32x4{v[0], v[1], v[2], v[3]};
-#else
-        u32x2 p;
-        p[0] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){v[0], v[1]}, bf16x2));
-        p[1] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){v[2], v[3]}, bf16x2));
-        *(u32x2 *)((bf16_t *)a.C + at) = p;
+            for (int r = 0; r < R; ++r) {
+                const int c = min(n + r, a.N - 1);
+                s[r] = a.sb0[c];
+#if GATED
+                u[r] = a.sb1[c];
 #endif
-        return;
+#if BIAS
+                b[r] = a.bias[c];
+#endif
+            }
+        }
     }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        if (n + r >= a.N) continue;
-        const float y = one(r);
+};
+
+// Columns n .. n + R - 1 of row m from their sums (GATED: g, and u the second
+// weight's).  Stores are of up to 16 bytes at any alignment.
+template <int R>
+__device__ __forceinline__ void finish(const GemmI8Args &a, long long m, int n, const int (&g)[R], const int (&u)[R], float sa,
+                                       const Cols<R> &c, bool in) {
 #if F32
-        ((float *)a.C)[at + r] = y;
+    float v[R];
 #else
-        ((bf16_t *)a.C)[at + r] = __builtin_bit_cast(bf16_t, (__bf16)y);
+    bf16_t v[R];
 #endif
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float y = (float)g[r] * (sa * c.s[r]);
+#if GATED
+        y = silu(y) * ((float)u[r] * (sa * c.u[r]));
+#endif
+#if BIAS
+        y += c.b[r];
+#endif
+#if F32
+        v[r] = y;
+#else
+        v[r] = __builtin_bit_cast(bf16_t, (__bf16)y);
+#endif
+    }
+#if F32
+    float *out = (float *)a.C + (size_t)m * a.N + n;
+#else
+    bf16_t *out = (bf16_t *)a.C + (size_t)m * a.N + n;
+#endif
+    if (in) {
+        __builtin_memcpy(out, v, sizeof v);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (n + r < a.N) out[r] = v[r];
     }
 }
 
@@ -192,12 +231,22 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     // weight row b of the tile: of wave column b / WTN, its first WTO rows
     // gate and the others up, so that one lane ends up with both sums of an
     // output
-#define SRC_ROW(b) ((b) / WTN * WTO + (b) % WTO)
+#define SRC_ROW(b) ((b) / WTN * WTO + SRC_IN((b) % WTO))
 #define SRC_UP(b) ((b) % WTN >= WTO)
 #else
     const i8 *const B1 = B0;
-#define SRC_ROW(b) (b)
+#define SRC_ROW(b) SRC_IN(b)
 #define SRC_UP(b) false
+#endif
+    // Which output column a weight row of the tile is: a lane's sums of an
+    // MFMA are runs of 4 columns; taking the rows in this order puts two such
+    // runs side by side, so that a lane stores 16 bytes of bf16.
+#if RUN == 8 && MF == 16
+#define SRC_IN(b) ((b) / 32 * 32 + (b) / 4 % 4 * 8 + (b) / 16 % 2 * 4 + (b) % 4)
+#elif RUN == 8
+#define SRC_IN(b) ((b) / 16 * 16 + (b) / 4 % 2 * 8 + (b) / 8 % 2 * 4 + (b) % 4)
+#else
+#define SRC_IN(b) (b)
 #endif
 
     accT acc[FM][FN];
@@ -505,6 +554,21 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
 #pragma unroll
                 for (int j = 0; j < FN; ++j) acc[i][j] = mfma(x.b[g][j], x.a[g][i], acc[i][j]);
     };
+    // the block of 16 x 16 outputs that this wave finishes first: its scales
+    // are loaded ahead of K, not after it
+    constexpr int FO = GATED ? FN / 2 : FN;
+    int b_m, b_n;
+    float b_sa = 0.f;
+    Cols<4> b_cols = {};
+    auto block = [&](int b) {
+        b_m = b / FO * 16 + lane % 16;
+        b_n = b % FO * 16 + 4 * (lane / 16);
+        if (b_m < mrows && b_n < ncols) {
+            b_sa = args.sa[m0 + b_m];
+            b_cols.load(args, n0 + b_n, n0 + b_n + 4 <= N);
+        }
+    };
+    if (wave < FM * FO) block(wave);
     const int whole = K / TK * TK;                      // whole batches
     int k0 = wave * TK;
     if (k0 < whole) fetch(f[0], k0);
@@ -539,7 +603,6 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
             for (int j = 0; j < FN; ++j) sums[wave][i * FN + j][lane] = acc[i][j];
         __syncthreads();
     }
-    constexpr int FO = GATED ? FN / 2 : FN;
     for (int b = wave; b < FM * FO; b += WK) {
         const int i = b / FO, j = b % FO;
         i32x4 s = {0, 0, 0, 0}, u = {0, 0, 0, 0};
@@ -558,48 +621,80 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
                     if (GATED) u = acc[x / FO][x % FO + FO % FN];
                 }
         }
-        const int ml = i * 16 + lane % 16, nl = j * 16 + 4 * (lane / 16);
-        if (ml >= mrows || nl >= ncols) continue;
+        if (b != wave) block(b);
+        if (b_m >= mrows || b_n >= ncols) continue;
         const int sv[4] = {s[0], s[1], s[2], s[3]}, uv[4] = {u[0], u[1], u[2], u[3]};
-        finish(args, m0 + ml, n0 + nl, sv, uv, (N & 3) == 0);
+        finish<4>(args, m0 + b_m, n0 + b_n, sv, uv, b_sa, b_cols, n0 + b_n + 4 <= N);
     }
     return;
 #endif
 
     // ---- epilogue ---------------------------------------------------------
     // The weight fragment was the MFMA's first operand: a lane holds one
-    // output row m and runs of 4 consecutive columns.
-    const bool quads = (N & 3) == 0;
+    // output row m and runs of RUN neighbouring columns, run q of a fragment
+    // row at column run_at(q) of the tile.
+    constexpr int RUNS = WTO / RUN / (64 / MF);
+    auto run_at = [&](int q) { return wn * WTO + q * RUN * (64 / MF) + RUN * (lane / MF); };
+    auto sums_of = [&](auto ic, auto qc, int (&s)[RUN], int (&u)[RUN]) __attribute__((always_inline)) {
+        constexpr int i = decltype(ic)::value, q = decltype(qc)::value, F = MF == 16 ? RUN / 4 : 1, G = MF == 16 ? 0 : q % 2;
+        constexpr int j = MF == 16 ? q * F : q / 2;
+#pragma unroll
+        for (int r = 0; r < RUN; ++r) {
+            s[r] = acc[i][j + (MF == 16 ? r / 4 : 0)][MF == 16 ? r % 4 : G * 8 + r];
+            u[r] = GATED ? acc[i][j + (MF == 16 ? r / 4 : 0) + FN / 2][MF == 16 ? r % 4 : G * 8 + r] : 0;
+        }
+    };
 #if SPLITS > 1
     const int ldp = (N + 3) & ~3;                                  // of a partial row, per weight
-#endif
+    seq<0, FM>([&](auto ic) __attribute__((always_inline)) {
+        const int ml = wm * WTM + decltype(ic)::value * MF + lane % MF;
+        // (row by row: the scheduler would form all addresses at once, next
+        // to all sums, and spill)
+        __builtin_amdgcn_sched_barrier(0);
+        int *row = args.P + (((size_t)kz * args.M + m0 + ml) * (GATED ? 2 : 1)) * ldp + n0;
+        seq<0, RUNS>([&](auto qc) __attribute__((always_inline)) {
+            int s[RUN], u[RUN];
+            sums_of(ic, qc, s, u);
+            const int nl = run_at(decltype(qc)::value);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int ml = wm * WTM + i * MF + lane % MF;
-        if (ml >= mrows) continue;
-#pragma unroll
-        for (int j = 0; j < (GATED ? FN / 2 : FN); ++j) {
-#pragma unroll
-            for (int g = 0; g < ACCN / 4; ++g) {
-                const int nl = wn * WTO + j * MF + g * 8 + 4 * (lane / MF);
-                if (nl >= ncols) continue;
-                int s[4], u[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[r] = acc[i][j][g * 4 + r];
-                    u[r] = GATED ? acc[i][j + (GATED ? FN / 2 : 0)][g * 4 + r] : 0;
-                }
-#if SPLITS > 1
+            for (int r = 0; r < RUN; r += 4) {
                 // (columns past N up to the next four are stored too)
-                int *p = args.P + (((size_t)kz * args.M + m0 + ml) * (GATED ? 2 : 1)) * ldp + n0 + nl;
-                *(i32x4 *)p = i32x4{s[0], s[1], s[2], s[3]};
-                if (GATED) *(i32x4 *)(p + ldp) = i32x4{u[0], u[1], u[2], u[3]};
-#else
-                finish(args, m0 + ml, n0 + nl, s, u, quads);
-#endif
+                if (ml < mrows && nl + r < ncols) {
+                    *(i32x4 *)(row + nl + r) = i32x4{s[r], s[r + 1], s[r + 2], s[r + 3]};
+                    if (GATED) *(i32x4 *)(row + ldp + nl + r) = i32x4{u[r], u[r + 1], u[r + 2], u[r + 3]};
+                }
             }
-        }
-    }
+        });
+    });
+#else
+    // All scales at once (a load behind every store's branch would cost its
+    // whole latency each): columns of a whole tile without a test.
+    auto store = [&](auto whole) __attribute__((always_inline)) {
+        constexpr bool W = decltype(whole)::value;
+        Cols<RUN> cols[RUNS];
+        float sa[FM];
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) cols[q].load(args, n0 + run_at(q), W || n0 + run_at(q) + RUN <= N);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = args.sa[m0 + min(wm * WTM + i * MF + lane % MF, mrows - 1)];
+        seq<0, FM>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            const int ml = wm * WTM + i * MF + lane % MF;
+            seq<0, RUNS>([&](auto qc) __attribute__((always_inline)) {
+                constexpr int q = decltype(qc)::value;
+                int s[RUN], u[RUN];
+                sums_of(ic, qc, s, u);
+                const int nl = run_at(q);
+                if (ml < mrows && (W || nl < ncols))
+                    finish<RUN>(args, m0 + ml, n0 + nl, s, u, sa[i], cols[q], W || n0 + nl + RUN <= N);
+            });
+        });
+    };
+    if (ncols == TNO)
+        store(IntC<1>{});
+    else
+        store(IntC<0>{});
+#endif
 }
 
 extern "C" __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(OCC, 8)))
@@ -667,6 +762,8 @@ extern "C" __global__ __launch_bounds__(256) void rc_gemm_i8_join(GemmI8Args arg
         if (GATED) u += *(const i32x4 *)(p + ldp);
     }
     const int sv[4] = {s[0], s[1], s[2], s[3]}, uv[4] = {u[0], u[1], u[2], u[3]};
-    finish(args, m, n, sv, uv, (N & 3) == 0);
+    Cols<4> cols;
+    cols.load(args, n, n + 4 <= N);
+    finish<4>(args, m, n, sv, uv, args.sa[m], cols, n + 4 <= N);
 }
 #endif
