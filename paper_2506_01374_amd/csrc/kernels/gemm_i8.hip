@@ -123,8 +123,9 @@ __device__ __forceinline__ i32x4 load16(const i8 *p, int left) {
 }
 
 __device__ __forceinline__ float silu(float x) {
-    // x * sigmoid(x); exp(-x) as 2^(-x log2 e) on the hardware exp2 unit
-    return x / (1.0f + __builtin_amdgcn_exp2f(-x * 1.4426950408889634f));
+    // x * sigmoid(x); exp(-x) as 2^(-x log2 e) and the reciprocal on the
+    // hardware's units, one step of fp32 off each
+    return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * 1.4426950408889634f));
 }
 
 // R neighbouring columns' scales (and bias).
@@ -633,8 +634,12 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     // The weight fragment was the MFMA's first operand: a lane holds one
     // output row m and runs of RUN neighbouring columns, run q of a fragment
     // row at column run_at(q) of the tile.
+    // (The lane is counted anew: kept from the start, it would hold a register
+    // through the main loop, where 256 x 256 tiles of 8 waves have none left.)
+    int el;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(el));
     constexpr int RUNS = WTO / RUN / (64 / MF);
-    auto run_at = [&](int q) { return wn * WTO + q * RUN * (64 / MF) + RUN * (lane / MF); };
+    auto run_at = [&](int q) { return wn * WTO + q * RUN * (64 / MF) + RUN * (el / MF); };
     auto sums_of = [&](auto ic, auto qc, int (&s)[RUN], int (&u)[RUN]) __attribute__((always_inline)) {
         constexpr int i = decltype(ic)::value, q = decltype(qc)::value, F = MF == 16 ? RUN / 4 : 1, G = MF == 16 ? 0 : q % 2;
         constexpr int j = MF == 16 ? q * F : q / 2;
@@ -646,12 +651,14 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     };
 #if SPLITS > 1
     const int ldp = (N + 3) & ~3;                                  // of a partial row, per weight
+    // (one pointer, moved row by row: the scheduler would form all addresses
+    // at once, next to all sums, and spill)
+    int *row = args.P + (((size_t)kz * args.M + m0 + wm * WTM + el % MF) * (GATED ? 2 : 1)) * ldp + n0;
     seq<0, FM>([&](auto ic) __attribute__((always_inline)) {
-        const int ml = wm * WTM + decltype(ic)::value * MF + lane % MF;
-        // (row by row: the scheduler would form all addresses at once, next
-        // to all sums, and spill)
+        const int ml = wm * WTM + decltype(ic)::value * MF + el % MF;
+        if constexpr (decltype(ic)::value > 0) row += (size_t)MF * (GATED ? 2 : 1) * ldp;
+        asm volatile("" : "+v"(row));
         __builtin_amdgcn_sched_barrier(0);
-        int *row = args.P + (((size_t)kz * args.M + m0 + ml) * (GATED ? 2 : 1)) * ldp + n0;
         seq<0, RUNS>([&](auto qc) __attribute__((always_inline)) {
             int s[RUN], u[RUN];
             sums_of(ic, qc, s, u);
@@ -676,10 +683,10 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
 #pragma unroll
         for (int q = 0; q < RUNS; ++q) cols[q].load(args, n0 + run_at(q), W || n0 + run_at(q) + RUN <= N);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] = args.sa[m0 + min(wm * WTM + i * MF + lane % MF, mrows - 1)];
+        for (int i = 0; i < FM; ++i) sa[i] = args.sa[m0 + min(wm * WTM + i * MF + el % MF, mrows - 1)];
         seq<0, FM>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
-            const int ml = wm * WTM + i * MF + lane % MF;
+            const int ml = wm * WTM + i * MF + el % MF;
             seq<0, RUNS>([&](auto qc) __attribute__((always_inline)) {
                 constexpr int q = decltype(qc)::value;
                 int s[RUN], u[RUN];

@@ -13,8 +13,8 @@ Integers are compared for equality.  Tolerances of the others, with u = 2^-24
           two) or none (fp32).
   gated   g and u carry 3 u each; SiLU multiplies a relative error of g by at
           most 1 + |g|, and its exponential has |g| u from the product with
-          log2 e, 2 u of its own, then a sum and a division: (4 |g| + 8) u,
-          the product u more.
+          log2 e, 2 u of its own, then a sum, a reciprocal (2 u) and a
+          product: (4 |g| + 9) u, the product with u one u more.
 """
 import math
 import os
@@ -224,7 +224,7 @@ def gemm_reference(ins, flags):
         u = d[0] @ d[4].T * d[1][:, None] * d[5][None, :]
         with np.errstate(over="ignore"):
             out = y / (1 + np.exp(-y)) * u
-        rel = (4 * np.abs(y) + 8 + 3 * (1 + np.abs(y)) + 3 + 1) * U
+        rel = (4 * np.abs(y) + 9 + 3 * (1 + np.abs(y)) + 3 + 1) * U
         return out, np.abs(out) * (BF16 + 2 * rel)
     err = 3 * U * np.abs(y)
     if flags & B:
