@@ -762,29 +762,118 @@ static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
     set_knob(d, s, "rows", rows);
 }
 
+// Int8 product.  The time of a ring schedule is estimated as
+//   start + rounds (turn + K pace), at least what the bytes take from HBM,
+// with rounds of workgroups over the chip and K the depth of one split, plus
+// the joining launch of K splits.  The constants (us, and us per 1000 of K)
+// are measured ones of each tile: over 236 sizes (1 to 4096 rows, weights of
+// 256 x 256 to 14336 x 4096 and 4096 x 14336, plain and gated) the schedule
+// with the least estimate takes 1.2 % more than the best of some 40 measured
+// (geometric mean).  One tile for all sizes is far off: 256 x 256 x 64 takes
+// 62.6 us for 4096 x 4096 x 4096 and 128 x 128 x 128 85, but for 1024 rows 56
+// and 22, and for 64 rows 32 x 32 x 256 takes 7.3 where 128 x 128 x 128
+// takes 21.
+struct RingTile {
+    int tm, tn, tk, wm, wn;          // tn: weight rows (twice the columns when gated)
+    double start, turn, pace;
+};
+static const RingTile RING_TILES[] = {
+    {256, 256, 64, 2, 4, 0.0, 7.6, 11.0}, {256, 128, 128, 4, 2, 0.0, 5.2, 7.0}, {128, 256, 128, 2, 4, 0.0, 5.2, 7.0},
+    {128, 128, 128, 2, 4, 0.0, 4.9, 3.5}, {64, 128, 128, 2, 2, 0.0, 4.2, 2.35}, {128, 64, 128, 2, 2, 0.0, 4.2, 2.35},
+    {64, 64, 256, 2, 2, 0.0, 3.9, 1.45},  {64, 32, 256, 2, 2, 0.0, 3.45, 1.1},  {32, 64, 256, 2, 2, 0.0, 3.45, 1.1},
+    {32, 32, 256, 1, 2, 1.5, 1.8, 1.06},  {32, 64, 128, 1, 2, 1.0, 2.6, 1.6},   {16, 32, 256, 1, 2, 1.6, 1.75, 0.87},
+    {16, 16, 256, 1, 1, 1.6, 1.6, 0.8},   {16, 64, 128, 1, 2, 1.6, 1.75, 1.15}, {16, 32, 128, 1, 1, 1.6, 1.7, 1.1}};
+
 static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
+    const int nb = (d->flags & RC_FLAG_GATED) ? 2 : 1;
     auto set = [&](const char *name, int v) { set_knob(d, s, name, v); };
-    if (M <= 16) {
-        set("stages", 3);
-        set("tile_m", 16);
-        set("tile_n", 16);
-        set("tile_k", K >= 256 ? 256 : K > 64 ? 128 : 64);
-        int wk = 8;
-        while (wk > 1 && (int64_t)wk / 2 * (K >= 256 ? 256 : K > 64 ? 128 : 64) >= K) wk /= 2;
-        set("waves_k", wk);
-        return;
+    auto tile = [&](int tm, int tn, int tk, int wm, int wn, int wk, int stages, int splits, int tail) {
+        set("tile_m", tm), set("tile_n", tn), set("tile_k", tk), set("waves_m", wm), set("waves_n", wn);
+        set("waves_k", wk), set("stages", stages), set("order", 1), set("splits", splits), set("tail", tail);
+        return check_schedule(d, s).empty();
+    };
+    auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
+
+    // Streaming, where few workgroups are needed and their start counts (us,
+    // against the best ring): up to 8 rows and weights of 2048 (4096 with a
+    // long K) to 8192 rows (4 x 4096 x 4096: 5.8 and 6.3; 1 x 4096 x 14336:
+    // 10.9 and 12.8; but 1 x 14336 x 4096: 11.6 and 10.9, 1 x 1024 x 8192:
+    // 7.0 and 5.8); up to 64 rows where 16 x 16 tiles with a
+    // short K are one round (64 x 1024 x 1024: 3.9 and 4.2); up to 16 rows
+    // with very large weights (16 x 16384 x 16384: 51.6 and 55.4).  K that is
+    // no multiple of 16 has no ring: also 64 rows of such tiles (16 x 1000 x
+    // 1001: 5.6 and 8.4 in the double buffer), and single tokens.
+    const int64_t small = count(M, 16) * count(nb * N, 16);
+    if (M <= 8 && nb * N >= (K > 4096 ? 4096 : 2048) && nb * N <= 8192) {
+        for (int wk = 4; wk >= 1; wk /= 2)
+            if (tile(16, 16, K > 64 ? 128 : 64, 1, 1, wk, 3, 1, 0)) return;
     }
-    static const int tiles[][4] = {{128, 128, 2, 2}, {64, 64, 2, 2}, {32, 32, 2, 2}, {16, 16, 1, 1}};
+    if (M <= 64 && small <= (K % 16 && M <= 2 ? 1024 : 256) && (K <= 1024 || (K % 16 && M <= 2))) {
+        const int tk = K > 512 ? 256 : 64;
+        for (int wk = K > 2048 ? 8 : 4; wk >= 1; wk /= 2)
+            if (tile(16, 16, tk, 1, 1, wk, 3, 1, 0)) return;
+    }
+    if (M <= 16 && (double)nb * N * K >= 160e6 && tile(16, 32, 128, 1, 1, 8, 3, 1, 0)) return;
+
+    if (K % 16 == 0) {
+        struct Option {
+            double us;
+            const RingTile *t;
+            int splits, tail;
+        };
+        std::vector<Option> all;
+        const double bytes = (double)M * K + nb * (double)N * K + 2.0 * M * N;
+        for (const RingTile &t : RING_TILES) {
+            if (t.tn / nb < 16 || (t.tm == 16 && M > 16)) continue;
+            const int waves = t.wm * t.wn;
+            const int64_t lds = (int64_t)gemm_i8_ring_stages(t.tm, t.tn, t.tk, waves, 1) * (t.tm + t.tn) * t.tk;
+            const int64_t slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
+            const int64_t tiles = count(M, t.tm) * count(N, t.tn / nb);
+            for (int sp = 1; sp <= 16; sp *= 2) {
+                const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0;
+                for (int tail = 0; tail <= (sp == 1); ++tail) {
+                    const int64_t w = tiles * sp;
+                    const double rounds = tail ? (double)(w / slots) + 0.5 : (double)count(w, slots);
+                    double us = t.start + rounds * (t.turn + kp * t.pace);
+                    us = std::max(us, 2.8 + bytes / std::min(5.6e6, (double)w * 4e4));
+                    if (sp > 1) us += 1.8 + (double)M * N * nb * (8 * sp + 2) / 6e6;
+                    all.push_back({us, &t, sp, tail});
+                }
+            }
+        }
+        std::stable_sort(all.begin(), all.end(), [](const Option &a, const Option &b) { return a.us < b.us; });
+        for (const Option &o : all) {
+            int tk = o.t->tk;
+            while (tk > 64 && tk / 2 >= K) tk /= 2;
+            if (tile(o.t->tm, o.t->tn / nb, tk, o.t->wm, o.t->wn, 1, 2, o.splits, o.tail)) return;
+        }
+    }
+
+    // Double buffer: the largest tile that gives every CU one, from K of 2000
+    // on with K splits of 1000 or more (us: 4096 x 4096 x 4099 in 256 x 128
+    // tiles 102, 128 x 128 126; 256 rows in 128 x 128 tiles of 4 splits 24,
+    // 64 x 64 tiles without 40; 32 rows in 32 x 32 tiles of 4 splits 12, 16 x
+    // 32 tiles without 23; but 256 x 1000 x 1001 in 32 x 32 tiles without
+    // 7.7, of 4 splits 10.7).
+    static const int tiles[][6] = {{256, 128, 64, 4, 2, 512}, {128, 128, 128, 2, 4, 256}, {64, 64, 64, 2, 2, 256},
+                                   {32, 32, 128, 2, 2, 256},  {16, 32, 128, 1, 2, 256}};
+    const bool split = K >= 2000;
     for (const int *t : tiles) {
-        set("tile_m", t[0]);
-        set("tile_n", t[1]);
-        set("waves_m", t[2]);
-        set("waves_n", t[3]);
-        if (((M + t[0] - 1) / t[0]) * ((N + t[1] - 1) / t[1]) >= 256 && check_schedule(d, s).empty()) break;
+        if (t[0] / 2 >= M && t[0] > 16) continue;
+        if (t[1] / nb / t[4] < 16) continue;
+        int tk = split && t[0] == 64 ? 128 : t[2], sp = 1;
+        while (tk > 64 && tk / 2 >= K) tk /= 2;
+        const int64_t n = count(M, t[0]) * count(N, t[1] / nb);
+        while (split && sp < 4 && n * sp < 512 && K / (2 * sp) >= 1000) sp *= 2;
+        if (n * sp >= t[5] && tile(t[0], t[1] / nb, tk, t[3], t[4], 1, 1, sp, 0)) return;
     }
-    set("tile_k", K > 64 ? 128 : 64);
-    set("order", 1);
+    for (int tm : {32, 16})
+        for (int tn : {32, 16})
+            for (int tk : {128, 64})
+                for (int sp : {4, 2, 1})
+                    if (K / sp >= 1000 || sp == 1)
+                        if (tile(tm, tn, tk, tm / 16, 1, 1, 1, sp, 0)) return;
 }
 
 }  // namespace rc

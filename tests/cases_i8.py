@@ -1,7 +1,8 @@
 """Sizes and schedules of the 8-bit integer operators' tests."""
 from __future__ import annotations
 
-import itertools
+import math
+import random
 
 from paper_2506_01374_amd import rc
 
@@ -71,29 +72,30 @@ def gemm_jobs(flags):
     return jobs
 
 
-def suggested(kind, flags, rows, cols, depths=(None,)):
-    """The different schedules suggested over a grid of sizes, each with a
-    size that it is suggested for."""
+def _sizes(ndims, count, most, seed):
+    """Sizes spread over the logarithm, whole multiples of 16 and odd ones."""
+    g = random.Random(seed)
+    for _ in range(count):
+        dims = [max(1, int(2 ** g.uniform(0, math.log2(m)))) for m in most[:ndims]]
+        if g.random() < 0.8:
+            dims[-1] = min(most[ndims - 1], -(-dims[-1] // 16) * 16)
+        yield dims
+
+
+def suggested_jobs(count=20000, seed=1):
+    """(op, schedule text): the different code objects that suggested schedules
+    ask for over the range of sizes (the kernels take sizes as arguments, so
+    that these are few), each with a size that it is suggested for."""
     found = {}
-    for dims in itertools.product(rows, cols, depths):
-        op = rc.Op(kind, dims if dims[2] is not None else dims[:2], flags)
-        found.setdefault(str(op.suggest()), op)
-    return [(op, text) for text, op in found.items()]
-
-
-_STEPS = [1, 2, 4, 8, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512, 768, 1000, 1536, 2048, 4096, 8192]
-_WIDE = [1, 2, 3, 8, 16, 32, 64, 128, 200, 256, 512, 777, 1024, 1536, 2048, 4096, 6144, 8192, 14336, 16384, 28672, 65536, 131072]
-
-
-def suggested_jobs():
-    """(op, schedule text): every code object that a suggested schedule can
-    ask for (the kernels of these kinds take sizes as arguments)."""
-    jobs = []
     for kind, flags in ((rc.RC_OP_QUANT_I8, 0), (rc.RC_OP_RMSNORM_I8, 0), (rc.RC_OP_RMSNORM_I8, R)):
-        jobs += suggested(kind, flags, _STEPS, _WIDE)
+        for dims in _sizes(2, count // 3, (1 << 20, 1 << 18), seed):
+            op = rc.Op(kind, dims, flags)
+            found.setdefault((kind, flags, str(op.suggest())), op)
     for flags in (0, B, F, B | F, G):
-        jobs += suggested(rc.RC_OP_GEMM_I8, flags, _STEPS, _WIDE, [1, 16, 64, 100, 128, 900, 1024, 4096, 4100, 14336, 131071])
-    return jobs
+        for dims in _sizes(3, count, (16384, 262144, 131071), seed):
+            op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
+            found.setdefault((op.kind, flags, str(op.suggest())), op)
+    return [(op, text) for (_, _, text), op in found.items()]
 
 
 def compile_jobs():

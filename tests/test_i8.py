@@ -117,7 +117,7 @@ def test_suggestions_share_few_code_objects():
     # sizes are kernel arguments: the suggestions over the whole range of
     # sizes are a handful of schedules, built ahead of time
     jobs = cases_i8.compile_jobs()
-    assert len(jobs) < 400
+    assert len(jobs) < 900
     for m, n, k in ((1, 1, 1), (3, 5000, 77), (999, 12345, 11008), (100000, 64, 64), (1, 128256, 8192)):
         for flags in (0, B, F, B | F, G):
             op = rc.Op(rc.RC_OP_GEMM_I8, (m, n, k), flags)
