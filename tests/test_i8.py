@@ -168,6 +168,24 @@ def test_tensor_checks(kind, dims, flags):
                     check(*sides)
 
 
+@pytest.mark.parametrize("kind,dims,flags", KINDS)
+def test_packed_block_is_the_structure(kind, dims, flags, monkeypatch):
+    op = rc.Op(kind, dims, flags)
+    want = rc._i8_tensors(op)
+    ins, outs = _tensors(op)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    pack = rc._i8_packer(want, -1)
+    assert pack(ins, tuple(outs), None, None) == (bytes(rc.Plan._args(ins, outs)), 0)
+    if len(outs) == 1:
+        assert pack(iter(ins), outs[0], None, None) == (bytes(rc.Plan._args(ins, outs)), 0)
+    for bad in ((ins[:-1], outs), (ins, outs[:-1]), (ins + outs, ()), (ins, outs + [outs[0]]), ([None] + ins[1:], outs),
+                ([ins[0].double()] + ins[1:], outs), (ins, [outs[0][:-1]] + outs[1:])):
+        with pytest.raises(ValueError):
+            pack(bad[0], bad[1], None, None)
+    with pytest.raises(ValueError):
+        rc._i8_packer(want, 0)(ins, outs, None, None)
+
+
 def test_argument_block_of_several_outputs():
     class Tensor:
         def __init__(self, p):
