@@ -129,7 +129,7 @@ typedef enum rc_op_kind {
      * in[2] = r [T][Hd] bf16 (RC_FLAG_RESIDUAL).  out[0] = q [T][Hd] int8;
      * out[1] = scale [T] fp32; out[2] = h [T][Hd] bf16 (RC_FLAG_RESIDUAL),
      * which may be the buffer of x or of r (no other overlap is allowed).
-     * Hd need not be a multiple of anything. */
+     * Hd need not be a multiple of anything; T at most 2^26 - 1, Hd 2^30. */
     RC_OP_RMSNORM_I8 = 6,
     /* Rows of bf16 to int8 with a scale for each row, without a norm:
      *   scale = max |x| / 127,  q = x / scale rounded as above
@@ -144,7 +144,8 @@ typedef enum rc_op_kind {
      * With RC_FLAG_GATED (alone) two weights share A, and
      *   out = bf16(SiLU(g) * u),  g and u the two products.
      * dim = {M, N, K}, K at most 131071 (the sums of 128 * 128 stay in 32
-     * bits), N at most 2^30, M at most 2^31 - 1.  in[0] = A [M][K] int8;
+     * bits), N at most 2^30, M at most 2^31 - 1, and at most 2^26 - 1 tiles of
+     * 16 x 16 outputs.  in[0] = A [M][K] int8;
      * in[1] = sa [M] fp32; in[2] = B [N][K] int8; in[3] = sb [N] fp32;
      * in[4] = bias [N] fp32 (RC_FLAG_BIAS), or in[4] = the up weight [N][K]
      * int8 and in[5] = its scales [N] fp32 (RC_FLAG_GATED; in[2] and in[3]

@@ -232,6 +232,7 @@ static std::string fmt(const char *f, ...) {
 }
 
 static const int64_t LDS_LIMIT = 163840;   // bytes one workgroup may allocate on gfx950
+static const int64_t MAX_GRID_THREADS = 4294967295LL;   // a grid's size is counted in threads
 
 // Depth of the direct-to-LDS ring of bf16 GEMM stages 7: as many stages as
 // fit the LDS share of one workgroup when occ waves per SIMD are resident,
@@ -427,7 +428,7 @@ static std::string check_i8_desc(const rc_op_desc *d, bool *size) {
             // fall through: the same row sizes
         case RC_OP_QUANT_I8:
             *size = true;
-            if (D[0] > INT32_MAX) return fmt("%lld rows exceed the grid's 2^31 - 1", (long long)D[0]);
+            if (D[0] * 64 > MAX_GRID_THREADS) return fmt("%lld rows of a wave each exceed the grid's 2^32 - 1 threads", (long long)D[0]);
             if (D[1] > (1LL << 30)) return fmt("rows of %lld elements exceed the 32-bit column indices", (long long)D[1]);
             return "";
         case RC_OP_GEMM_I8:
@@ -437,6 +438,8 @@ static std::string check_i8_desc(const rc_op_desc *d, bool *size) {
             if (D[2] > 131071) return fmt("K = %lld: sums of more than 131071 products can exceed int32", (long long)D[2]);
             if (D[0] > INT32_MAX) return fmt("M = %lld exceeds 2^31 - 1", (long long)D[0]);
             if (D[1] > (1LL << 30)) return fmt("N = %lld exceeds 2^30", (long long)D[1]);
+            if ((D[0] + 15) / 16 * ((D[1] + 15) / 16) > MAX_GRID_THREADS / 64)
+                return "tiles of 16 x 16 outputs exceed the grid's 2^32 - 1 threads";
             return "";
     }
     return "";
@@ -446,6 +449,8 @@ static std::string check_rows_i8(const rc_op_desc *d, const rc_schedule *s) {
     const int w = kv(d, s, "waves"), r = kv(d, s, "rows"), vec = kv(d, s, "vec"), held = kv(d, s, "held");
     const int64_t T = d->dim[0], C = d->dim[1];
     if (w * r > 16) return fmt("waves x rows = %d exceeds 16 waves per workgroup", w * r);
+    if ((T + r - 1) / r * 64 * w * r > MAX_GRID_THREADS)
+        return fmt("%lld rows of %d waves exceed the grid's 2^32 - 1 threads", (long long)T, w);
     if (redundant_tile(d, "rows", r, T)) return fmt("rows %d: rows %d already cover T = %lld", r, r / 2, (long long)T);
     if (redundant_tile(d, "vec", vec, C)) return fmt("vec %d: vec %d already covers a row of %lld", vec, vec / 2, (long long)C);
     const int64_t step = 64LL * w * vec;     // elements of one vector of every thread of a row
@@ -469,7 +474,9 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     if (redundant_tile(d, "tile_m", tm, M)) return fmt("tile_m %d: tile_m %d already covers M = %lld", tm, tm / 2, (long long)M);
     if (redundant_tile(d, "tile_n", tno, N)) return fmt("tile_n %d: tile_n %d already covers N = %lld", tno, tno / 2, (long long)N);
     if (redundant_tile(d, "tile_k", tk, K)) return fmt("tile_k %d: tile_k %d already covers K = %lld", tk, tk / 2, (long long)K);
-    if (sp * ((M + tm - 1) / tm) * ((N + tno - 1) / tno) > INT32_MAX) return "the tiles exceed the grid's 2^31 - 1";
+    const int64_t tiles = ((M + tm - 1) / tm) * ((N + tno - 1) / tno);
+    if (tiles > INT32_MAX || (tail ? 2 : 1) * sp * tiles * nt * wk > MAX_GRID_THREADS)
+        return "the tiles exceed the grid's 2^32 - 1 threads";
     const int64_t acc = (int64_t)tm * tn / nt;
     if (acc > 256) return fmt("%lld accumulators per lane exceed 256", (long long)acc);
     if (occ > 1 && acc > 512 / occ - 32) return fmt("%lld accumulators leave no registers at %d waves/SIMD", (long long)acc, occ);
@@ -477,7 +484,7 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
         if (st == 3) return "the streaming stage (3) splits K over waves (waves_k), not over workgroups";
         if ((sp - 1) * gemm_i8_split_k(K, tk, sp) >= K)
             return fmt("%d splits of K = %lld in tiles of %d leave one empty", sp, (long long)K, tk);
-        if ((M * ((N + 3) / 4) + 255) / 256 > INT32_MAX) return "the outputs exceed the joining launch's grid";
+        if (M * ((N + 3) / 4) + 255 > MAX_GRID_THREADS) return "the outputs exceed the joining launch's grid";
     }
     if (wk > 1 && st != 3) return "waves share a tile's K in the streaming stage (3) only";
     const int64_t stage_bytes = (int64_t)(tm + tn) * tk;
@@ -743,23 +750,33 @@ static void set_knob(const rc_op_desc *d, rc_schedule *s, const char *name, int3
     s->knob[knob_index(d->kind, name)] = v;
 }
 
-// Rows to int8: a row in registers, 16-byte loads, two vectors a thread.
+// Rows to int8: a row in registers, 16-byte loads, a workgroup a row with as
+// many waves as its vectors fill, up to 8, then 16 (us: 8192 x 4096 with the
+// residual, 8 waves of one vector 47.8, 4 waves of two 50.6, two rows a
+// workgroup 49.6; one row of 4096 3.6 and 4.6; 2048 x 14336, 16 waves of two
+// 22.2, 8 of four 21.9, but 16 rows 4.6 and 5.6).  Narrow rows take 8-byte
+// loads and four rows a workgroup (4096 x 128: 4.3, with 16 bytes 5.1).
 static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t T = d->dim[0], C = d->dim[1];
-    int vec = 8;
+    int vec = C > 256 ? 8 : 4, waves = 1, held = 1, rows = 1;
     while (vec > 1 && vec / 2 >= C) vec /= 2;
-    int waves = 1, held = 1;
-    while (64LL * waves * vec * held < C && waves < 4) waves *= 2;
-    while (64LL * waves * vec * held < C && held < 2) held *= 2;
-    while (64LL * waves * vec * held < C && waves < 16) waves *= 2;
-    while (64LL * waves * vec * held < C && held < 4) held *= 2;
-    if (64LL * waves * vec * held < C) held = 0;
-    int rows = 1;
-    while (rows * waves < 4 && rows < T) rows *= 2;
-    set_knob(d, s, "vec", vec);
-    set_knob(d, s, "waves", waves);
-    set_knob(d, s, "held", held);
-    set_knob(d, s, "rows", rows);
+    auto holds = [&]() { return 64LL * waves * vec * held >= C; };
+    while (!holds() && waves < 16) waves *= 2;
+    while (!holds() && held < 4) held *= 2;
+    if (!holds()) held = 0;
+    while (C <= 256 && rows < 4 && rows < T) rows *= 2;
+    for (; waves >= 1; waves /= 2) {          // fewer where the grid would be too large
+        for (held = 1; !holds() && held < 4;) held *= 2;
+        if (!holds()) held = 0;
+        set_knob(d, s, "vec", vec);
+        set_knob(d, s, "waves", waves);
+        set_knob(d, s, "held", held);
+        for (; rows >= 1; rows /= 2) {
+            set_knob(d, s, "rows", rows);
+            if (check_schedule(d, s).empty()) return;
+        }
+        rows = 1;
+    }
 }
 
 // Int8 product.  The time of a ring schedule is estimated as

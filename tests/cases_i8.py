@@ -63,6 +63,17 @@ def tail_jobs(flags):
     return [(dims, text) for dims, text in jobs if rc.Op(rc.RC_OP_GEMM_I8, dims, flags).from_string(text).validate() == ""]
 
 
+# an operand, the output and the partial sums past 2^32 bytes or elements
+LARGE = [
+    ((3, 270000, 16384), dict(stages=3, tile_k=256, waves_k=4)),
+    ((3, 270000, 16384), dict(stages=2, tile_k=256, tile_n=32, waves_n=2, order=1)),
+    ((3, 270000, 16384), dict(stages=1, tile_n=64, tile_k=128, waves_n=2)),
+    ((270000, 48, 16384), dict(stages=2, tile_m=256, tile_n=64, tile_k=128, waves_m=4, order=1)),
+    ((270000, 48, 16384), dict(stages=1, tile_m=128, tile_n=32, tile_k=128, waves_m=2, waves_n=2)),
+    ((70000, 65536, 128), dict(stages=2, tile_m=128, tile_n=128, tile_k=128, waves_m=2, waves_n=2, order=1)),
+    ((17000, 65536, 256), dict(stages=2, tile_m=128, tile_n=128, tile_k=128, waves_m=2, waves_n=2, order=1, splits=2))]
+
+
 def gemm_jobs(flags):
     jobs = []
     for dims in GEMM_DIMS:
@@ -109,5 +120,8 @@ def compile_jobs():
         for dims, text in gemm_jobs(flags) + tail_jobs(flags):
             op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
             jobs.append((op, [op.from_string(text)]))
+    for dims, knobs in LARGE:
+        op = rc.Op(rc.RC_OP_GEMM_I8, dims)
+        jobs.append((op, [op.schedule(**knobs)]))
     # one job a code object: a schedule and the flags, whatever the sizes
     return list({(op.kind, op.flags, str(s[0])): (op, s) for op, s in jobs}.values())

@@ -276,6 +276,47 @@ def test_sums_at_the_limit_of_int32(dims):
     check_gemm(dims, 0, 2)
 
 
+@pytest.mark.parametrize("job", range(len(cases_i8.LARGE)))
+def test_offsets_past_32_bits(job):
+    (m, n, k), knobs = cases_i8.LARGE[job]
+    op = rc.Op(rc.RC_OP_GEMM_I8, (m, n, k))
+    sched = op.schedule(**knobs)
+    assert sched.validate() == "", sched.validate()
+    print(f"[gpu] gemm_i8 dims={op.dims} sched={sched}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(job)
+    a, b = (torch.randint(-128, 128, (x, k), generator=g, device="cuda", dtype=torch.int8) for x in (m, n))
+    sa, sb = (torch.rand(x, generator=g, device="cuda") for x in (m, n))
+    out = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    plan = rc.Plan(op, sched)
+    plan.launch([a, sa, b, sb], out, plan.workspace())
+    torch.cuda.synchronize()
+    rows, cols = (torch.tensor(sorted({0, 1, x // 3, x // 2 + 1, x - 2, x - 1})) for x in (m, n))
+    ins = [t[i.cuda()].cpu() for t, i in ((a, rows), (sa, rows), (b, cols), (sb, cols))]
+    want, tol = gemm_reference(ins, 0)
+    assert np.all(np.abs(f64(out[rows.cuda()][:, cols.cuda()]) - want) <= tol)
+    # nothing is left out (a product of random rows is never NaN)
+    for r in range(0, m, 8192):
+        assert not out[r:r + 8192].isnan().any()
+
+
+def test_rows_past_32_bits():
+    t, c, block = 600 * 1024, 8192, 1024
+    x, w, r = rows_inputs(block, c, 9)
+    q, scale, h = rows_reference(x, w, r)
+    dx, dr = (bf16(v).cuda().repeat(t // block, 1) for v in (x, r))
+    op = rc.Op(rc.RC_OP_RMSNORM_I8, (t, c), R, eps=EPS)
+    plan = rc.Plan(op, op.suggest())
+    dq, ds = torch.empty(t, c, dtype=torch.int8, device="cuda"), torch.empty(t, device="cuda")
+    print(f"[gpu] rows dims={op.dims}", flush=True)
+    plan.launch([dx, bf16(w).cuda(), dr], (dq, ds, dx), None)          # h in place of x
+    torch.cuda.synchronize()
+    want_q, want_h = torch.from_numpy(q).cuda(), bf16(h).cuda()
+    for i in range(0, t, block):
+        assert torch.equal(dq[i:i + block], want_q) and torch.equal(dx[i:i + block], want_h)
+    assert torch.equal(ds.view(-1, block), ds[:block].expand(t // block, block))
+    assert np.all(np.abs(f64(ds[:block]) - scale) <= ((c / 64 + 21) / 2 + 5) * U * scale)
+
+
 def test_scales_that_are_not_finite_or_zero():
     dims = (40, 70, 200)
     ins = gemm_inputs(dims, F, 5)

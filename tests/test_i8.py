@@ -33,7 +33,7 @@ def test_descriptor_and_default(kind, dims, flags):
     (rc.RC_OP_RMSNORM_I8, (8,), 0, rc.RC_ERR_INVALID_ARGUMENT),
     (rc.RC_OP_RMSNORM_I8, (8, 8), B, rc.RC_ERR_INVALID_ARGUMENT),
     (rc.RC_OP_QUANT_I8, (8, 8), R, rc.RC_ERR_INVALID_ARGUMENT),
-    (rc.RC_OP_QUANT_I8, (1 << 31, 8), 0, rc.RC_ERR_UNSUPPORTED),
+    (rc.RC_OP_QUANT_I8, (1 << 26, 8), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_QUANT_I8, (1, (1 << 30) + 1), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_GEMM_I8, (8, 8), 0, rc.RC_ERR_INVALID_ARGUMENT),
     (rc.RC_OP_GEMM_I8, (8, 8, -1), 0, rc.RC_ERR_INVALID_ARGUMENT),
@@ -43,6 +43,7 @@ def test_descriptor_and_default(kind, dims, flags):
     (rc.RC_OP_GEMM_I8, (8, 8, 131072), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_GEMM_I8, (1 << 31, 8, 8), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_GEMM_I8, (8, (1 << 30) + 1, 8), 0, rc.RC_ERR_UNSUPPORTED),
+    (rc.RC_OP_GEMM_I8, (1 << 20, 16400, 8), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_GEMM_F32, (8, 8, 8), B, rc.RC_ERR_INVALID_ARGUMENT)])
 def test_refused_descriptors(kind, dims, flags, status):
     with pytest.raises(rc.RCError) as e:
@@ -99,6 +100,10 @@ def test_rows_legality():
     assert "already hold" in op.schedule(vec=8, held=4).validate()
     assert "already cover" in op.schedule(vec=8, waves=4).validate()
     assert "already cover T" in rc.Op(rc.RC_OP_QUANT_I8, (1, 1000)).schedule(rows=2).validate()
+    # a grid is counted in threads: 2^26 - 1 rows are a wave each
+    huge = rc.Op(rc.RC_OP_QUANT_I8, (2 ** 26 - 1, 4096))
+    assert huge.default().validate() == "" and "2^32 - 1 threads" in huge.schedule(waves=2).validate()
+    assert huge.suggest()["waves"] == 1
     assert "vec 4 already" in rc.Op(rc.RC_OP_QUANT_I8, (1, 4)).schedule(vec=8).validate()
 
 
@@ -107,6 +112,30 @@ def test_gemm_legality():
     assert "multiple of the 32x32" in op.schedule(mfma=32).validate()
     assert "exceed 256" in op.schedule(tile_m=256, tile_n=256).validate()
     assert "LDS" in op.schedule(tile_m=256, tile_n=256, waves_m=4, waves_n=4, tile_k=256).validate()
+    huge = rc.Op(rc.RC_OP_GEMM_I8, (1 << 20, 16000, 1024))
+    assert huge.default().validate() == "" and "2^32 - 1 threads" in huge.schedule(splits=2).validate()
+    # the ring: aligned rows, whole wave-loads, a depth of three, enough K
+    # tiles where the MFMA steps of one are odd
+    ring = dict(tile_m=64, tile_n=64, tile_k=128, waves_m=2, waves_n=2, stages=2)
+    assert rc.Op(rc.RC_OP_GEMM_I8, (1000, 1000, 1008)).schedule(**ring).validate() == ""
+    assert "multiple of 16" in op.schedule(**ring).validate()
+    op = rc.Op(rc.RC_OP_GEMM_I8, (1000, 1000, 1024))
+    assert "wave-loads" in op.schedule(**{**ring, "tile_m": 64, "waves_m": 4, "tile_n": 32, "tile_k": 64}).validate()
+    assert "K tiles" in rc.Op(rc.RC_OP_GEMM_I8, (1000, 1000, 256)).schedule(**{**ring, "tile_k": 64}).validate()
+    assert "ring stages" in op.schedule(tile_m=256, tile_n=256, tile_k=128, waves_m=4, waves_n=4, stages=2).validate()
+    # streaming: one wave column, few rows, no splits over workgroups
+    assert op.schedule(stages=3, waves_k=8).validate() == ""
+    assert "one wave column" in op.schedule(stages=3, waves_n=2, tile_n=32).validate()
+    assert "at most 64 rows" in op.schedule(stages=3, tile_m=128).validate()
+    assert "over waves" in op.schedule(stages=3, splits=2).validate()
+    assert "half of them" in op.schedule(stages=3, waves_k=16, tile_k=256).validate()
+    assert "streaming stage (3) only" in op.schedule(waves_k=2).validate()
+    # K splits of which none is empty; half-height tiles where they help
+    assert op.schedule(splits=16).validate() == "" and "empty" in op.schedule(splits=16, tile_k=128).validate()
+    wide = dict(tile_m=256, tile_n=128, tile_k=64, waves_m=2, waves_n=4, stages=2, tail=1)
+    assert rc.Op(rc.RC_OP_GEMM_I8, (256, 128 * 300, 1024)).schedule(**wide).validate() == ""
+    assert "no partial round" in rc.Op(rc.RC_OP_GEMM_I8, (256, 128 * 256, 1024)).schedule(**wide).validate()
+    assert "need the ring" in op.schedule(tail=1).validate()
     small = rc.Op(rc.RC_OP_GEMM_I8, (1, 16, 64))
     assert "tile_m" in small.schedule(tile_m=32).validate()
     assert "tile_n" in small.schedule(tile_n=32).validate()
@@ -123,9 +152,19 @@ def test_suggestions_share_few_code_objects():
             op = rc.Op(rc.RC_OP_GEMM_I8, (m, n, k), flags)
             assert op.suggest().validate() == ""
             assert any(o.kind == op.kind and o.flags == flags and str(s[0]) == str(op.suggest()) for o, s in jobs), (m, n, k)
-    for t, c in ((1, 1), (3, 5000), (5000, 3), (1, 128256), (2, 1 << 30), (2 ** 31 - 1, 4096)):
+    for t, c in ((1, 1), (3, 5000), (5000, 3), (1, 128256), (2, 1 << 30), (1 << 22, 4096), (2 ** 26 - 1, 100)):
         op = rc.Op(rc.RC_OP_QUANT_I8, (t, c))
         assert any(o.kind == op.kind and str(s[0]) == str(op.suggest()) for o, s in jobs), (t, c)
+
+
+def test_search_over_an_8_bit_operator():
+    # the generic search runs over these kinds' knobs: with the tile area as
+    # the reward it ends at the largest legal tile
+    op = rc.Op(rc.RC_OP_GEMM_I8, (512, 512, 1024), G)
+    s = rc.Search(op, lambda x: float(x["tile_m"] * x["tile_n"]), budget=150, seed=3).run()
+    best, reward, _ = s.best()
+    assert best.validate() == "" and reward >= 128 * 128
+    assert all(h["schedule"].validate() == "" for h in s.history())
 
 
 def test_kernels_do_not_depend_on_the_sizes():
