@@ -322,7 +322,9 @@ rc_status rc_plan_kernel_flops(const rc_plan *p, int32_t kernel, double *flops);
  *   unfused epilogues: "gate.f32", "up.f32" or "pre.f32" (fp32 [rows][cols]);
  *   RC_OP_ATTENTION with chunk > 0: "partials"; RC_OP_GEMM_F32 streaming
  *   stage with splits > 1: "splitk.partials"; RC_OP_GEMM_I8 with splits > 1:
- *   "splitk.partials" int32 [splits][M][1, or 2 gated][N rounded up to 4].
+ *   "splitk.partials" int32 [splits][M][1, or 2 gated][N rounded up to 4], and
+ *   with pad 1 "padded.rows" int8 [M + N, or M + 2 N gated][K rounded up to
+ *   16] (A, then the weights).
  * RC_ERR_INVALID_ARGUMENT if the plan has no part of that name.  (The
  * routing preparation of the MoE layer of Sec. 4.1 is integer index work:
  * these parts let it be checked exactly.) */

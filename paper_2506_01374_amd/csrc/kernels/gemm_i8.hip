@@ -16,9 +16,10 @@
 //                tile, any sizes (ComputeLocation); 2: a ring of NSTAGE LDS
 //                buffers filled by direct-to-LDS buffer loads issued
 //                NSTAGE - 1 tiles ahead (K a multiple of 16: a lane moves 16
-//                aligned bytes); 3: streaming, for few rows of A - operands
-//                go straight to registers in the MFMA's layout, the WK waves
-//                of a tile take K in turns and add up through LDS
+//                aligned bytes; rows of another length are copied first, by
+//                rc_pad_i8); 3: streaming, for few rows of A -
+//                operands go straight to registers in the MFMA's layout, the
+//                WK waves of a tile take K in turns and add up through LDS
 //   SPLITS       the K range cut over that many workgroups of a tile, whose
 //                int32 sums rc_gemm_i8_join adds and finishes (Parallel)
 //   ORDER        0: tile n fastest; 1: bands of 8 M tiles, m fastest within

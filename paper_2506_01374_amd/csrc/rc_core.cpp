@@ -148,6 +148,7 @@ static std::vector<KnobDef> gemm_i8_knobs() {
         {"occ", "Parallel", {1, 2}, 1},                       // waves per SIMD to budget registers for
         {"splits", "Parallel", {1, 2, 4, 8, 16}, 1},          // K splits across workgroups
         {"tail", "Parallel", {0, 1}, 0},                      // half-height tiles in a last, partial round
+        {"pad", "Layout", {0, 1}, 0},                         // rows copied to whole 16-byte chunks first
     };
 }
 
@@ -466,7 +467,8 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     const int tm = kv(d, s, "tile_m"), tno = kv(d, s, "tile_n"), tn = nb * tno, tk = kv(d, s, "tile_k");
     const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), wk = kv(d, s, "waves_k"), mf = kv(d, s, "mfma");
     const int st = kv(d, s, "stages"), occ = kv(d, s, "occ"), sp = kv(d, s, "splits"), tail = kv(d, s, "tail");
-    const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
+    const int pad = kv(d, s, "pad");
+    const int64_t M = d->dim[0], N = d->dim[1], K = pad ? (d->dim[2] + 15) / 16 * 16 : d->dim[2];
     const int nt = 64 * wm * wn;
     if (tm % wm || (tm / wm) % mf) return fmt("tile_m/waves_m = %d/%d is not a multiple of the %dx%d MFMA", tm, wm, mf, mf);
     if (tno % wn || (tno / wn) % mf) return fmt("tile_n/waves_n = %d/%d is not a multiple of the %dx%d MFMA", tno, wn, mf, mf);
@@ -486,13 +488,18 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
             return fmt("%d splits of K = %lld in tiles of %d leave one empty", sp, (long long)K, tk);
         if (M * ((N + 3) / 4) + 255 > MAX_GRID_THREADS) return "the outputs exceed the joining launch's grid";
     }
+    if (pad) {
+        if (st != 2) return "only the ring (stages 2) needs rows of whole 16-byte chunks (pad)";
+        if (d->dim[2] % 16 == 0) return fmt("pad: K = %lld is a multiple of 16 already", (long long)K);
+        if ((M + nb * N) * (K / 16) + 255 > MAX_GRID_THREADS) return "pad: the operands exceed the copying launch's grid";
+    }
     if (wk > 1 && st != 3) return "waves share a tile's K in the streaming stage (3) only";
     const int64_t stage_bytes = (int64_t)(tm + tn) * tk;
     int64_t lds = 2 * stage_bytes;
     int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 4;     // register staging of the next tile
     int64_t waves = (int64_t)wm * wn;
     if (st == 2) {
-        if (K % 16) return fmt("the direct-to-LDS ring moves 16 aligned bytes a lane: K = %lld is no multiple of 16", (long long)K);
+        if (K % 16) return fmt("the direct-to-LDS ring moves 16 aligned bytes a lane: K = %lld is no multiple of 16 (pad 1 makes it one)", (long long)K);
         if ((int64_t)tm * tk % (1024 * waves)) return fmt("A tile is not a whole number of 1 KiB wave-loads for %lld waves", (long long)waves);
         if ((int64_t)tn * tk % (1024 * waves)) return fmt("B tile is not a whole number of 1 KiB wave-loads for %lld waves", (long long)waves);
         const int ns = gemm_i8_ring_stages(tm, tn, tk, (int)waves, occ);
@@ -801,13 +808,35 @@ static const RingTile RING_TILES[] = {
     {32, 32, 256, 1, 2, 1.5, 1.8, 1.06},  {32, 64, 128, 1, 2, 1.0, 2.6, 1.6},   {16, 32, 256, 1, 2, 1.6, 1.75, 0.87},
     {16, 16, 256, 1, 1, 1.6, 1.6, 0.8},   {16, 64, 128, 1, 2, 1.6, 1.75, 1.15}, {16, 32, 128, 1, 1, 1.6, 1.7, 1.1}};
 
+// K that is no multiple of 16: the ring on rows copied to whole chunks (pad),
+// at 3.9 us and 4.2 TB/s for the copy, or the double buffer, whose workgroups
+// on one CU (`wgs`) together take `pace` each for 1000 of K, but no less than
+// `least`, both 25 % less where rows start on 4 bytes, and which stores
+// `store` TB/s at most.  Over 159 sizes (17 to 16384 rows, K of 16 to 14339)
+// the least estimate takes 3.0 % more than the best of some 40 measured, and
+// 6 % more without the copy (us, copy and double buffer: 2048 x 14336 x 4098
+// 166 and 213, 4096 x 4096 x 14339 291 and 372; but 512 x 14336 x 4098 70 and
+// 52, 256 x 2048 x 1004 9.2 and 7.8).  The large tile pays where K is short
+// (4096 x 14336 x 64: 34, 128 x 128 tiles 40, 32 x 32 64).
+struct BufferTile {
+    int tm, tn, tk, wm, wn, wgs;
+    double turn, least, pace, store;
+};
+static const BufferTile BUFFER_TILES[] = {{256, 128, 64, 4, 2, 2, 1.8, 16.7, 12.8, 3.8},
+                                          {128, 128, 128, 2, 4, 2, 3.3, 8.6, 6.4, 3.1},
+                                          {64, 64, 128, 2, 2, 4, 2.4, 5.9, 3.1, 2.2},
+                                          {32, 32, 128, 2, 2, 4, 0.1, 3.8, 1.4, 1.9},
+                                          {16, 32, 128, 1, 2, 8, 0.5, 3.7, 1.04, 1.4}};
+
 static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
     const int nb = (d->flags & RC_FLAG_GATED) ? 2 : 1;
+    const bool pad = K % 16;
     auto set = [&](const char *name, int v) { set_knob(d, s, name, v); };
     auto tile = [&](int tm, int tn, int tk, int wm, int wn, int wk, int stages, int splits, int tail) {
         set("tile_m", tm), set("tile_n", tn), set("tile_k", tk), set("waves_m", wm), set("waves_n", wn);
         set("waves_k", wk), set("stages", stages), set("order", 1), set("splits", splits), set("tail", tail);
+        set("pad", pad && stages == 2);
         return check_schedule(d, s).empty();
     };
     auto count = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
@@ -819,78 +848,72 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     // 7.0 and 5.8); up to 64 rows where 16 x 16 tiles with a
     // short K are one round (64 x 1024 x 1024: 3.9 and 4.2); up to 16 rows
     // with very large weights (16 x 16384 x 16384: 51.6 and 55.4).  K that is
-    // no multiple of 16 has no ring: also 64 rows of such tiles (16 x 1000 x
-    // 1001: 5.6 and 8.4 in the double buffer), and single tokens.
+    // no multiple of 16 (against the double buffer): two rounds of such tiles
+    // (16 x 1000 x 1001: 5.6 and 8.0; 64 x 1000 x 1001 gated 6.9 and 9.5), and
+    // up to 32 rows that start on 4 bytes (32 x 4096 x 4100: 9.6 and 11.4; but
+    // 32 x 4096 x 4099 19.8 and 12.0, 32 x 14336 x 4100 gated 48 and 37).
     const int64_t small = count(M, 16) * count(nb * N, 16);
-    if (M <= 8 && nb * N >= (K > 4096 ? 4096 : 2048) && nb * N <= 8192) {
+    if (!pad && M <= 8 && nb * N >= (K > 4096 ? 4096 : 2048) && nb * N <= 8192) {
         for (int wk = 4; wk >= 1; wk /= 2)
             if (tile(16, 16, K > 64 ? 128 : 64, 1, 1, wk, 3, 1, 0)) return;
     }
-    if (M <= 64 && small <= (K % 16 && M <= 2 ? 1024 : 256) && (K <= 1024 || (K % 16 && M <= 2))) {
-        const int tk = K > 512 ? 256 : 64;
+    if ((M <= 64 && small <= (pad ? 512 : 256) && K <= 1024) || (pad && K % 4 == 0 && M <= (nb * N <= 8192 ? 32 : 16))) {
         for (int wk = K > 2048 ? 8 : 4; wk >= 1; wk /= 2)
-            if (tile(16, 16, tk, 1, 1, wk, 3, 1, 0)) return;
+            if (tile(K > 1024 && M > 16 ? 32 : 16, 16, K > 512 ? 256 : 64, 1, 1, wk, 3, 1, 0)) return;
     }
-    if (M <= 16 && (double)nb * N * K >= 160e6 && tile(16, 32, 128, 1, 1, 8, 3, 1, 0)) return;
+    if (!pad && M <= 16 && (double)nb * N * K >= 160e6 && tile(16, 32, 128, 1, 1, 8, 3, 1, 0)) return;
 
-    if (K % 16 == 0) {
-        struct Option {
-            double us;
-            const RingTile *t;
-            int splits, tail;
-        };
-        std::vector<Option> all;
-        const double bytes = (double)M * K + nb * (double)N * K + 2.0 * M * N;
-        for (const RingTile &t : RING_TILES) {
-            if (t.tn / nb < 16 || (t.tm == 16 && M > 16)) continue;
-            const int waves = t.wm * t.wn;
-            const int64_t lds = (int64_t)gemm_i8_ring_stages(t.tm, t.tn, t.tk, waves, 1) * (t.tm + t.tn) * t.tk;
-            const int64_t slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
-            const int64_t tiles = count(M, t.tm) * count(N, t.tn / nb);
-            for (int sp = 1; sp <= 16; sp *= 2) {
-                const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0;
-                for (int tail = 0; tail <= (sp == 1); ++tail) {
-                    const int64_t w = tiles * sp;
-                    const double rounds = tail ? (double)(w / slots) + 0.5 : (double)count(w, slots);
-                    double us = t.start + rounds * (t.turn + kp * t.pace);
-                    us = std::max(us, 2.8 + bytes / std::min(5.6e6, (double)w * 4e4));
-                    if (sp > 1) us += 1.8 + (double)M * N * nb * (8 * sp + 2) / 6e6;
-                    all.push_back({us, &t, sp, tail});
-                }
+    struct Option {
+        double us;
+        int tm, tn, tk, wm, wn, stages, splits, tail;
+    };
+    std::vector<Option> all;
+    const double out = 2.0 * M * N, bytes = (double)M * K + nb * (double)N * K + out;
+    const double copy = pad ? 3.9 + 2.0 * K * (M + nb * (double)N) / 4.2e6 : 0.0;
+    auto join = [&](int sp) { return sp > 1 ? 1.8 + (double)M * N * nb * (8 * sp + 2) / 6e6 : 0.0; };
+    for (const RingTile &t : RING_TILES) {
+        // 16 rows a tile for narrow weights too (1024 x 16 x 4096: 5.1 us, 32 x
+        // 16 tiles of the double buffer 6.5)
+        if (t.tn / nb < 16 || (t.tm == 16 && M > 16 && N > 16)) continue;
+        const int waves = t.wm * t.wn;
+        const int64_t lds = (int64_t)gemm_i8_ring_stages(t.tm, t.tn, t.tk, waves, 1) * (t.tm + t.tn) * t.tk;
+        const int64_t slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
+        const int64_t tiles = count(M, t.tm) * count(N, t.tn / nb);
+        for (int sp = 1; sp <= 16; sp *= 2) {
+            const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0;
+            for (int tail = 0; tail <= (sp == 1); ++tail) {
+                const int64_t w = tiles * sp;
+                const double rounds = tail ? (double)(w / slots) + 0.5 : (double)count(w, slots);
+                double us = t.start + rounds * (t.turn + kp * t.pace);
+                us = std::max(us, 2.8 + bytes / std::min(5.6e6, (double)w * 4e4)) + copy + join(sp);
+                all.push_back({us, t.tm, t.tn / nb, t.tk, t.wm, t.wn, 2, sp, tail});
             }
         }
-        std::stable_sort(all.begin(), all.end(), [](const Option &a, const Option &b) { return a.us < b.us; });
-        for (const Option &o : all) {
-            int tk = o.t->tk;
-            while (tk > 64 && tk / 2 >= K) tk /= 2;
-            if (tile(o.t->tm, o.t->tn / nb, tk, o.t->wm, o.t->wn, 1, 2, o.splits, o.tail)) return;
+    }
+    for (const BufferTile &t : BUFFER_TILES) {
+        if (t.tm == 16 && M > 16 && M <= 32) continue;
+        const double four = K % 4 ? 1.0 : 0.75;
+        for (int sp = 1; sp <= 16; sp *= 2) {
+            const int64_t cu = count(count(M, t.tm) * count(N, t.tn / nb) * sp, 256);      // tiles of a CU
+            const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0 * four;
+            double us = 5.0 + count(cu, t.wgs) * t.turn + kp * (cu / t.wgs) * std::max(t.least, t.wgs * t.pace);
+            if (cu % t.wgs) us += kp * std::max(t.least, (cu % t.wgs) * t.pace);
+            us = std::max(us, 2.8 + (bytes - out) / 5e6 + out / (1e6 * t.store)) + join(sp) + (pad ? 0.0 : 1e9);      // last where no copy is needed
+            all.push_back({us, t.tm, t.tn / nb, t.tk, t.wm, std::min(t.wn, t.tn / nb / 16), 1, sp, 0});
         }
     }
-
-    // Double buffer: the largest tile that gives every CU one, from K of 2000
-    // on with K splits of 1000 or more (us: 4096 x 4096 x 4099 in 256 x 128
-    // tiles 102, 128 x 128 126; 256 rows in 128 x 128 tiles of 4 splits 24,
-    // 64 x 64 tiles without 40; 32 rows in 32 x 32 tiles of 4 splits 12, 16 x
-    // 32 tiles without 23; but 256 x 1000 x 1001 in 32 x 32 tiles without
-    // 7.7, of 4 splits 10.7).
-    static const int tiles[][6] = {{256, 128, 64, 4, 2, 512}, {128, 128, 128, 2, 4, 256}, {64, 64, 64, 2, 2, 256},
-                                   {32, 32, 128, 2, 2, 256},  {16, 32, 128, 1, 2, 256}};
-    const bool split = K >= 2000;
-    for (const int *t : tiles) {
-        if (t[0] / 2 >= M && t[0] > 16) continue;
-        if (t[1] / nb / t[4] < 16) continue;
-        int tk = split && t[0] == 64 ? 128 : t[2], sp = 1;
+    std::stable_sort(all.begin(), all.end(), [](const Option &a, const Option &b) { return a.us < b.us; });
+    for (const Option &o : all) {
+        int tk = o.tk;
         while (tk > 64 && tk / 2 >= K) tk /= 2;
-        const int64_t n = count(M, t[0]) * count(N, t[1] / nb);
-        while (split && sp < 4 && n * sp < 512 && K / (2 * sp) >= 1000) sp *= 2;
-        if (n * sp >= t[5] && tile(t[0], t[1] / nb, tk, t[3], t[4], 1, 1, sp, 0)) return;
+        if (tile(o.tm, o.tn, tk, o.wm, o.wn, 1, o.stages, o.splits, o.tail)) return;
     }
+    // few rows or columns, that larger tiles would cover twice
     for (int tm : {32, 16})
-        for (int tn : {32, 16})
-            for (int tk : {128, 64})
-                for (int sp : {4, 2, 1})
-                    if (K / sp >= 1000 || sp == 1)
-                        if (tile(tm, tn, tk, tm / 16, 1, 1, 1, sp, 0)) return;
+        for (int tk : {128, 64})
+            for (int sp : {4, 2, 1})
+                if (K / sp >= 1000 || sp == 1)
+                    if (tile(tm, 16, tk, tm / 16, 1, 1, 1, sp, 0)) return;
 }
 
 }  // namespace rc

@@ -80,6 +80,12 @@ struct GemmI8Args {
     long long M;
     int N, K, KP, tail;
 };
+struct PadI8Args {
+    const void *A, *B0, *B1;
+    void *out;
+    long long rows, M;
+    int N, K;
+};
 
 // A kernel's by-value argument block (fixed storage: launching allocates
 // nothing on the host).
@@ -886,13 +892,31 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             k.block = dim3(64 * wm * wn * wk, 1, 1);
             k.flops = rc_op_flops(d);
             const long long M = D[0];
-            const int N = (int)D[1], K = (int)D[2], KP = (int)gemm_i8_split_k(K, tk, sp);
+            const int N = (int)D[1], K0 = (int)D[2];
+            // rows copied to whole 16-byte chunks: A's, then the weight's
+            const bool pad = kv(d, s, "pad");
+            const int K = pad ? (K0 + 15) / 16 * 16 : K0, KP = (int)gemm_i8_split_k(K, tk, sp);
+            const size_t nrows = (size_t)M + (gated ? 2 : 1) * (size_t)N;
+            const size_t offR = pad ? ws.add(nrows * K, "padded.rows") : 0;
+            if (pad) {
+                Kern kp;
+                kp.src = Source{SRC_pad_i8, "rc_pad_i8", ""};
+                kp.grid = dim3((unsigned)((nrows * (K / 16) + 255) / 256), 1, 1);
+                kp.block = dim3(256, 1, 1);
+                kp.bind = [=](const rc_args *a, char *w, ArgBlob &b) {
+                    put(b, PadI8Args{a->in[0], a->in[2], gated ? a->in[4] : nullptr, w + offR, (long long)nrows, M, N, K0});
+                };
+                p.kerns.push_back(kp);
+            }
             const size_t offP = sp > 1 ? ws.add((size_t)sp * M * (gated ? 2 : 1) * ((N + 3) / 4 * 4) * 4, "splitk.partials") : 0;
             k.bind = [=](const rc_args *a, char *w, ArgBlob &b) {
-                put(b, GemmI8Args{a->in[0], a->in[2], gated ? a->in[4] : nullptr, a->in[1], a->in[3],
+                char *r = w + offR;
+                put(b, GemmI8Args{pad ? r : a->in[0], pad ? r + (size_t)M * K : a->in[2],
+                                  !gated ? nullptr : pad ? r + ((size_t)M + N) * K : a->in[4], a->in[1], a->in[3],
                                   gated ? a->in[5] : nullptr, bias ? a->in[4] : nullptr, a->out[0],
                                   sp > 1 ? w + offP : nullptr, M, N, K, KP, tail});
             };
+            p.dominant = (int)p.kerns.size();
             p.kerns.push_back(k);
             if (sp > 1) {
                 Kern kj = k;
@@ -902,7 +926,6 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
                 kj.block = dim3(256, 1, 1);
                 p.kerns.push_back(kj);
             }
-            p.dominant = 0;
             break;
         }
         default: return fail(RC_ERR_UNSUPPORTED, "unknown operator kind");

@@ -41,12 +41,16 @@ GEMM_TEXTS = [_TILE.format(*t) for t in (
     # streaming
     (16, 16, 64, 1, 1, 1, 16, 3, 0, 1, 1), (16, 16, 256, 1, 1, 8, 16, 3, 0, 1, 1), (16, 64, 128, 1, 1, 4, 16, 3, 1, 1, 1),
     (32, 32, 128, 1, 1, 16, 16, 3, 0, 1, 1), (64, 32, 128, 1, 1, 2, 16, 3, 1, 1, 1), (64, 64, 64, 1, 1, 8, 16, 3, 0, 1, 1))]
+# the ring on rows copied to whole 16-byte chunks
+GEMM_TEXTS += [_TILE.format(*t) + ",pad=1" for t in (
+    (64, 64, 128, 2, 2, 1, 16, 2, 1, 1, 1), (32, 32, 128, 1, 1, 1, 16, 2, 0, 2, 4), (64, 128, 256, 2, 2, 1, 32, 2, 1, 1, 1),
+    (16, 16, 256, 1, 1, 1, 16, 2, 1, 1, 1), (256, 256, 64, 2, 4, 1, 16, 2, 1, 1, 1), (128, 128, 128, 2, 4, 1, 16, 2, 1, 1, 2))]
 
 # (M, N, K): one of each, around 16 and the tiles, K around a chunk, an MFMA
 # step and the K tiles, rows that start on no alignment
 GEMM_DIMS = [(1, 1, 1), (1, 17, 16), (2, 3, 15), (15, 16, 17), (16, 100, 64), (17, 33, 65), (1, 260, 1000), (33, 64, 63),
              (64, 129, 127), (65, 128, 128), (100, 61, 129), (130, 257, 256), (257, 130, 257), (300, 272, 400),
-             (128, 256, 1040), (16, 64, 4096), (70, 96, 2064)]
+             (128, 256, 1040), (16, 64, 4096), (70, 96, 2064), (300, 260, 1001), (16, 40, 2050), (5, 48, 1100)]
 
 
 # a last, partial round of workgroups in half-height tiles: with a last row
@@ -56,10 +60,12 @@ TAIL_TEXT = "tile_m=32,tile_n=16,tile_k=128,waves_m=1,waves_n=1,mfma=16,stages=2
 TAIL_WIDE = "tile_m=256,tile_n=128,tile_k=64,waves_m=2,waves_n=4,mfma=16,stages=2,order=1,occ=1,tail=1"
 TAIL_DIMS = [(32 * 10, 16 * 110, 128), (32 * 9 + 5, 16 * 140, 400), (32 * 9 + 20, 16 * 120 - 3, 1600), (32 * 20, 16 * 60, 80)]
 TAIL_WIDE_DIMS = [(256 * 5 + 140, 128 * 45, 512), (256 * 6 + 4, 128 * 40 + 10, 1040)]
+TAIL_PAD_DIMS = (256 * 6 + 4, 128 * 40 + 10, 1029)
 
 
 def tail_jobs(flags):
     jobs = [(dims, TAIL_TEXT) for dims in TAIL_DIMS] + [(dims, TAIL_WIDE) for dims in TAIL_WIDE_DIMS]
+    jobs += [(TAIL_PAD_DIMS, TAIL_WIDE + ",pad=1")]
     return [(dims, text) for dims, text in jobs if rc.Op(rc.RC_OP_GEMM_I8, dims, flags).from_string(text).validate() == ""]
 
 
@@ -68,6 +74,7 @@ LARGE = [
     ((3, 270000, 16384), dict(stages=3, tile_k=256, waves_k=4)),
     ((3, 270000, 16384), dict(stages=2, tile_k=256, tile_n=32, waves_n=2, order=1)),
     ((3, 270000, 16384), dict(stages=1, tile_n=64, tile_k=128, waves_n=2)),
+    ((3, 270000, 16383), dict(stages=2, tile_k=256, tile_n=32, waves_n=2, order=1, pad=1)),
     ((270000, 48, 16384), dict(stages=2, tile_m=256, tile_n=64, tile_k=128, waves_m=4, order=1)),
     ((270000, 48, 16384), dict(stages=1, tile_m=128, tile_n=32, tile_k=128, waves_m=2, waves_n=2)),
     ((70000, 65536, 128), dict(stages=2, tile_m=128, tile_n=128, tile_k=128, waves_m=2, waves_n=2, order=1)),

@@ -264,7 +264,7 @@ def test_gemm(dims, flags):
 @pytest.mark.parametrize("flags", [0, B | F, G])
 def test_gemm_with_half_height_tiles(flags):
     jobs = cases_i8.tail_jobs(flags)
-    assert len(jobs) == len(cases_i8.TAIL_DIMS) + len(cases_i8.TAIL_WIDE_DIMS)
+    assert len(jobs) == len(cases_i8.TAIL_DIMS) + len(cases_i8.TAIL_WIDE_DIMS) + 1
     for i, (dims, text) in enumerate(jobs):
         check_gemm(dims, flags, 300 + i, text)
 
