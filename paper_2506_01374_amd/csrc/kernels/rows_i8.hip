@@ -21,7 +21,7 @@
 // The norm's factor cancels from q, which so needs no sum: p is a product of
 // two 8-bit significands, 127 p has at most 23 bits, and the remainder 127 p
 // - q a of a trial q is exact in fp32, so q is the correctly rounded integer
-// whatever the order in which the row was read (see quant).  The sum of
+// whatever the order in which the row was read (see nearest).  The sum of
 // squares and both statistics are fp32.
 // A row of zeros has scale 0 and q 0.  A row that holds a NaN or an infinity,
 // or (NORM) whose squares sum past fp32, has scale NaN and q 0: what is
@@ -45,22 +45,34 @@ struct RowsI8Args {
 };
 
 __device__ __forceinline__ bf16_t f2bf(float x) { return __builtin_bit_cast(bf16_t, (__bf16)x); }
-__device__ __forceinline__ float bf2f(u32 b) { return __builtin_bit_cast(float, b << 16); }
 
+// VEC elements, two a word.
+#define WORDS ((VEC + 1) / 2)
 struct Vec {
-    bf16_t e[VEC];
+    u32 w[WORDS];
+    __device__ __forceinline__ float at(int j) const {
+        return __builtin_bit_cast(float, j % 2 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
 };
 
-// Elements c .. c + VEC - 1 of a row of `cols`, zeros past its end.
-__device__ __forceinline__ Vec load(const bf16_t *row, int c, int cols) {
-    Vec v;
-    if (c + VEC <= cols) {
-        __builtin_memcpy(&v, row + c, sizeof v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) v.e[j] = c + j < cols ? row[c + j] : (bf16_t)0;
-    }
+// Elements c .. c + VEC - 1 of a row of `cols`, zeros past its end.  In two
+// steps, so that a thread's loads are all under way before it waits for one:
+// `fetch` loads whole vectors without a branch (a lane whose vector is not
+// whole loads the row's last one), `ends` puts right the lanes at the end.
+__device__ __forceinline__ Vec fetch(const bf16_t *row, int c, int cols) {
+    Vec v = {};
+    if (cols >= VEC) __builtin_memcpy(&v, row + (c < cols - VEC ? c : cols - VEC), 2 * VEC);
     return v;
+}
+
+__device__ __forceinline__ void ends(Vec &v, const bf16_t *row, int c, int cols) {
+    if (c + VEC <= cols) return;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v.w[i] = 0;
+    if (c >= cols) return;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        if (c + j < cols) v.w[j / 2] |= (u32)row[c + j] << (16 * (j % 2));
 }
 
 template <class T> __device__ __forceinline__ void store(T *row, const T (&v)[VEC], int c, int cols) {
@@ -73,26 +85,31 @@ template <class T> __device__ __forceinline__ void store(T *row, const T (&v)[VE
     }
 }
 
-// rint(127 p / a) for |p| <= a, halves to even.  p and a are scaled by a
-// power of two that brings a near 1, `inv` is near 1 / a.  The trial t is
-// within one of the result, and 127 p - t a is exact: both terms are
-// multiples of the smaller term's last bit, and their difference is below
-// 2 a, so that it has no more bits than 127 p has (t = 0 leaves 127 p).
-__device__ __forceinline__ int quant(float p, float a, float inv) {
-    const float s = 127.f * p;
-    const float t = __builtin_rintf(s * inv);
-    const float rem = __builtin_fmaf(-t, a, s);
-    const float twice = 2.f * __builtin_fabsf(rem);
-    const int n = (int)t;
+// An integer t near s / a, |s| <= 127 a, as SHIFT + t: the last bit of a
+// float there is 1, so that the addition rounds to an integer, which the low
+// bits then are.
+#define SHIFT 12582912.f        // 1.5 * 2^23
+__device__ __forceinline__ float trial(float s, float inv) { return __builtin_fmaf(s, inv, SHIFT); }
+
+// rint(s / a), halves to even, s = 127 p and |p| <= a.  The trial t is within
+// one of the result, and s - t a is exact: both terms are multiples of the
+// smaller term's last bit, and their difference is below 2 a, so that it has
+// no more bits than s has (t = 0 leaves s).  Where it is below a / 2, t is
+// the result.
+__device__ __forceinline__ int nearest(float s, float a, float inv) {
+    const float t = trial(s, inv);
+    const float rem = __builtin_fmaf(-(t - SHIFT), a, s);
+    const float r = __builtin_fabsf(rem);
+    const int n = __builtin_bit_cast(int, t);
     // past half a step, or at the half and odd: the neighbour on that side
-    const bool move = twice > a || (twice == a && (n & 1));
+    const bool move = r > 0.5f * a || (r == 0.5f * a && (n & 1));
     return move ? n + (rem > 0.f ? 1 : -1) : n;
 }
 
 extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args a) {
     const int tid = threadIdx.x;
     const int part = tid % LANES;                       // thread of its row
-    const int slot = tid / LANES;                       // row of the workgroup
+    const int slot = ROWS > 1 ? __builtin_amdgcn_readfirstlane(tid / LANES) : 0;     // row of the workgroup
     const long long row_at = (long long)blockIdx.x * ROWS + slot;
     const bool live = row_at < a.rows;                  // (the last workgroup may have fewer rows)
     const long long base = (live ? row_at : 0) * a.cols;
@@ -103,40 +120,54 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     bf16_t *ho = a.h + base;
 #endif
 
-    // one vector of the row: h in v (stored where RES), w in wv
-    auto fetch = [&](int c, Vec &v, Vec &wv) {
-        v = load(x, c, cols);
-#if RES
-        const Vec b = load(r, c, cols);
+    // a thread's vectors of the row: h in v (stored where RES), w in wv
+    auto read = [&](int c, auto &v, auto &wv, int n) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) v.e[j] = f2bf(bf2f(v.e[j]) + bf2f(b.e[j]));
-        store(ho, v.e, c, cols);
+        for (int i = 0; i < n; ++i) v[i] = fetch(x, c + i * LANES * VEC, cols);
+#if RES
+        Vec b[HELD ? HELD : 1];
+#pragma unroll
+        for (int i = 0; i < n; ++i) b[i] = fetch(r, c + i * LANES * VEC, cols);
 #endif
 #if NORM
-        wv = load(a.w, c, cols);
-#else
-        (void)wv;
+#pragma unroll
+        for (int i = 0; i < n; ++i) wv[i] = fetch(a.w, c + i * LANES * VEC, cols);
 #endif
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const int ci = c + i * LANES * VEC;
+            ends(v[i], x, ci, cols);
+#if RES
+            ends(b[i], r, ci, cols);
+            bf16_t h[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) h[j] = f2bf(v[i].at(j) + b[i].at(j));
+            store(ho, h, ci, cols);
+            v[i] = {};
+            __builtin_memcpy(&v[i], h, sizeof h);
+#endif
+#if NORM
+            ends(wv[i], a.w, ci, cols);
+#endif
+        }
     };
     auto product = [&](const Vec &v, const Vec &wv, int j) {
 #if NORM
-        return bf2f(v.e[j]) * bf2f(wv.e[j]);
+        return v.at(j) * wv.at(j);
 #else
         (void)wv;
-        return bf2f(v.e[j]);
+        return v.at(j);
 #endif
     };
-    // |p| as bits: unsigned order is the order of the magnitudes, with NaN
-    // above infinity, so the maximum keeps both
-    u32 top = 0;
+    // the maximum keeps a NaN
+    float top = 0.f;
     float ss = 0.f;
     auto take = [&](const Vec &v, const Vec &wv) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-            const u32 b = __builtin_bit_cast(u32, product(v, wv, j)) & 0x7FFFFFFFu;
-            top = b > top ? b : top;
+            top = __builtin_elementwise_maximum(top, __builtin_fabsf(product(v, wv, j)));
 #if NORM
-            const float h = bf2f(v.e[j]);
+            const float h = v.at(j);
             ss = __builtin_fmaf(h, h, ss);
 #endif
         }
@@ -144,30 +175,27 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
 
 #if HELD
     Vec v[HELD], wv[HELD];
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) fetch((i * LANES + part) * VEC, v[i], wv[i]);
+    read(part * VEC, v, wv, HELD);
 #pragma unroll
     for (int i = 0; i < HELD; ++i) take(v[i], wv[i]);
 #else
     for (int c = part * VEC; c < cols; c += LANES * VEC) {
-        Vec v, wv;
-        fetch(c, v, wv);
-        take(v, wv);
+        Vec v[1], wv[1];
+        read(c, v, wv, 1);
+        take(v[0], wv[0]);
     }
 #endif
 
     // over the row's lanes and waves, in a fixed order
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const u32 o = (u32)__shfl_xor((int)top, d);
-        top = o > top ? o : top;
+        top = __builtin_elementwise_maximum(top, __shfl_xor(top, d));
 #if NORM
         ss += __shfl_xor(ss, d);
 #endif
     }
 #if WAVES > 1
-    __shared__ u32 tops[ROWS][WAVES];
-    __shared__ float sums[ROWS][WAVES];
+    __shared__ float tops[ROWS][WAVES], sums[ROWS][WAVES];
     if (part % 64 == 0) {
         tops[slot][part / 64] = top;
         sums[slot][part / 64] = ss;
@@ -177,14 +205,13 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     ss = sums[slot][0];
 #pragma unroll
     for (int i = 1; i < WAVES; ++i) {
-        const u32 o = tops[slot][i];
-        top = o > top ? o : top;
+        top = __builtin_elementwise_maximum(top, tops[slot][i]);
         ss += sums[slot][i];
     }
 #endif
 
-    bool bad = top >= 0x7F800000u;
-    float scale = __builtin_bit_cast(float, top);
+    bool bad = !(top < __builtin_inff());
+    float scale = top;
 #if NORM
     // (the host keeps eps at 2^-100 or more, next to which a square that
     // leaves fp32's normal range is nothing)
@@ -195,19 +222,30 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     if (bad) scale = __builtin_nanf("");
     if (live && part == 0) a.scale[row_at] = scale;
 
-    // a in [1, 2) times a power of two: p and a are brought there by its
-    // inverse (exact), so that no product above leaves fp32's range
-    const float am = __builtin_bit_cast(float, top);
+    // a is brought near 1 by a power of two, and p with it (exact), so that no
+    // product below leaves fp32's range
     float up = 1.f;
-    if (top < 0x20000000u) up = 18446744073709551616.f;             // a < 2^-63: 2^64
-    if (top >= 0x5F800000u) up = 5.421010862427522e-20f;            // a >= 2^64: 2^-64
-    const float as = am * up;
-    const float inv = bad || top == 0u ? 0.f : __builtin_amdgcn_rcpf(as);
+    if (top < 0x1p-63f) up = 0x1p64f;
+    if (top >= 0x1p64f) up = 0x1p-64f;
+    const float as = bad || top == 0.f ? 1.f : top * up;
+    const float inv = __builtin_amdgcn_rcpf(as);
+    const u32 keep = bad ? 0u : ~0u;
     auto emit = [&](const Vec &v, const Vec &wv, int c) {
+        // trials of all elements, and again where one of them is not nearest
         signed char o[VEC];
+        float far = 0.f;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            o[j] = inv == 0.f ? (signed char)0 : (signed char)quant(product(v, wv, j) * up, as, inv);
+        for (int j = 0; j < VEC; ++j) {
+            const float s = product(v, wv, j) * (127.f * up);
+            const float t = trial(s, inv);
+            far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(-(t - SHIFT), as, s)));
+            o[j] = (signed char)(__builtin_bit_cast(u32, t) & keep);
+        }
+        if (far >= 0.5f * as) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                o[j] = (signed char)(nearest(product(v, wv, j) * (127.f * up), as, inv) & keep);
+        }
         store(a.q + base, o, c, cols);
     };
 #if HELD
@@ -218,14 +256,17 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     }
 #else
     for (int c = part * VEC; c < cols; c += LANES * VEC) {
-        Vec wv = {};
+        // RES: its own store, as x or r may be gone
 #if RES
-        const Vec v = load(ho, c, cols);                 // its own store: x or r may be gone
+        const bf16_t *src = ho;
 #else
-        const Vec v = load(x, c, cols);
+        const bf16_t *src = x;
 #endif
+        Vec v = fetch(src, c, cols), wv = {};
+        ends(v, src, c, cols);
 #if NORM
-        wv = load(a.w, c, cols);
+        wv = fetch(a.w, c, cols);
+        ends(wv, a.w, c, cols);
 #endif
         emit(v, wv, c);
     }

@@ -757,24 +757,34 @@ static void set_knob(const rc_op_desc *d, rc_schedule *s, const char *name, int3
     s->knob[knob_index(d->kind, name)] = v;
 }
 
-// Rows to int8: a row in registers, 16-byte loads, a workgroup a row with as
-// many waves as its vectors fill, up to 8, then 16 (us: 8192 x 4096 with the
-// residual, 8 waves of one vector 47.8, 4 waves of two 50.6, two rows a
-// workgroup 49.6; one row of 4096 3.6 and 4.6; 2048 x 14336, 16 waves of two
-// 22.2, 8 of four 21.9, but 16 rows 4.6 and 5.6).  Narrow rows take 8-byte
-// loads and four rows a workgroup (4096 x 128: 4.3, with 16 bytes 5.1).
+// Rows to int8: a row in registers, 16-byte loads, a workgroup a row.  Few
+// rows: as many waves as the row's vectors fill, up to 16, as the time is that
+// of one row (us: one row of 4096, 8 waves of one vector 3.2, 4 of two 3.8; 16
+// rows of 14336, 16 of two 4.4, 8 of four 5.0).  From 2^22 elements on up to 8
+// waves, and without the residual two vectors a thread before more waves, so
+// that a CU holds more workgroups in different phases (4096 x 8192: 4 waves of
+// four 22.0, 16 of one 27.5; 2048 x 14336: 8 of four 18.8, 16 of two 20.5; but
+// with the residual, 4096 x 14336: 16 of two 76, 8 of four 78, and 8192 x
+// 4096: 8 of one 45.1, 4 of two 46.3).  Narrow rows take 8- and 4-byte loads
+// and four rows a workgroup (4096 x 128 with the residual: 4-byte loads 3.4,
+// 8-byte 3.7, 16-byte 4.3, one row a workgroup of these 4.0 and 4.6).
 static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t T = d->dim[0], C = d->dim[1];
-    int vec = C > 256 ? 8 : 4, waves = 1, held = 1, rows = 1;
+    const bool many = T * C >= 1 << 22, lean = many && !(d->flags & RC_FLAG_RESIDUAL);
+    int vec = C > 256 ? 8 : C > 128 ? 4 : 2, waves = 1, held = 1, rows = 1;
     while (vec > 1 && vec / 2 >= C) vec /= 2;
     auto holds = [&]() { return 64LL * waves * vec * held >= C; };
-    while (!holds() && waves < 16) waves *= 2;
-    while (!holds() && held < 4) held *= 2;
+    auto grow = [&](int &knob, int most) {
+        while (!holds() && knob < most) knob *= 2;
+    };
+    if (lean) grow(held, 2);
+    grow(waves, many ? 8 : 16);
+    grow(held, lean ? 4 : many ? 2 : 1);
+    grow(waves, 16);
+    grow(held, 4);
     if (!holds()) held = 0;
     while (C <= 256 && rows < 4 && rows < T) rows *= 2;
-    for (; waves >= 1; waves /= 2) {          // fewer where the grid would be too large
-        for (held = 1; !holds() && held < 4;) held *= 2;
-        if (!holds()) held = 0;
+    for (;;) {
         set_knob(d, s, "vec", vec);
         set_knob(d, s, "waves", waves);
         set_knob(d, s, "held", held);
@@ -782,7 +792,12 @@ static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
             set_knob(d, s, "rows", rows);
             if (check_schedule(d, s).empty()) return;
         }
-        rows = 1;
+        if (waves == 1) return;
+        // fewer waves where the grid would be too large
+        rows = held = 1;
+        waves /= 2;
+        grow(held, 4);
+        if (!holds()) held = 0;
     }
 }
 
