@@ -108,19 +108,37 @@ __device__ __forceinline__ int swz_x(int row) {
 }
 __device__ __forceinline__ int swz(int row, int chunk) { return row * TK + ((chunk ^ swz_x(row)) << 4); }
 
-// 16 elements at p, of which `left` are in the row (the rest reads zero)
-__device__ __forceinline__ i32x4 load16(const i8 *p, int left) {
-    i32x4 v = {0, 0, 0, 0};
-    if (left >= 16) {
-        __builtin_memcpy(&v, p, 16);
-    } else {
-        unsigned w[4] = {0, 0, 0, 0};
+// n fragments of 16 elements at p(i), of which left(i) are in the row (the
+// rest reads zero), of rows `ld` long: loads without a branch, of the row's
+// last 16 where fewer are left, so that none waits for another, which are then
+// moved down.
+template <int CNT, class P, class L> __device__ __forceinline__ void ends16(i32x4 (&v)[CNT], P p, L left, int ld) {
+    if (ld >= 16) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < left) w[j / 4] |= (unsigned)(unsigned char)p[j] << (8 * (j % 4));
-        v = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+        for (int i = 0; i < CNT; ++i) __builtin_memcpy(&v[i], p(i) + min(left(i) - 16, 0), 16);
+#pragma unroll
+        for (int i = 0; i < CNT; ++i) {
+            const unsigned by = (unsigned)(16 - min(max(left(i), 0), 16));
+            i32x4 w = v[i];
+            if (by & 8) w = i32x4{w[2], w[3], 0, 0};
+            if (by & 4) w = i32x4{w[1], w[2], w[3], 0};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v[i][j] = by == 16 ? 0 : (int)__builtin_amdgcn_alignbyte(j < 3 ? (unsigned)w[j + 1] : 0u, (unsigned)w[j], by & 3);
+        }
+    } else {
+        // (a row shorter than a load)
+#pragma unroll
+        for (int i = 0; i < CNT; ++i) {
+            unsigned long long w[2] = {0, 0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+                for (int j = 0; j < 8 && 8 * h + j < left(i); ++j)
+                    w[h] |= (unsigned long long)(unsigned char)p(i)[8 * h + j] << (8 * j);
+            v[i] = i32x4{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
+        }
     }
-    return v;
 }
 
 __device__ __forceinline__ float silu(float x) {
@@ -291,8 +309,7 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
 #pragma unroll
             for (int i = 0; i < CH; ++i) __builtin_memcpy(&reg[i], src[i] + k0, 16);
         } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) reg[i] = load16(src[i] + k0, K - k0 - kc[i]);
+            ends16(reg, [&](int i) { return src[i] + k0; }, [&](int i) { return K - k0 - kc[i]; }, ld);
         }
     };
     auto put = [&](int b) {
@@ -587,10 +604,8 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     for (int k = whole + wave * 64; k < K; k += WK * 64) {
         const int left = K - k - lane / 16 * 16;
         i32x4 a[FM], b[FN];
-#pragma unroll
-        for (int i = 0; i < FM; ++i) a[i] = load16(Ab + k + ao[i], left);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) b[j] = load16((SRC_UP(j * 16) ? B1 : B0) + k + bo[j], left);
+        ends16(a, [&](int i) { return Ab + k + ao[i]; }, [&](int) { return left; }, ld);
+        ends16(b, [&](int j) { return (SRC_UP(j * 16) ? B1 : B0) + k + bo[j]; }, [&](int) { return left; }, ld);
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll

@@ -31,15 +31,14 @@ extern "C" __global__ __launch_bounds__(256) void rc_pad_i8(PadI8Args a) {
         }
     }
     src += (size_t)row * a.K + k;
+    const int left = a.K - k;
     i32x4 v = {0, 0, 0, 0};
-    if (a.K - k >= 16) {
+    if (left >= 16) {
         __builtin_memcpy(&v, src, 16);
     } else {
-        unsigned w[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < a.K - k) w[j / 4] |= (unsigned)(unsigned char)src[j] << (8 * (j % 4));
-        v = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+        for (int j = 0; j < 15; ++j)
+            if (j < left) v[j / 4] |= (int)((unsigned)(unsigned char)src[j] << (8 * (j % 4)));
     }
     *(i32x4 *)(a.out + (size_t)at * 16) = v;
 }
