@@ -2,8 +2,8 @@
 // them, which add nothing to a product's sums: two or three matrices of rows
 // of K, one after the other, a chunk a thread.
 //
-// Bound by memory: every row read and written once (2048 + 14336 rows of 4099,
-// 135 MB: 30 us, 4.5 TB/s).  It pays where the product would otherwise read
+// Bound by memory: every row read and written once (2048 + 14336 rows of 4098,
+// 134 MB: 26.8 us, 5.0 TB/s).  It pays where the product would otherwise read
 // each row many times at addresses that start on no 16 bytes.
 typedef signed char i8;
 typedef int i32x4 __attribute__((ext_vector_type(4)));

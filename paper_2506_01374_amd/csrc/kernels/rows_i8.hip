@@ -26,6 +26,14 @@
 // A row of zeros has scale 0 and q 0.  A row that holds a NaN or an infinity,
 // or (NORM) whose squares sum past fp32, has scale NaN and q 0: what is
 // computed from it is NaN, not a silent zero.
+//
+// Bound by memory with many rows: 2048 x 14336 plain, 88 MB, 18.7 us (4.7
+// TB/s); the norm with the residual, 2048 x 4096, 59 MB, 13.1 us (4.5 TB/s),
+// 8192 x 4096 45 us (5.2).  A row stays in registers between the passes:
+// reading it again takes 22.5 us in the first of these.  Bound by the way to
+// memory and back with few: one row of 4096 takes 3.0 us, of which an empty
+// kernel takes 2.2, so that its waves are many and their loads all under way
+// at once.
 
 typedef unsigned short bf16_t;
 typedef unsigned int u32;
