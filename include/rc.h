@@ -292,7 +292,9 @@ rc_status rc_precompile(const rc_op_desc *d, const rc_schedule *s, int32_t n, in
 rc_status rc_set_cache_dir(const char *dir);
 
 /* Bytes of device workspace a launch needs (0 if none).  The caller
- * allocates it; its contents need not be initialised. */
+ * allocates it; its contents need not be initialised.  It serves one launch
+ * at a time: launches that may overlap (on two streams, in two captured
+ * graphs) take one each. */
 rc_status rc_plan_workspace(const rc_plan *p, size_t *bytes);
 /* Number of kernels one launch enqueues, and the index of the one doing
  * most of the FLOPs (the contraction). */

@@ -37,6 +37,7 @@
 
 typedef unsigned short bf16_t;
 typedef unsigned int u32;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 #define LANES (64 * WAVES)
 
@@ -83,13 +84,25 @@ __device__ __forceinline__ void ends(Vec &v, const bf16_t *row, int c, int cols)
         if (c + j < cols) v.w[j / 2] |= (u32)row[c + j] << (16 * (j % 2));
 }
 
-template <class T> __device__ __forceinline__ void store(T *row, const T (&v)[VEC], int c, int cols) {
+// VEC elements of type T, packed in v, to a row of `cols` at c
+template <class T, int W> __device__ __forceinline__ void store(T *row, const u32 (&v)[W], int c, int cols) {
+    constexpr int PER = 4 / sizeof(T);                  // of a word
     if (c + VEC <= cols) {
-        __builtin_memcpy(row + c, v, sizeof v);
+        __builtin_memcpy(row + c, v, VEC * sizeof(T));
     } else {
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
-            if (c + j < cols) row[c + j] = v[j];
+            if (c + j < cols) row[c + j] = (T)(v[j / PER] >> (32 / PER * (j % PER)));
+    }
+}
+
+// the low bytes of t, four a word
+__device__ __forceinline__ void pack(u32 (&q)[(VEC + 3) / 4], const u32 (&t)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < (VEC + 3) / 4; ++i) {
+        const int j = 4 * i;
+        q[i] = VEC > 1 ? __builtin_amdgcn_perm(t[j + (VEC > 1)], t[j], 0x0C0C0400u) : t[j];
+        if (VEC > 3) q[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[j + 3 * (VEC > 3)], t[j + 2 * (VEC > 3)], 0x0C0C0400u), q[i], 0x05040100u);
     }
 }
 
@@ -147,12 +160,11 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
             ends(v[i], x, ci, cols);
 #if RES
             ends(b[i], r, ci, cols);
-            bf16_t h[VEC];
+            Vec h = {};
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) h[j] = f2bf(v[i].at(j) + b[i].at(j));
-            store(ho, h, ci, cols);
-            v[i] = {};
-            __builtin_memcpy(&v[i], h, sizeof h);
+            for (int j = 0; j < VEC; ++j) h.w[j / 2] |= (u32)f2bf(v[i].at(j) + b[i].at(j)) << (16 * (j % 2));
+            store(ho, h.w, ci, cols);
+            v[i] = h;
 #endif
 #if NORM
             ends(wv[i], a.w, ci, cols);
@@ -167,18 +179,24 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
         return v.at(j);
 #endif
     };
-    // the maximum keeps a NaN
+    // the maximum keeps a NaN: of magnitudes as bits, above all others (the
+    // plain kind, two a word), or by the instruction
     float top = 0.f;
+    u16x2 tops2 = {0, 0};
     float ss = 0.f;
     auto take = [&](const Vec &v, const Vec &wv) {
+#if NORM
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             top = __builtin_elementwise_maximum(top, __builtin_fabsf(product(v, wv, j)));
-#if NORM
             const float h = v.at(j);
             ss = __builtin_fmaf(h, h, ss);
-#endif
         }
+#else
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            tops2 = __builtin_elementwise_max(tops2, __builtin_bit_cast(u16x2, v.w[i] & 0x7FFF7FFFu));
+#endif
     };
 
 #if HELD
@@ -192,6 +210,10 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
         read(c, v, wv, 1);
         take(v[0], wv[0]);
     }
+#endif
+
+#if !NORM
+    top = __builtin_bit_cast(float, (u32)(tops2[0] > tops2[1] ? tops2[0] : tops2[1]) << 16);
 #endif
 
     // over the row's lanes and waves, in a fixed order
@@ -240,21 +262,24 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     const u32 keep = bad ? 0u : ~0u;
     auto emit = [&](const Vec &v, const Vec &wv, int c) {
         // trials of all elements, and again where one of them is not nearest
-        signed char o[VEC];
+        u32 o[VEC], q[(VEC + 3) / 4];
         float far = 0.f;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             const float s = product(v, wv, j) * (127.f * up);
             const float t = trial(s, inv);
             far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(-(t - SHIFT), as, s)));
-            o[j] = (signed char)(__builtin_bit_cast(u32, t) & keep);
+            o[j] = __builtin_bit_cast(u32, t);
         }
+        pack(q, o);
         if (far >= 0.5f * as) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                o[j] = (signed char)(nearest(product(v, wv, j) * (127.f * up), as, inv) & keep);
+            for (int j = 0; j < VEC; ++j) o[j] = (u32)nearest(product(v, wv, j) * (127.f * up), as, inv);
+            pack(q, o);
         }
-        store(a.q + base, o, c, cols);
+#pragma unroll
+        for (int i = 0; i < (VEC + 3) / 4; ++i) q[i] &= keep;
+        store(a.q + base, q, c, cols);
     };
 #if HELD
 #pragma unroll
