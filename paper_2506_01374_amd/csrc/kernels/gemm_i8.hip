@@ -12,8 +12,8 @@
 //   WM WN WK     waves along M, N and K (Parallel); NT = 64 * WM * WN * WK
 //   MF           MFMA shape: 16 -> v_mfma_i32_16x16x64_i8,
 //                            32 -> v_mfma_i32_32x32x32_i8
-//   STAGES       1: LDS double buffer with register prefetch of the next K
-//                tile, any sizes (ComputeLocation); 2: a ring of NSTAGE LDS
+//   STAGES       1: LDS double buffer with register prefetch of the next two
+//                K tiles, any sizes (ComputeLocation); 2: a ring of NSTAGE LDS
 //                buffers filled by direct-to-LDS buffer loads issued
 //                NSTAGE - 1 tiles ahead (K a multiple of 16: a lane moves 16
 //                aligned bytes; rows of another length are copied first, by
@@ -44,8 +44,10 @@
 //   4096 x 14336 in 256 x 128 tiles, one round of workgroups: 124 us, 1.93.  A
 //   256 x 256 tile costs some 10 us around its K loop: 3 to the first MFMA, 4
 //   of stores, the rest between workgroups.
-//   The double buffer is 10 to 30 % behind the ring (1024 x 4096 x 4096: 27.9
-//   and 21.4 us); it is there for rows that are no whole 16-byte chunks.
+//   The double buffer is behind the ring (1024 x 4096 x 4096: 23.4 and 21.4
+//   us); it is there for rows that are no whole 16-byte chunks.  With loads two
+//   tiles ahead these take 31.5 us for K of 4099, with one 42.3; loads that
+//   start on 4 bytes 27.3 (K of 4100), as the others are split up on their way.
 //   The 32 x 32 MFMA is about 5 % slower than the 16 x 16 one in the same tile.
 
 #define NT (64 * WM * WN * WK)
@@ -124,37 +126,26 @@ __device__ __forceinline__ int swz_x(int row) {
 }
 __device__ __forceinline__ int swz(int row, int chunk) { return row * TK + ((chunk ^ swz_x(row)) << 4); }
 
-// n fragments of 16 elements at p(i), of which left(i) are in the row (the
-// rest reads zero), of rows `ld` long: loads without a branch, of the row's
-// last 16 where fewer are left, so that none waits for another, which are then
-// moved down.
-template <int CNT, class P, class L> __device__ __forceinline__ void ends16(i32x4 (&v)[CNT], P p, L left, int ld) {
-    if (ld >= 16) {
+// The row's last 16 elements v, moved down so that the last `left` of them
+// (none to 16) are the first, with zeros behind them.
+__device__ __forceinline__ void shift16(i32x4 &v, int left) {
+    const unsigned by = (unsigned)(16 - min(max(left, 0), 16));
+    i32x4 w = v;
+    if (by & 8) w = i32x4{w[2], w[3], 0, 0};
+    if (by & 4) w = i32x4{w[1], w[2], w[3], 0};
 #pragma unroll
-        for (int i = 0; i < CNT; ++i) __builtin_memcpy(&v[i], p(i) + min(left(i) - 16, 0), 16);
+    for (int j = 0; j < 4; ++j)
+        v[j] = by == 16 ? 0 : (int)__builtin_amdgcn_alignbyte(j < 3 ? (unsigned)w[j + 1] : 0u, (unsigned)w[j], by & 3);
+}
+
+// The first `left` elements at p, fewer than 16, and zeros.
+__device__ __forceinline__ i32x4 bytes16(const i8 *p, int left) {
+    unsigned long long w[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < CNT; ++i) {
-            const unsigned by = (unsigned)(16 - min(max(left(i), 0), 16));
-            i32x4 w = v[i];
-            if (by & 8) w = i32x4{w[2], w[3], 0, 0};
-            if (by & 4) w = i32x4{w[1], w[2], w[3], 0};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v[i][j] = by == 16 ? 0 : (int)__builtin_amdgcn_alignbyte(j < 3 ? (unsigned)w[j + 1] : 0u, (unsigned)w[j], by & 3);
-        }
-    } else {
-        // (a row shorter than a load)
-#pragma unroll
-        for (int i = 0; i < CNT; ++i) {
-            unsigned long long w[2] = {0, 0};
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll 1
-                for (int j = 0; j < 8 && 8 * h + j < left(i); ++j)
-                    w[h] |= (unsigned long long)(unsigned char)p(i)[8 * h + j] << (8 * j);
-            v[i] = i32x4{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
-        }
-    }
+        for (int j = 0; j < 8 && 8 * h + j < left; ++j) w[h] |= (unsigned long long)(unsigned char)p[8 * h + j] << (8 * j);
+    return i32x4{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
 }
 
 __device__ __forceinline__ float silu(float x) {
@@ -307,41 +298,39 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     int kc[CH], dst[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int v = tid + i * NT;
+        // (threads past the tile's last chunk move it again)
+        const int v = min(tid + i * NT, (HM + TN) * CPR - 1);
         const int row = v / CPR, c = v % CPR;
         kc[i] = c * 16;
         if (row < HM) {
             dst[i] = swz(row, c);
-            src[i] = Ab + (size_t)min(row, mrows - 1) * ld + kc[i];
+            src[i] = Ab + (size_t)min(row, mrows - 1) * ld;
         } else {
             const int b = row - HM;
-            dst[i] = v < (HM + TN) * CPR ? HM * TK + swz(b, c) : -1;
-            src[i] = (SRC_UP(b) ? B1 : B0) + (size_t)min(SRC_ROW(b), ncols - 1) * ld + kc[i];
+            dst[i] = HM * TK + swz(b, c);
+            src[i] = (SRC_UP(b) ? B1 : B0) + (size_t)min(SRC_ROW(b), ncols - 1) * ld;
         }
     }
-    i32x4 reg[CH];
-    auto fetch = [&](int k0) {
-        if (k0 + TK <= K) {
+    // Two tiles ahead of the one that is multiplied: of tile t + 1, whose
+    // loads had an iteration's time, and of tile t + 2.
+    i32x4 reg[2][CH];
+    const int tiles = (K + TK - 1) / TK, whole = K / TK;
+    auto plain = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) __builtin_memcpy(&reg[i], src[i] + k0, 16);
-        } else {
-            ends16(reg, [&](int i) { return src[i] + k0; }, [&](int i) { return K - k0 - kc[i]; }, ld);
-        }
+        for (int i = 0; i < CH; ++i) __builtin_memcpy(&r[i], src[i] + (kc[i] + t * TK), 16);
     };
-    auto put = [&](int b) {
+    // chunks that are not whole, or past the last: the row's last 16 elements
+    // (a branch around loads would make what follows wait for all of them)
+    auto fetch = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-            if (dst[i] >= 0) *(i32x4 *)(lds + b * BUF + dst[i]) = reg[i];
+        for (int i = 0; i < CH; ++i) __builtin_memcpy(&r[i], src[i] + min(kc[i] + t * TK, K - 16), 16);
     };
-    const int tiles = (K + TK - 1) / TK;
-    fetch(0);
-    put(0);
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-        // buffer (t + 1) & 1 was last read in iteration t - 1, which ended
-        // with a barrier
-        if (t + 1 < tiles) fetch((t + 1) * TK);
-        const i8 *la = lds + (t & 1) * BUF + wm * WTM * TK, *lb = lds + (t & 1) * BUF + (HM + wn * WTN) * TK;
+    auto put = [&](const i32x4 (&r)[CH], int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) *(i32x4 *)(lds + b * BUF + dst[i]) = r[i];
+    };
+    auto multiply = [&](int b) __attribute__((always_inline)) {
+        const i8 *la = lds + b * BUF + wm * WTM * TK, *lb = lds + b * BUF + (HM + wn * WTN) * TK;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             i32x4 fa[FM], fb[FN];
@@ -354,8 +343,51 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
 #pragma unroll
                 for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[j], fa[i], acc[i][j]);
         }
-        if (t + 1 < tiles) put((t + 1) & 1);
+    };
+    auto ends = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
+        if (t == whole)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) shift16(r[i], K - t * TK - kc[i]);
+    };
+    if (ld < 16) {                                      // (rows shorter than a load: one tile)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) reg[0][i] = bytes16(src[i] + kc[i], K - kc[i]);
+        put(reg[0], 0);
         __syncthreads();
+        multiply(0);
+    } else {
+        fetch(reg[0], 0);
+        fetch(reg[1], 1);
+        ends(reg[0], 0);
+        put(reg[0], 0);
+        __syncthreads();
+        // buffer (t + 1) & 1 was last read in iteration t - 1, which ended
+        // with a barrier
+        int t = 0;
+        for (; t + 3 < whole; t += 2) {
+            plain(reg[0], t + 2);
+            multiply(0);
+            put(reg[1], 1);
+            __syncthreads();
+            plain(reg[1], t + 3);
+            multiply(1);
+            put(reg[0], 0);
+            __syncthreads();
+        }
+        for (;; t += 2) {
+            fetch(reg[0], t + 2);
+            multiply(0);
+            if (t + 1 >= tiles) break;
+            ends(reg[1], t + 1);
+            put(reg[1], 1);
+            __syncthreads();
+            fetch(reg[1], t + 3);
+            multiply(1);
+            if (t + 2 >= tiles) break;
+            ends(reg[0], t + 2);
+            put(reg[0], 0);
+            __syncthreads();
+        }
     }
 #elif STAGES == 2
     // buffer_load_dwordx4 ... lds moves 64 lanes x 16 B into 1 KiB of LDS at
@@ -616,12 +648,27 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
         multiply(f[1]);
         k0 = k2;
     }
-    // what is left of K, a step a wave
+    // what is left of K, a step a wave: loads of the row's last 16 elements
+    // where fewer are left, all under way before one is moved down
     for (int k = whole + wave * 64; k < K; k += WK * 64) {
-        const int left = K - k - lane / 16 * 16;
+        const int left = K - k - lane / 16 * 16, back = min(left - 16, 0);
         i32x4 a[FM], b[FN];
-        ends16(a, [&](int i) { return Ab + k + ao[i]; }, [&](int) { return left; }, ld);
-        ends16(b, [&](int j) { return (SRC_UP(j * 16) ? B1 : B0) + k + bo[j]; }, [&](int) { return left; }, ld);
+        if (ld >= 16) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) __builtin_memcpy(&a[i], Ab + (k + back) + (size_t)ao[i], 16);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) __builtin_memcpy(&b[j], (SRC_UP(j * 16) ? B1 : B0) + (k + back) + (size_t)bo[j], 16);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) shift16(a[i], left);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) shift16(b[j], left);
+        } else {
+            // (a row shorter than a load)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) a[i] = bytes16(Ab + k + ao[i], left);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) b[j] = bytes16((SRC_UP(j * 16) ? B1 : B0) + k + bo[j], left);
+        }
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll

@@ -827,21 +827,21 @@ static const RingTile RING_TILES[] = {
 // at 3.9 us and 4.2 TB/s for the copy, or the double buffer, whose workgroups
 // on one CU (`wgs`) together take `pace` each for 1000 of K, but no less than
 // `least`, both 25 % less where rows start on 4 bytes, and which stores
-// `store` TB/s at most.  Over 154 sizes (1 to 4096 rows, K of 515 to 14339)
-// the suggestion takes 2.9 % more than the best of some 40 measured (us,
-// copy and double buffer: 2048 x 14336 x 4098 166 and 213, 4096 x 4096 x 14339
-// 291 and 392; but 512 x 14336 x 4098 68 and 53, 256 x 2048 x 1004 9.2 and
-// 5.8).  The large tile pays where K is short (4096 x 14336 x 64: 34, 128 x
-// 128 tiles 40, 32 x 32 64).
+// `store` TB/s at most.  Over 153 sizes (1 to 4096 rows, K of 515 to 14339)
+// the suggestion takes 2.1 % more than the best of some 40 measured (us, copy
+// and double buffer: 2048 x 14336 x 4098 170 and 211, 4096 x 4096 x 14339 291
+// and 422; but 512 x 14336 x 4098 68 and 51, 256 x 2048 x 1004 9.2 and 5.2).
+// The large tile pays where K is short (4096 x 14336 x 64: 37, 128 x 128 tiles
+// 41, 32 x 32 64).
 struct BufferTile {
     int tm, tn, tk, wm, wn, wgs;
     double turn, least, pace, store;
 };
-static const BufferTile BUFFER_TILES[] = {{256, 128, 64, 4, 2, 2, 2.4, 16.3, 13.0, 3.8},
-                                          {128, 128, 128, 2, 4, 2, 2.3, 8.7, 6.7, 3.1},
-                                          {64, 64, 128, 2, 4, 2, 0.4, 4.9, 3.0, 2.4},
-                                          {32, 32, 128, 2, 2, 4, 0.0, 3.7, 1.5, 1.9},
-                                          {16, 32, 128, 1, 2, 8, 0.0, 3.3, 1.05, 1.4}};
+static const BufferTile BUFFER_TILES[] = {{256, 128, 64, 4, 2, 2, 2.2, 6.6, 12.8, 3.8},
+                                          {128, 128, 128, 2, 4, 2, 2.6, 1.2, 6.5, 3.1},
+                                          {64, 64, 128, 2, 4, 2, 0.5, 3.2, 3.0, 2.4},
+                                          {32, 32, 128, 2, 2, 4, 0.0, 2.0, 1.45, 1.9},
+                                          {16, 32, 128, 1, 2, 8, 0.0, 1.9, 1.03, 1.4}};
 
 static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t M = d->dim[0], N = d->dim[1], K = d->dim[2];
@@ -863,16 +863,16 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
     // 7.0 and 5.8); up to 64 rows where 16 x 16 tiles with a
     // short K are one round (64 x 1024 x 1024: 3.9 and 4.2); up to 16 rows
     // with very large weights (16 x 16384 x 16384: 51.6 and 55.4).  K that is
-    // no multiple of 16 (against the double buffer): two rounds of such tiles
-    // (16 x 1000 x 1001: 4.6 and 5.7; 64 x 1000 x 1001 gated 5.6 and 7.3), and
-    // up to 32 rows that start on 4 bytes (32 x 4096 x 4100: 8.4 and 11.0; but
-    // 32 x 4096 x 4099 19.2 and 11.9, 32 x 14336 x 4100 gated 48 and 36).
+    // no multiple of 16 (against the double buffer): such a round too (16 x
+    // 2048 x 1004: 3.6 and 4.3), and up to 32 rows that start on 4 bytes (32 x
+    // 4096 x 4100: 8.7 and 9.9; but 32 x 4096 x 4099 19.2 and 10.3, 16 x 5000
+    // x 515 5.2 and 4.3, 32 x 14336 x 4100 gated 48 and 32).
     const int64_t small = count(M, 16) * count(nb * N, 16);
     if (!pad && M <= 8 && nb * N >= (K > 4096 ? 4096 : 2048) && nb * N <= 8192) {
         for (int wk = 4; wk >= 1; wk /= 2)
             if (tile(16, 16, K > 64 ? 128 : 64, 1, 1, wk, 3, 1, 0)) return;
     }
-    if ((M <= 64 && small <= (pad ? 512 : 256) && K <= 1024) || (pad && K % 4 == 0 && M <= (nb * N <= 8192 ? 32 : 16))) {
+    if ((M <= 64 && small <= 256 && K <= 1024) || (pad && K % 4 == 0 && M <= (nb * N <= 8192 ? 32 : 16))) {
         for (int wk = K > 2048 ? 8 : 4; wk >= 1; wk /= 2)
             if (tile(K > 1024 && M > 16 ? 32 : 16, 16, K > 512 ? 256 : 64, 1, 1, wk, 3, 1, 0)) return;
     }

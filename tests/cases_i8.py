@@ -47,10 +47,12 @@ GEMM_TEXTS += [_TILE.format(*t) + ",pad=1" for t in (
     (16, 16, 256, 1, 1, 1, 16, 2, 1, 1, 1), (256, 256, 64, 2, 4, 1, 16, 2, 1, 1, 1), (128, 128, 128, 2, 4, 1, 16, 2, 1, 1, 2))]
 
 # (M, N, K): one of each, around 16 and the tiles, K around a chunk, an MFMA
-# step and the K tiles, rows that start on no alignment
+# step and the K tiles, rows that start on no alignment, a last split of K
+# that is shorter than a load (773 in four splits of tiles of 64)
 GEMM_DIMS = [(1, 1, 1), (1, 17, 16), (2, 3, 15), (15, 16, 17), (16, 100, 64), (17, 33, 65), (1, 260, 1000), (33, 64, 63),
              (64, 129, 127), (65, 128, 128), (100, 61, 129), (130, 257, 256), (257, 130, 257), (300, 272, 400),
-             (128, 256, 1040), (16, 64, 4096), (70, 96, 2064), (300, 260, 1001), (16, 40, 2050), (5, 48, 1100)]
+             (128, 256, 1040), (16, 64, 4096), (70, 96, 2064), (300, 260, 1001), (16, 40, 2050), (5, 48, 1100),
+             (20, 40, 773)]
 
 
 # a last, partial round of workgroups in half-height tiles: with a last row
