@@ -314,13 +314,14 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
     // Two tiles ahead of the one that is multiplied: of tile t + 1, whose
     // loads had an iteration's time, and of tile t + 2.
     i32x4 reg[2][CH];
-    const int tiles = (K + TK - 1) / TK, whole = K / TK;
+    const int tiles = (K + TK - 1) / TK;
     auto plain = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) __builtin_memcpy(&r[i], src[i] + (kc[i] + t * TK), 16);
     };
-    // chunks that are not whole, or past the last: the row's last 16 elements
-    // (a branch around loads would make what follows wait for all of them)
+    // the last tile's too: the row's last 16 elements for a chunk that is not
+    // whole or past the row (a branch around loads would make what follows wait
+    // for all of them)
     auto fetch = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) __builtin_memcpy(&r[i], src[i] + min(kc[i] + t * TK, K - 16), 16);
@@ -345,48 +346,51 @@ template <int HM> __device__ __forceinline__ void product(const GemmI8Args &args
         }
     };
     auto ends = [&](i32x4 (&r)[CH], int t) __attribute__((always_inline)) {
-        if (t == whole)
+        if (t * TK + TK > K)
 #pragma unroll
             for (int i = 0; i < CH; ++i) shift16(r[i], K - t * TK - kc[i]);
     };
     if (ld < 16) {                                      // (rows shorter than a load: one tile)
 #pragma unroll
         for (int i = 0; i < CH; ++i) reg[0][i] = bytes16(src[i] + kc[i], K - kc[i]);
+    } else {
+        fetch(reg[0], 0);
+        if (tiles > 1) fetch(reg[1], 1);
+        ends(reg[0], 0);
+    }
+    put(reg[0], 0);
+    __syncthreads();
+    // Tile t is in buffer 0 and t + 1 in reg[1].  Buffer (t + 1) & 1 was last
+    // read in iteration t - 1, which ended with a barrier.
+    int t = 0;
+    for (; t + 3 < tiles; t += 2) {
+        plain(reg[0], t + 2);
+        multiply(0);
+        put(reg[1], 1);
+        __syncthreads();
+        fetch(reg[1], t + 3);
+        multiply(1);
+        put(reg[0], 0);
+        __syncthreads();
+    }
+    // one to three tiles are left
+    if (t + 3 == tiles) {
+        fetch(reg[0], t + 2);
+        multiply(0);
+        put(reg[1], 1);
+        __syncthreads();
+        multiply(1);
+        ends(reg[0], t + 2);
         put(reg[0], 0);
         __syncthreads();
         multiply(0);
     } else {
-        fetch(reg[0], 0);
-        fetch(reg[1], 1);
-        ends(reg[0], 0);
-        put(reg[0], 0);
-        __syncthreads();
-        // buffer (t + 1) & 1 was last read in iteration t - 1, which ended
-        // with a barrier
-        int t = 0;
-        for (; t + 3 < whole; t += 2) {
-            plain(reg[0], t + 2);
-            multiply(0);
-            put(reg[1], 1);
-            __syncthreads();
-            plain(reg[1], t + 3);
-            multiply(1);
-            put(reg[0], 0);
-            __syncthreads();
-        }
-        for (;; t += 2) {
-            fetch(reg[0], t + 2);
-            multiply(0);
-            if (t + 1 >= tiles) break;
+        multiply(0);
+        if (t + 2 == tiles) {
             ends(reg[1], t + 1);
             put(reg[1], 1);
             __syncthreads();
-            fetch(reg[1], t + 3);
             multiply(1);
-            if (t + 2 >= tiles) break;
-            ends(reg[0], t + 2);
-            put(reg[0], 0);
-            __syncthreads();
         }
     }
 #elif STAGES == 2

@@ -828,7 +828,7 @@ static const RingTile RING_TILES[] = {
 // on one CU (`wgs`) together take `pace` each for 1000 of K, but no less than
 // `least`, both 25 % less where rows start on 4 bytes, and which stores
 // `store` TB/s at most.  Over 153 sizes (1 to 4096 rows, K of 515 to 14339)
-// the suggestion takes 2.1 % more than the best of some 40 measured (us, copy
+// the suggestion takes 1.9 % more than the best of some 40 measured (us, copy
 // and double buffer: 2048 x 14336 x 4098 170 and 211, 4096 x 4096 x 14339 291
 // and 422; but 512 x 14336 x 4098 68 and 51, 256 x 2048 x 1004 9.2 and 5.2).
 // The large tile pays where K is short (4096 x 14336 x 64: 37, 128 x 128 tiles
