@@ -496,7 +496,10 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     if (wk > 1 && st != 3) return "waves share a tile's K in the streaming stage (3) only";
     const int64_t stage_bytes = (int64_t)(tm + tn) * tk;
     int64_t lds = 2 * stage_bytes;
-    int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 4;     // register staging of the next tile
+    // register staging of the next two tiles, with 4 registers of addresses a
+    // chunk, one k-step's fragments, and 16 that the compiler adds (64 x 64 x
+    // 128 to 256 x 128 x 64 take 62 to 177 in all)
+    int64_t regs = acc + (stage_bytes / 16 + nt - 1) / nt * 12 + 4 * (tm / wm / mf + tn / wn / mf) + 16;
     int64_t waves = (int64_t)wm * wn;
     if (st == 2) {
         if (K % 16) return fmt("the direct-to-LDS ring moves 16 aligned bytes a lane: K = %lld is no multiple of 16 (pad 1 makes it one)", (long long)K);
@@ -526,12 +529,12 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
         if (!gemm_i8_tail_tiles(((M + tm - 1) / tm) * ((N + tno - 1) / tno), tm, tn, tk, (int)waves, occ))
             return "tail: no partial round of workgroups that half-height tiles shorten";
     }
+    const int64_t wgs = occ > 1 ? (occ * 4 + waves - 1) / waves : 1;
+    if (wgs * lds > LDS_LIMIT) return fmt("%lld workgroups of %lld B LDS do not fit a CU", (long long)wgs, (long long)lds);
     // registers of a lane: all waves of a workgroup are resident together
     const int64_t per_simd = std::max<int64_t>(occ, (waves + 3) / 4);
     if (regs + 24 > 512 / per_simd)
         return fmt("%lld accumulator and operand registers per lane leave too few at %lld waves/SIMD", (long long)regs, (long long)per_simd);
-    const int64_t wgs = occ > 1 ? (occ * 4 + waves - 1) / waves : 1;
-    if (wgs * lds > LDS_LIMIT) return fmt("%lld workgroups of %lld B LDS do not fit a CU", (long long)wgs, (long long)lds);
     return "";
 }
 
