@@ -27,13 +27,15 @@
 // or (NORM) whose squares sum past fp32, has scale NaN and q 0: what is
 // computed from it is NaN, not a silent zero.
 //
-// Bound by memory with many rows: 2048 x 14336 plain, 88 MB, 18.7 us (4.7
-// TB/s); the norm with the residual, 2048 x 4096, 59 MB, 13.1 us (4.5 TB/s),
-// 8192 x 4096 45 us (5.2).  A row stays in registers between the passes:
-// reading it again takes 22.5 us in the first of these.  Bound by the way to
-// memory and back with few: one row of 4096 takes 3.0 us, of which an empty
-// kernel takes 2.2, so that its waves are many and their loads all under way
-// at once.
+// Bound by memory with many rows: 2048 x 14336 plain, 88 MB, 16.7 us (5.3
+// TB/s); the norm with the residual, 2048 x 4096, 59 MB, 12.4 us (4.7 TB/s),
+// 8192 x 4096 43.3 us (5.4).  Vector instructions are next: the integers took
+// three times as many, and the first of these 22.0 us, before one trial and
+// one check of a vector's remainders replaced a comparison for each.  A row
+// stays in registers between the passes: reading it again takes 18.8 us there.
+// Bound by the way to memory and back with few rows: one row of 4096 takes 3.0
+// us, of which an empty kernel takes 2.2, so that its waves are many and their
+// loads all under way at once.
 
 typedef unsigned short bf16_t;
 typedef unsigned int u32;
@@ -115,8 +117,8 @@ __device__ __forceinline__ float trial(float s, float inv) { return __builtin_fm
 // rint(s / a), halves to even, s = 127 p and |p| <= a.  The trial t is within
 // one of the result, and s - t a is exact: both terms are multiples of the
 // smaller term's last bit, and their difference is below 2 a, so that it has
-// no more bits than s has (t = 0 leaves s).  Where it is below a / 2, t is
-// the result.
+// no more bits than s has (t = 0 leaves s).  Where it is below a / 2, or that
+// with an even t, t is the result.
 __device__ __forceinline__ int nearest(float s, float a, float inv) {
     const float t = trial(s, inv);
     const float rem = __builtin_fmaf(-(t - SHIFT), a, s);
@@ -258,7 +260,9 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     if (top < 0x1p-63f) up = 0x1p64f;
     if (top >= 0x1p64f) up = 0x1p-64f;
     const float as = bad || top == 0.f ? 1.f : top * up;
-    const float inv = __builtin_amdgcn_rcpf(as);
+    // above 1 / a by its last bits: then the trial of p = a / 2, the one tie
+    // that is met often, is 64, the even neighbour of 63.5
+    const float inv = __builtin_amdgcn_rcpf(as) * 0x1.000004p0f;
     const u32 keep = bad ? 0u : ~0u;
     auto emit = [&](const Vec &v, const Vec &wv, int c) {
         // trials of all elements, and again where one of them is not nearest
@@ -268,11 +272,19 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
         for (int j = 0; j < VEC; ++j) {
             const float s = product(v, wv, j) * (127.f * up);
             const float t = trial(s, inv);
-            far = __builtin_fmaxf(far, __builtin_fabsf(__builtin_fmaf(-(t - SHIFT), as, s)));
             o[j] = __builtin_bit_cast(u32, t);
+            float rem = __builtin_fmaf(-(t - SHIFT), as, s);
+#if !NORM
+            // Ties: an odd trial's last bit makes a remainder of a / 2 larger
+            // (a and so a / 2 have 8 bits, their last one is 0), and no smaller
+            // one as large.  (bf16 values of half the maximum are many; of a
+            // norm's products few are, and every tie is done again.)
+            rem = __builtin_bit_cast(float, __builtin_bit_cast(u32, rem) | (o[j] & 1));
+#endif
+            far = __builtin_fmaxf(far, __builtin_fabsf(rem));
         }
         pack(q, o);
-        if (far >= 0.5f * as) {
+        if (NORM ? far >= 0.5f * as : far > 0.5f * as) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j) o[j] = (u32)nearest(product(v, wv, j) * (127.f * up), as, inv);
             pack(q, o);

@@ -762,15 +762,15 @@ static void set_knob(const rc_op_desc *d, rc_schedule *s, const char *name, int3
 
 // Rows to int8: a row in registers, 16-byte loads, a workgroup a row.  Few
 // rows: as many waves as the row's vectors fill, up to 16, as the time is that
-// of one row (us: one row of 4096, 8 waves of one vector 3.2, 4 of two 3.8; 16
-// rows of 14336, 16 of two 4.4, 8 of four 5.0).  From 2^22 elements on up to 8
+// of one row (us: one row of 4096, 8 waves of one vector 3.0, 4 of two 3.3; 16
+// rows of 14336, 16 of two 3.9, 8 of four 4.3).  From 2^22 elements on up to 8
 // waves, and without the residual two vectors a thread before more waves, so
-// that a CU holds more workgroups in different phases (4096 x 8192: 4 waves of
-// four 22.0, 16 of one 27.5; 2048 x 14336: 8 of four 18.8, 16 of two 20.5; but
-// with the residual, 4096 x 14336: 16 of two 76, 8 of four 78, and 8192 x
-// 4096: 8 of one 45.1, 4 of two 46.3).  Narrow rows take 8- and 4-byte loads
+// that a CU holds more workgroups in different phases (4096 x 8192: 8 waves of
+// two 20.6, 16 of one 22.5; 16384 x 4096: 4 of two 36.4, 8 of one 41.3; but
+// with the residual, 4096 x 14336: 16 of two 75, 8 of four 76, and 8192 x
+// 4096: 8 of one 43.3, 4 of two 43.9).  Narrow rows take 8- and 4-byte loads
 // and four rows a workgroup (4096 x 128 with the residual: 4-byte loads 3.4,
-// 8-byte 3.7, 16-byte 4.3, one row a workgroup of these 4.0 and 4.6).
+// 8-byte 3.6, 16-byte 4.2, one row a workgroup of these 3.8, 4.0 and 4.5).
 static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
     const int64_t T = d->dim[0], C = d->dim[1];
     const bool many = T * C >= 1 << 22, lean = many && !(d->flags & RC_FLAG_RESIDUAL);
