@@ -13,6 +13,7 @@
 #include <cstdio>
 #include <algorithm>
 #include <cstring>
+#include <new>
 #include <string>
 
 #include "rc_internal.h"
@@ -1080,7 +1081,7 @@ rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out) {
     return RC_OK;
 }
 
-rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) {
+rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) try {
     if (!desc_ok(d) || !out) return fail(RC_ERR_INVALID_ARGUMENT, "bad descriptor");
     rc_schedule s;
     std::memset(&s, 0, sizeof s);
@@ -1098,6 +1099,8 @@ rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) {
     if (!why.empty()) return fail(RC_ERR_UNSUPPORTED, "no schedule to suggest: " + why);
     *out = s;
     return RC_OK;
+} catch (const std::bad_alloc &) {
+    return RC_ERR_OUT_OF_MEMORY;
 }
 
 rc_status rc_validate(const rc_op_desc *d, const rc_schedule *s, char *why, size_t why_len) {

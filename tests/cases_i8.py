@@ -129,6 +129,8 @@ def compile_jobs():
         for dims, text in gemm_jobs(flags) + tail_jobs(flags):
             op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
             jobs.append((op, [op.from_string(text)]))
+    op = rc.Op(rc.RC_OP_GEMM_I8, (130, 200, 1001), B)
+    jobs.append((op, [op.schedule(tile_m=64, tile_n=64, tile_k=128, waves_m=2, waves_n=2, stages=2, order=1, splits=2, pad=1)]))
     for dims, knobs in LARGE:
         op = rc.Op(rc.RC_OP_GEMM_I8, dims)
         jobs.append((op, [op.schedule(**knobs)]))

@@ -457,6 +457,45 @@ def test_one_plan_on_two_streams():
         assert np.all(np.abs(f64(outs[i]) - want) <= tol)
 
 
+def test_captured_products_of_three_launches():
+    # copied rows, the ring on two K splits and their sum: two graphs with a
+    # workspace each, replayed on two streams and next to eager launches
+    dims, flags = (130, 200, 1001), B
+    op = rc.Op(rc.RC_OP_GEMM_I8, dims, flags)
+    text = "tile_m=64,tile_n=64,tile_k=128,waves_m=2,waves_n=2,mfma=16,stages=2,order=1,splits=2,pad=1"
+    plan = rc.Plan(op, op.from_string(text))
+    assert plan.nkernels == 3 and plan.dominant == 1
+    sets = []
+    for i in range(2):
+        ins = gemm_inputs(dims, flags, 90 + i)
+        sets.append((ins, [x.cuda() for x in ins], torch.empty(dims[:2], dtype=torch.bfloat16, device="cuda"),
+                     plan.workspace(), torch.cuda.CUDAGraph(), torch.cuda.Stream()))
+    for _, dev, out, ws, graph, _ in sets:
+        plan.launch(dev, out, ws)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            plan.launch(dev, out, ws)
+    for turn in range(3):
+        for i, (ins, dev, out, ws, _, _) in enumerate(sets):
+            ins[:] = gemm_inputs(dims, flags, 100 + 2 * turn + i)
+            for x, y in zip(dev, ins):
+                x.copy_(y)
+            out.zero_()
+            ws.fill_(0x55)
+        torch.cuda.synchronize()
+        for *_, graph, stream in sets:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for ins, dev, out, ws, _, _ in sets:
+            want, tol = gemm_reference(ins, flags)
+            assert np.all(np.abs(f64(out) - want) <= tol)
+            eager = torch.empty_like(out)
+            plan.launch(dev, eager, ws)
+            torch.cuda.synchronize()
+            assert torch.equal(eager, out)
+
+
 def test_refused_launches():
     op = rc.Op(rc.RC_OP_GEMM_I8, (10, 20, 64))
     plan = rc.Plan(op, op.suggest())
