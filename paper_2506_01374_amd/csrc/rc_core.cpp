@@ -809,10 +809,9 @@ static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
 //   start + rounds (turn + K pace), at least what the bytes take from HBM,
 // with rounds of workgroups over the chip and K the depth of one split, plus
 // the joining launch of K splits.  The constants (us, and us per 1000 of K)
-// are measured ones of each tile: over 236 sizes (1 to 4096 rows, weights of
-// 256 x 256 to 14336 x 4096 and 4096 x 14336, plain and gated) the schedule
-// with the least estimate takes 1.2 % more than the best of some 40 measured
-// (geometric mean).  One tile for all sizes is far off: 256 x 256 x 64 takes
+// are measured ones of each tile: over 452 sizes (1 to 5000 rows, weights of
+// 256 x 256 to 28672 x 8192, plain and gated) the suggestion takes 1.3 % more
+// than the best of some 20 to 40 measured (geometric mean).  One tile for all sizes is far off: 256 x 256 x 64 takes
 // 62.6 us for 4096 x 4096 x 4096 and 128 x 128 x 128 85, but for 1024 rows 56
 // and 22, and for 64 rows 32 x 32 x 256 takes 7.3 where 128 x 128 x 128
 // takes 21.
@@ -898,11 +897,14 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
         const int64_t lds = (int64_t)gemm_i8_ring_stages(t.tm, t.tn, t.tk, waves, 1) * (t.tm + t.tn) * t.tk;
         const int64_t slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
         const int64_t tiles = count(M, t.tm) * count(N, t.tn / nb);
+        // a round of half-height tiles (1536 x 8192 x 8192 in 256 x 128 tiles
+        // with such a round: 134 us, in 256 x 256 tiles 108)
+        const double half = t.tm * t.tn == 256 * 128 ? 0.6 : 0.5;
         for (int sp = 1; sp <= 16; sp *= 2) {
             const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0;
             for (int tail = 0; tail <= (sp == 1); ++tail) {
                 const int64_t w = tiles * sp;
-                const double rounds = tail ? (double)(w / slots) + 0.5 : (double)count(w, slots);
+                const double rounds = tail ? (double)(w / slots) + half : (double)count(w, slots);
                 double us = t.start + rounds * (t.turn + kp * t.pace);
                 us = std::max(us, 2.8 + bytes / std::min(5.6e6, (double)w * 4e4)) + copy + join(sp);
                 all.push_back({us, t.tm, t.tn / nb, t.tk, t.wm, t.wn, 2, sp, tail});
