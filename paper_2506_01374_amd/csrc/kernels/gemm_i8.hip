@@ -46,8 +46,8 @@
 //   of stores, the rest between workgroups.
 //   The double buffer is behind the ring (1024 x 4096 x 4096: 23.4 and 21.4
 //   us); it is there for rows that are no whole 16-byte chunks.  With loads two
-//   tiles ahead these take 31.5 us for K of 4099, with one 42.3; loads that
-//   start on 4 bytes 27.3 (K of 4100), as the others are split up on their way.
+//   tiles ahead these take 31.5 us for K of 4099, with one 42.3, and 27.3 for K
+//   of 4100, whose rows start on 4 bytes.
 //   The 32 x 32 MFMA is about 5 % slower than the 16 x 16 one in the same tile.
 
 #define NT (64 * WM * WN * WK)
