@@ -430,7 +430,7 @@ static std::string check_i8_desc(const rc_op_desc *d, bool *size) {
             // fall through: the same row sizes
         case RC_OP_QUANT_I8:
             *size = true;
-            if (D[0] * 64 > MAX_GRID_THREADS) return fmt("%lld rows of a wave each exceed the grid's 2^32 - 1 threads", (long long)D[0]);
+            if (D[0] > MAX_GRID_THREADS / 64) return fmt("%lld rows of a wave each exceed the grid's 2^32 - 1 threads", (long long)D[0]);
             if (D[1] > (1LL << 30)) return fmt("rows of %lld elements exceed the 32-bit column indices", (long long)D[1]);
             return "";
         case RC_OP_GEMM_I8:
@@ -1085,6 +1085,10 @@ rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out) {
 
 rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) try {
     if (!desc_ok(d) || !out) return fail(RC_ERR_INVALID_ARGUMENT, "bad descriptor");
+    // (the rules below multiply sizes)
+    bool size = false;
+    const std::string bad = check_i8_desc(d, &size);
+    if (!bad.empty()) return fail(RC_ERR_UNSUPPORTED, "no schedule to suggest: " + bad);
     rc_schedule s;
     std::memset(&s, 0, sizeof s);
     s.struct_size = sizeof s;
