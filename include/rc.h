@@ -372,9 +372,16 @@ typedef struct rc_args {
 /* Enqueue one execution of the operator on `stream`.  Checks pointers
  * (non-NULL, 16-byte aligned) and the workspace size; never synchronises.
  * The plan of an 8-bit kind is launched with the device current that it was
- * created on (RC_ERR_INVALID_ARGUMENT otherwise). */
+ * created on, and what it writes (outputs, workspace) overlaps none of its
+ * other buffers but for RC_OP_RMSNORM_I8's h, as stated there
+ * (RC_ERR_INVALID_ARGUMENT otherwise). */
 rc_status rc_launch(const rc_plan *p, const rc_args *a, void *workspace, size_t ws_bytes,
                     void *stream);
+
+/* rc_launch's checks of the pointers, host only: NULL, alignment and, for the
+ * 8-bit kinds, overlap, with a workspace of `ws_bytes` bytes in use (NULL and 0
+ * for none). */
+rc_status rc_check_args(const rc_op_desc *d, const rc_args *a, const void *workspace, size_t ws_bytes);
 
 /* Enqueue one execution with a HIP event recorded before and after each
  * kernel: events[0..nkernels] (caller-created hipEvent_t, passed as void*).

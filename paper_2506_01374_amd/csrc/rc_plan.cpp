@@ -1193,13 +1193,56 @@ rc_status rc_time_release(void) {
     return r;
 }
 
-static rc_status check_args(const rc_plan *p, const rc_args *a, void *ws, size_t ws_bytes) {
-    if (!p || !a) return fail(RC_ERR_INVALID_ARGUMENT, "null plan or args");
-    const int no = n_outputs(p->desc);
+// Bytes of the operands of an 8-bit kind.
+static void i8_operand_bytes(const rc_op_desc &d, size_t (&in)[8], size_t (&out)[4]) {
+    const size_t r = (size_t)d.dim[0], c = (size_t)d.dim[1], k = (size_t)d.dim[2];
+    if (d.kind == RC_OP_GEMM_I8) {
+        const size_t v[] = {r * k, 4 * r, c * k, 4 * c, (d.flags & RC_FLAG_GATED) ? c * k : 4 * c, 4 * c};
+        std::copy(v, v + 6, in);
+        out[0] = r * c * ((d.flags & RC_FLAG_OUT_F32) ? 4 : 2);
+    } else {
+        in[0] = in[2] = out[2] = 2 * r * c;
+        in[1] = 2 * c;
+        out[0] = r * c;
+        out[1] = 4 * r;
+    }
+}
+
+// The first overlap of what a launch of an 8-bit kind writes (outputs and
+// workspace) with anything else it is given, "" if none.  Workgroups read
+// their inputs while others write: an overlap would give wrong results
+// without an error.
+static std::string i8_overlap(const rc_op_desc &d, const rc_args *a, const void *ws, size_t ws_bytes) {
+    const int ni = n_inputs(d), no = n_outputs(d);
+    size_t in[8] = {}, out[4] = {};
+    i8_operand_bytes(d, in, out);
+    auto meet = [](const void *p, size_t n, const void *q, size_t m) {
+        return (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n;
+    };
+    auto said = [](const char *what, int i, const char *with, int j) {
+        return std::string(what) + (i < 0 ? "" : " " + std::to_string(i)) + " overlaps " + with + " " + std::to_string(j);
+    };
+    for (int o = 0; o < no; ++o) {
+        for (int i = 0; i < ni; ++i) {
+            // the norm's h may be x or r: a thread reads what it then replaces
+            if (d.kind == RC_OP_RMSNORM_I8 && o == 2 && i != 1 && a->out[o] == a->in[i]) continue;
+            if (meet(a->out[o], out[o], a->in[i], in[i])) return said("output", o, "input", i);
+        }
+        for (int i = 0; i < o; ++i)
+            if (meet(a->out[o], out[o], a->out[i], out[i])) return said("output", o, "output", i);
+        if (ws && meet(ws, ws_bytes, a->out[o], out[o])) return said("the workspace", -1, "output", o);
+    }
+    for (int i = 0; ws && i < ni; ++i)
+        if (meet(ws, ws_bytes, a->in[i], in[i])) return said("the workspace", -1, "input", i);
+    return "";
+}
+
+static rc_status check_pointers(const rc_op_desc &d, const rc_args *a) {
+    const int no = n_outputs(d);
     // a block without out[2] and out[3] serves operators that have none
     const size_t least = no > 2 ? sizeof(rc_args) : offsetof(rc_args, out) + 2 * sizeof(void *);
     if (a->struct_size < least) return fail(RC_ERR_INVALID_ARGUMENT, "rc_args struct_size too small");
-    int ni = n_inputs(p->desc);
+    int ni = n_inputs(d);
     for (int i = 0; i < ni; ++i) {
         if (!a->in[i]) return fail(RC_ERR_INVALID_ARGUMENT, "input " + std::to_string(i) + " is NULL");
         if ((uintptr_t)a->in[i] & 15) return fail(RC_ERR_MISALIGNED, "input " + std::to_string(i) + " is not 16-byte aligned");
@@ -1209,6 +1252,30 @@ static rc_status check_args(const rc_plan *p, const rc_args *a, void *ws, size_t
         if (!a->out[i]) return fail(RC_ERR_INVALID_ARGUMENT, name(i) + " is NULL");
         if ((uintptr_t)a->out[i] & 15) return fail(RC_ERR_MISALIGNED, name(i) + " is not 16-byte aligned");
     }
+    return RC_OK;
+}
+
+static rc_status check_buffers(const rc_op_desc &d, const rc_args *a, const void *ws, size_t ws_bytes) {
+    if (ws && ((uintptr_t)ws & 255)) return fail(RC_ERR_MISALIGNED, "workspace is not 256-byte aligned");
+    if (d.kind >= RC_OP_RMSNORM_I8) {
+        const std::string bad = i8_overlap(d, a, ws, ws_bytes);
+        if (!bad.empty()) return fail(RC_ERR_INVALID_ARGUMENT, bad);
+    }
+    return RC_OK;
+}
+
+rc_status rc_check_args(const rc_op_desc *d, const rc_args *a, const void *workspace, size_t ws_bytes) {
+    if (!desc_ok(d) || !a) return fail(RC_ERR_INVALID_ARGUMENT, "bad descriptor or args");
+    rc_status r = check_pointers(*d, a);
+    if (r == RC_OK) r = check_buffers(*d, a, workspace, ws_bytes);
+    if (r == RC_OK) clear_error();
+    return r;
+}
+
+static rc_status check_args(const rc_plan *p, const rc_args *a, void *ws, size_t ws_bytes) {
+    if (!p || !a) return fail(RC_ERR_INVALID_ARGUMENT, "null plan or args");
+    rc_status r = check_pointers(p->desc, a);
+    if (r != RC_OK) return r;
     if (p->desc.kind >= RC_OP_RMSNORM_I8) {
         int dev = -1;
         hipError_t e = hipGetDevice(&dev);
@@ -1217,12 +1284,10 @@ static rc_status check_args(const rc_plan *p, const rc_args *a, void *ws, size_t
             return fail(RC_ERR_INVALID_ARGUMENT, "the plan is of device " + std::to_string(p->device) +
                                                      ", the current device is " + std::to_string(dev));
     }
-    if (p->workspace) {
-        if (!ws || ws_bytes < p->workspace)
-            return fail(RC_ERR_INVALID_ARGUMENT, "workspace of " + std::to_string(p->workspace) + " bytes required");
-        if ((uintptr_t)ws & 255) return fail(RC_ERR_MISALIGNED, "workspace is not 256-byte aligned");
-    }
-    return RC_OK;
+    if (p->workspace && (!ws || ws_bytes < p->workspace))
+        return fail(RC_ERR_INVALID_ARGUMENT, "workspace of " + std::to_string(p->workspace) + " bytes required");
+    // (a workspace that the plan does not use is not looked at)
+    return check_buffers(p->desc, a, p->workspace ? ws : nullptr, p->workspace);
 }
 
 static rc_status launch_impl(const rc_plan *p, const rc_args *a, void *ws, size_t ws_bytes,

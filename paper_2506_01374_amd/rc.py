@@ -145,6 +145,8 @@ _SIGS = [
     ("rc_time_release", ctypes.c_int, []),
     ("rc_launch", ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(rc_args), ctypes.c_void_p,
                                  ctypes.c_size_t, ctypes.c_void_p]),
+    ("rc_check_args", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_args), ctypes.c_void_p,
+                                     ctypes.c_size_t]),
     ("rc_launch_timed", ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(rc_args), ctypes.c_void_p,
                                        ctypes.c_size_t, ctypes.c_void_p,
                                        ctypes.POINTER(ctypes.c_void_p), ctypes.c_int32]),

@@ -1,6 +1,7 @@
 """CPU tests of the 8-bit integer operators at and past the ends of their
 ranges."""
 import ctypes
+import math
 
 import pytest
 
@@ -23,3 +24,82 @@ def test_rows_past_every_limit_are_refused(kind, flags, rows):
     assert rc.lib().rc_default_schedule(op.ref, ctypes.byref(s)) == rc.RC_ERR_UNSUPPORTED
     assert rc.lib().rc_suggest_schedule(op.ref, ctypes.byref(s)) == rc.RC_ERR_UNSUPPORTED
     assert "2^32 - 1 threads" in sched.validate()
+
+
+# ---------------------------------------------------------------------------
+# Buffers that overlap
+# ---------------------------------------------------------------------------
+
+def operand_bytes(op):
+    """Bytes of each input and each output."""
+    size = {"torch.int8": 1, "torch.bfloat16": 2, "torch.float32": 4}
+    return [[size[str(dtype)] * math.prod(shape) for _, dtype, shape in side] for side in rc._i8_tensors(op)]
+
+
+def checked(op, ins, outs, ws=None, ws_bytes=0):
+    a = rc.rc_args()
+    a.struct_size = ctypes.sizeof(rc.rc_args)
+    for i, p in enumerate(ins):
+        a.in_[i] = p
+    for i, p in enumerate(outs):
+        a.out[i] = p
+    st = rc.lib().rc_check_args(op.ref, ctypes.byref(a), ws, ws_bytes)
+    return st, rc.lib().rc_last_error().decode() if st else ""
+
+
+OVERLAP_KINDS = [(rc.RC_OP_RMSNORM_I8, (5, 64), 0), (rc.RC_OP_RMSNORM_I8, (5, 64), R), (rc.RC_OP_QUANT_I8, (5, 64), 0)] + [
+    (rc.RC_OP_GEMM_I8, (4, 16, 32), f) for f in (0, B, F, B | F, G)]
+
+
+@pytest.mark.parametrize("kind,dims,flags", OVERLAP_KINDS)
+def test_what_a_launch_writes_overlaps_nothing(kind, dims, flags):
+    op = rc.Op(kind, dims, flags)
+    sizes = operand_bytes(op)
+    # all operands side by side, each at a multiple of 256 bytes, then a workspace
+    at, places = 1 << 20, []
+    for n in sizes[0] + sizes[1] + [512]:
+        places.append(at)
+        at += -(-n // 256) * 256
+    ni, no = len(sizes[0]), len(sizes[1])
+    ins, outs, ws = places[:ni], places[ni:ni + no], places[-1]
+    assert checked(op, ins, outs, ws, 512) == (rc.RC_OK, "")
+    assert checked(op, ins, outs) == (rc.RC_OK, "")
+    # inputs may share memory
+    assert checked(op, [ins[0]] * ni, outs, ws, 512) == (rc.RC_OK, "")
+    for o in range(no):
+        for i in range(ni):
+            moved = list(outs)
+            # the output's first chunk, and its last, on the input's last and first
+            for p in (ins[i], ins[i] + (sizes[0][i] - 1) // 16 * 16, ins[i] - (sizes[1][o] - 1) // 16 * 16):
+                moved[o] = p
+                st, why = checked(op, ins, moved, ws, 512)
+                allowed = kind == rc.RC_OP_RMSNORM_I8 and o == 2 and i != 1 and p == ins[i]
+                if allowed:
+                    assert st == rc.RC_OK
+                else:
+                    assert st == rc.RC_ERR_INVALID_ARGUMENT and "overlaps" in why
+            # next to it is no overlap: a lone pair of buffers far from the rest
+            far = list(ins)
+            far[i] = 1 << 30
+            moved[o] = far[i] + -(-sizes[0][i] // 16) * 16
+            assert checked(op, far, moved, ws, 512)[0] == rc.RC_OK
+        for i in range(no):
+            if i != o:
+                moved = list(outs)
+                moved[o] = outs[i]
+                assert checked(op, ins, moved, ws, 512)[0] == rc.RC_ERR_INVALID_ARGUMENT
+        assert checked(op, ins, outs, outs[o], 512)[0] == rc.RC_ERR_INVALID_ARGUMENT
+    for i in range(ni):
+        assert checked(op, ins, outs, ins[i], 512)[0] == rc.RC_ERR_INVALID_ARGUMENT
+        assert checked(op, ins, outs, ins[i] + (sizes[0][i] - 1) // 256 * 256, 512)[0] == rc.RC_ERR_INVALID_ARGUMENT
+
+
+def test_pointer_checks_need_no_device():
+    op = rc.Op(rc.RC_OP_QUANT_I8, (5, 64))
+    assert checked(op, [4096], [8192, 0])[0] == rc.RC_ERR_INVALID_ARGUMENT
+    assert checked(op, [4096 + 8], [8192, 12288])[0] == rc.RC_ERR_MISALIGNED
+    assert checked(op, [4096], [8192, 12288], 16384 + 16, 64)[0] == rc.RC_ERR_MISALIGNED
+    # the kinds whose sizes are not held against each other keep their checks
+    op = rc.Op(rc.RC_OP_GEMM_F32, (8, 8, 8))
+    assert checked(op, [4096, 4096], [4096])[0] == rc.RC_OK
+    assert checked(op, [4096, 0], [4096])[0] == rc.RC_ERR_INVALID_ARGUMENT
