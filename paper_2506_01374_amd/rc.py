@@ -517,6 +517,9 @@ def _check_tensors(tensors, device: int, inputs, output, workspace, stream):
                 raise ValueError(f"{name} is on {t.device}, the plan on cuda:{device}")
     if workspace is not None and workspace.get_device() != device:
         raise ValueError(f"the workspace is on {workspace.device}, the plan on cuda:{device}")
+    if workspace is not None and not workspace.is_contiguous():
+        # (its size is counted from its elements: an expanded tensor has fewer bytes)
+        raise ValueError("the workspace must be contiguous")
     if stream is not None and stream.device.index != device:
         raise ValueError(f"the stream is of {stream.device}, the plan on cuda:{device}")
     return inputs, output

@@ -103,3 +103,17 @@ def test_pointer_checks_need_no_device():
     op = rc.Op(rc.RC_OP_GEMM_F32, (8, 8, 8))
     assert checked(op, [4096, 4096], [4096])[0] == rc.RC_OK
     assert checked(op, [4096, 0], [4096])[0] == rc.RC_ERR_INVALID_ARGUMENT
+
+
+def test_a_workspace_of_fewer_bytes_than_elements_is_refused():
+    torch = pytest.importorskip("torch")
+    op = rc.Op(rc.RC_OP_GEMM_I8, (4, 16, 32))
+    want = rc._i8_tensors(op)
+    ins, outs = ([torch.zeros(shape, dtype=dtype) for _, dtype, shape in side] for side in want)
+    whole = torch.empty(4096, dtype=torch.uint8)
+    assert rc._check_tensors(want, -1, ins, outs, whole, None) == (ins, outs)
+    for ws in (torch.empty(1, dtype=torch.uint8).expand(4096), whole[::2]):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            rc._check_tensors(want, -1, ins, outs, ws, None)
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            rc._i8_packer(want, -1)(ins, outs, ws, None)
