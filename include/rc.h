@@ -230,9 +230,18 @@ rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out);
 /* A legal schedule for an 8-bit kind (RC_OP_RMSNORM_I8, RC_OP_QUANT_I8,
  * RC_OP_GEMM_I8) at the descriptor's sizes, by rules on sizes: for a caller
  * that has not searched, whose sizes change from call to call (the kernels of
- * these kinds take sizes as arguments, so that plans of all sizes share a few
- * code objects).  RC_ERR_UNSUPPORTED for the other kinds. */
+ * these kinds take sizes as arguments, so that plans of all sizes share the
+ * code objects that rc_suggestions lists).  RC_ERR_UNSUPPORTED for the other kinds. */
 rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out);
+
+/* All schedules that rc_suggest_schedule may return for a kind and flags,
+ * whatever the sizes, each with a descriptor of sizes at which it is legal: for
+ * compiling them ahead of time (rc_precompile), after which a plan of a
+ * suggested schedule compiles nothing.  (Of schedules with pad 1, which run
+ * the product of pad 0 after rc_pad_i8, one is listed.)  Writes up to `cap` of
+ * them and their number to *n.  RC_ERR_UNSUPPORTED for the other kinds. */
+rc_status rc_suggestions(int32_t kind, int32_t flags, rc_op_desc *descs, rc_schedule *out, int32_t cap,
+                         int32_t *n);
 
 /* Legality check, host only.  Returns RC_OK or RC_ERR_ILLEGAL_SCHEDULE with
  * the first violated rule written to `why` (may be NULL).  Tiles may end

@@ -937,6 +937,87 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
                     if (tile(tm, 16, tk, tm / 16, 1, 1, 1, sp, 0)) return;
 }
 
+typedef std::vector<std::pair<rc_op_desc, rc_schedule>> Suggestions;
+
+static void list_once(Suggestions *out, const rc_op_desc &d, const rc_schedule &s) {
+    for (auto &e : *out)
+        if (!std::memcmp(e.second.knob, s.knob, sizeof s.knob)) return;
+    out->push_back({d, s});
+}
+
+// Every schedule of suggest_gemm_i8 with a size at which it is legal; of those
+// with pad 1, whose product is the kernel of pad 0, only one.
+static void all_gemm_i8(const rc_op_desc *kind, Suggestions *out) {
+    const int nb = (kind->flags & RC_FLAG_GATED) ? 2 : 1;
+    rc_op_desc d = *kind;
+    rc_schedule s;
+    std::memset(&s, 0, sizeof s);
+    s.struct_size = sizeof s;
+    const auto &k = knobs_for(d.kind);
+    s.nknobs = (int32_t)k.size();
+    for (size_t i = 0; i < k.size(); ++i) s.knob[i] = k[i].def;
+    auto add = [&](int tm, int tn, int tk, int wm, int wn, int wk, int stages, int splits, int tail, int64_t N, int64_t K) {
+        auto set = [&](const char *name, int v) { set_knob(&d, &s, name, v); };
+        set("tile_m", tm), set("tile_n", tn), set("tile_k", tk), set("waves_m", wm), set("waves_n", wn);
+        set("waves_k", wk), set("stages", stages), set("order", 1), set("splits", splits), set("tail", tail);
+        d.dim[0] = tm, d.dim[1] = N, d.dim[2] = K;
+        if (check_schedule(&d, &s).empty()) list_once(out, d, s);
+    };
+    // streaming: (tile_m, tile_n, tile_k, waves_k) that its rules set
+    static const int STREAM[][4] = {{16, 16, 64, 1},  {16, 16, 64, 2},  {16, 16, 64, 4},  {16, 16, 128, 1},
+                                    {16, 16, 128, 2}, {16, 16, 128, 4}, {16, 16, 256, 1}, {16, 16, 256, 2},
+                                    {16, 16, 256, 4}, {16, 16, 256, 8}, {32, 16, 256, 4}, {32, 16, 256, 8},
+                                    {16, 32, 128, 8}};
+    for (auto &t : STREAM) add(t[0], t[1], t[2], 1, 1, t[3], 3, 1, 0, t[1], t[3] * t[2]);
+    for (const RingTile &t : RING_TILES) {
+        const int tn = t.tn / nb, waves = t.wm * t.wn;
+        if (tn < 16) continue;
+        // tile_k is halved where half of it covers K
+        for (int tk = t.tk; tk >= 64; tk /= 2) {
+            const int64_t ns = gemm_i8_ring_stages(t.tm, t.tn, tk, waves, 1);
+            const int64_t lds = ns * (t.tm + t.tn) * tk, slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
+            for (int sp = 1; sp <= (tk == t.tk ? 16 : 1); sp *= 2)
+                for (int tail = 0; tail <= (sp == 1); ++tail)
+                    add(t.tm, tn, tk, t.wm, t.wn, 1, 2, sp, tail, tail ? tn * (slots + 1) : tn,
+                        tk == t.tk ? sp * (ns - 1) * tk : tk);
+        }
+    }
+    for (const BufferTile &t : BUFFER_TILES)
+        for (int tk = t.tk; tk >= 64; tk /= 2)
+            for (int sp = 1; sp <= (tk == t.tk ? 16 : 1); sp *= 2)
+                add(t.tm, t.tn / nb, tk, t.wm, std::min(t.wn, t.tn / nb / 16), 1, 1, sp, 0, t.tn / nb, sp * tk);
+    for (int tm : {32, 16})
+        for (int tk : {128, 64})
+            for (int sp : {4, 2, 1}) add(tm, 16, tk, tm / 16, 1, 1, 1, sp, 0, 16, sp * tk);
+    // and the copying of rows
+    set_knob(&d, &s, "pad", 1);
+    add(64, 64 / nb, 256, 2, 2, 1, 2, 1, 0, 64 / nb, 257);
+}
+
+// The same of suggest_rows_i8, whose rules change at sizes next to powers of
+// two only: of rows, of columns and of their product.
+static void all_rows_i8(const rc_op_desc *kind, Suggestions *out) {
+    auto near = [](int64_t most, std::vector<int64_t> *v) {
+        for (int64_t p = 1; p / 2 <= most; p *= 2)
+            for (int64_t x : {p - 1, p, p + 1})
+                if (x >= 1 && x <= most && std::find(v->begin(), v->end(), x) == v->end()) v->push_back(x);
+    };
+    std::vector<int64_t> rows, cols;
+    near((1LL << 26) - 1, &rows);
+    near(1LL << 30, &cols);
+    for (int64_t T : rows)
+        for (int64_t C : cols) {
+            rc_op_desc d = *kind;
+            d.dim[0] = T, d.dim[1] = C;
+            rc_schedule s;
+            std::memset(&s, 0, sizeof s);
+            s.struct_size = sizeof s;
+            s.nknobs = (int32_t)knobs_for(d.kind).size();
+            suggest_rows_i8(&d, &s);
+            list_once(out, d, s);
+        }
+}
+
 }  // namespace rc
 
 using namespace rc;
@@ -1104,6 +1185,29 @@ rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) try {
     std::string why = check_schedule(d, &s);
     if (!why.empty()) return fail(RC_ERR_UNSUPPORTED, "no schedule to suggest: " + why);
     *out = s;
+    return RC_OK;
+} catch (const std::bad_alloc &) {
+    return RC_ERR_OUT_OF_MEMORY;
+}
+
+rc_status rc_suggestions(int32_t kind, int32_t flags, rc_op_desc *descs, rc_schedule *out, int32_t cap, int32_t *n) try {
+    if (!n || cap < 0 || (cap > 0 && (!descs || !out))) return fail(RC_ERR_INVALID_ARGUMENT, "bad arguments");
+    if (kind != RC_OP_RMSNORM_I8 && kind != RC_OP_QUANT_I8 && kind != RC_OP_GEMM_I8)
+        return fail(RC_ERR_UNSUPPORTED, "schedules of this kind are found by search, not suggested");
+    const int64_t one[] = {1, 1, 1};
+    rc_op_desc d;
+    rc_status r = rc_op_init(&d, kind, one, kind == RC_OP_GEMM_I8 ? 3 : 2, flags);
+    if (r != RC_OK) return r;
+    Suggestions all;
+    if (kind == RC_OP_GEMM_I8)
+        all_gemm_i8(&d, &all);
+    else
+        all_rows_i8(&d, &all);
+    *n = (int32_t)all.size();
+    for (int32_t i = 0; i < std::min(*n, cap); ++i) {
+        descs[i] = all[i].first;
+        out[i] = all[i].second;
+    }
     return RC_OK;
 } catch (const std::bad_alloc &) {
     return RC_ERR_OUT_OF_MEMORY;

@@ -111,6 +111,8 @@ _SIGS = [
                                       ctypes.POINTER(ctypes.c_int32)]),
     ("rc_default_schedule", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule)]),
     ("rc_suggest_schedule", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule)]),
+    ("rc_suggestions", ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(rc_op_desc),
+                                      ctypes.POINTER(rc_schedule), ctypes.c_int32, ctypes.POINTER(ctypes.c_int32)]),
     ("rc_validate", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule),
                                    ctypes.c_char_p, ctypes.c_size_t]),
     ("rc_apply", ctypes.c_int, [ctypes.POINTER(rc_op_desc), ctypes.POINTER(rc_schedule),
@@ -361,6 +363,18 @@ class Schedule:
 
     def hash(self) -> int:
         return lib().rc_schedule_hash(ctypes.byref(self.raw))
+
+
+def suggestions(kind: int, flags: int = 0) -> List[tuple]:
+    """(Op, Schedule) of every schedule that Op.suggest may return for a kind
+    and flags (the 8-bit kinds), each at sizes where it is legal."""
+    n = ctypes.c_int32()
+    _check(lib().rc_suggestions(kind, flags, None, None, 0, ctypes.byref(n)), "rc_suggestions")
+    descs, scheds = (rc_op_desc * n.value)(), (rc_schedule * n.value)()
+    _check(lib().rc_suggestions(kind, flags, descs, scheds, n, ctypes.byref(n)), "rc_suggestions")
+    nd = 3 if kind == RC_OP_GEMM_I8 else 2
+    ops = [Op(kind, list(d.dim)[:nd], flags) for d in descs]
+    return [(op, Schedule(op, s).copy()) for op, s in zip(ops, scheds)]
 
 
 def _precompile_worker(job):

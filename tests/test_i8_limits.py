@@ -2,6 +2,7 @@
 ranges."""
 import ctypes
 import math
+import random
 
 import pytest
 
@@ -117,3 +118,55 @@ def test_a_workspace_of_fewer_bytes_than_elements_is_refused():
             rc._check_tensors(want, -1, ins, outs, ws, None)
         with pytest.raises(ValueError, match="workspace must be contiguous"):
             rc._i8_packer(want, -1)(ins, outs, ws, None)
+
+
+# ---------------------------------------------------------------------------
+# The list of suggested schedules
+# ---------------------------------------------------------------------------
+
+SUGGESTING = [(rc.RC_OP_QUANT_I8, 0), (rc.RC_OP_RMSNORM_I8, 0), (rc.RC_OP_RMSNORM_I8, R)] + [
+    (rc.RC_OP_GEMM_I8, f) for f in (0, B, F, B | F, G)]
+
+
+def some_sizes(kind, seed):
+    """Sizes over the whole range, and next to powers of two."""
+    g = random.Random(seed)
+    most = (2 ** 26 - 1, 1 << 30) if kind != rc.RC_OP_GEMM_I8 else (1 << 20, 1 << 18, 131071)
+    for _ in range(4000):
+        yield tuple(max(1, int(2 ** g.uniform(0, math.log2(m)))) for m in most)
+        yield tuple(min(m, max(1, 2 ** g.randint(0, m.bit_length()) + g.choice((-1, 0, 1)))) for m in most)
+        if kind == rc.RC_OP_GEMM_I8:
+            # what is served: few to some thousand rows, and weights
+            yield tuple(max(1, int(2 ** g.uniform(0, math.log2(m)))) // s * s or s
+                        for m, s in zip((5000, 32768, 32768), (1, g.choice((1, 16)), g.choice((1, 4, 16)))))
+
+
+@pytest.mark.parametrize("kind,flags", SUGGESTING)
+def test_every_suggestion_is_listed(kind, flags):
+    listed = rc.suggestions(kind, flags)
+    texts = {str(s) for _, s in listed}
+    assert len(texts) == len(listed) <= 160
+    for op, s in listed:
+        assert op.kind == kind and op.flags == flags and s.validate() == ""
+    if kind == rc.RC_OP_GEMM_I8:
+        assert sum(s["pad"] for _, s in listed) == 1
+    sizes = list(some_sizes(kind, 11 * kind + flags))
+    if kind == rc.RC_OP_GEMM_I8:
+        sizes += [(23, 1915, 1656), (20, 4668, 1188), (70400, 64, 352)]
+    for dims in sizes:
+        if kind == rc.RC_OP_GEMM_I8 and -(-dims[0] // 16) * -(-dims[1] // 16) > 2 ** 26 - 1:
+            continue
+        text = str(rc.Op(kind, dims, flags).suggest())
+        assert text.replace("pad=1", "pad=0") in texts, dims
+
+
+def test_the_list_of_suggestions_is_of_the_8_bit_kinds():
+    for kind, flags, status in ((rc.RC_OP_GEMM_F32, 0, rc.RC_ERR_UNSUPPORTED), (99, 0, rc.RC_ERR_UNSUPPORTED),
+                                (rc.RC_OP_GEMM_I8, R, rc.RC_ERR_INVALID_ARGUMENT),
+                                (rc.RC_OP_GEMM_I8, G | B, rc.RC_ERR_INVALID_ARGUMENT)):
+        with pytest.raises(rc.RCError) as e:
+            rc.suggestions(kind, flags)
+        assert e.value.status == status
+    n = ctypes.c_int32()
+    assert rc.lib().rc_suggestions(rc.RC_OP_QUANT_I8, 0, None, None, 1, ctypes.byref(n)) == rc.RC_ERR_INVALID_ARGUMENT
+    assert rc.lib().rc_suggestions(rc.RC_OP_QUANT_I8, 0, None, None, 0, None) == rc.RC_ERR_INVALID_ARGUMENT
