@@ -872,19 +872,20 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             break;
         }
         case RC_OP_GEMM_I8: {
-            const bool gated = d->flags & RC_FLAG_GATED, bias = d->flags & RC_FLAG_BIAS;
+            const bool gated = d->flags & RC_FLAG_GATED, bias = d->flags & RC_FLAG_BIAS, f32 = d->flags & RC_FLAG_OUT_F32;
             const int tm = kv(d, s, "tile_m"), tn = kv(d, s, "tile_n"), tk = kv(d, s, "tile_k");
             const int wm = kv(d, s, "waves_m"), wn = kv(d, s, "waves_n"), wk = kv(d, s, "waves_k");
             const int st = kv(d, s, "stages"), sp = kv(d, s, "splits"), occ = kv(d, s, "occ");
             const int tnw = gated ? 2 * tn : tn;              // weight rows of a tile
             Kern k;
-            // sizes are arguments: plans of all sizes share the code object
+            // Sizes are arguments: plans of all sizes share the code object.  So
+            // do the K splits of all flags, whose sums have no epilogue yet.
             k.src = Source{SRC_gemm_i8, "rc_gemm_i8",
                            def("TM", tm) + def("TN", tnw) + def("TK", tk) + def("WM", wm) + def("WN", wn) +
                                def("WK", wk) + def("MF", kv(d, s, "mfma")) + def("STAGES", st) +
                                def("ORDER", kv(d, s, "order")) + def("OCC", occ) + def("SPLITS", sp) +
                                def("TAIL", kv(d, s, "tail")) +
-                               def("BIAS", bias) + def("F32", (d->flags & RC_FLAG_OUT_F32) != 0) + def("GATED", gated)};
+                               def("BIAS", bias && sp == 1) + def("F32", f32 && sp == 1) + def("GATED", gated)};
             if (st == 2) k.src.defines += def("NSTAGE", gemm_i8_ring_stages(tm, tnw, tk, wm * wn, occ));
             const int64_t tiles = ((D[0] + tm - 1) / tm) * ((D[1] + tn - 1) / tn);
             const int tail = kv(d, s, "tail") ? (int)gemm_i8_tail_tiles(tiles, tm, tnw, tk, wm * wn, occ) : 0;
@@ -921,7 +922,12 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             if (sp > 1) {
                 Kern kj = k;
                 kj.flops = 0;
-                kj.src.entry = "rc_gemm_i8_join";
+                // the smallest tile's object: the join does not depend on the tile
+                kj.src = Source{SRC_gemm_i8, "rc_gemm_i8_join",
+                                def("TM", 16) + def("TN", gated ? 32 : 16) + def("TK", 64) + def("WM", 1) + def("WN", 1) +
+                                    def("WK", 1) + def("MF", 16) + def("STAGES", 1) + def("ORDER", 0) + def("OCC", 1) +
+                                    def("SPLITS", sp) + def("TAIL", 0) + def("BIAS", bias) + def("F32", f32) +
+                                    def("GATED", gated)};
                 kj.grid = dim3((unsigned)((M * ((N + 3) / 4) + 255) / 256), 1, 1);
                 kj.block = dim3(256, 1, 1);
                 p.kerns.push_back(kj);

@@ -170,3 +170,18 @@ def test_the_list_of_suggestions_is_of_the_8_bit_kinds():
     n = ctypes.c_int32()
     assert rc.lib().rc_suggestions(rc.RC_OP_QUANT_I8, 0, None, None, 1, ctypes.byref(n)) == rc.RC_ERR_INVALID_ARGUMENT
     assert rc.lib().rc_suggestions(rc.RC_OP_QUANT_I8, 0, None, None, 0, None) == rc.RC_ERR_INVALID_ARGUMENT
+
+
+def test_k_splits_share_their_code_objects():
+    # the sums of the splits are those of every epilogue, and their join that
+    # of every tile
+    texts = ["tile_m=64,tile_n=64,tile_k=128,waves_m=2,waves_n=2,stages=2,splits=2", "tile_m=32,tile_n=32,tile_k=64,stages=1,splits=2"]
+    split, join = {}, {}
+    for flags in (0, B, F, B | F, G):
+        for i, text in enumerate(texts):
+            op = rc.Op(rc.RC_OP_GEMM_I8, (200, 300, 1024), flags)
+            for found, at, key in ((split, 0, (i, flags & G)), (join, 1, flags)):
+                got = rc.kernel_defines(op, op.from_string(text), at)
+                assert found.setdefault(key, got) == got
+    assert {(int(d["BIAS"]), int(d["F32"]), int(d["GATED"])) for d in join.values()} == {
+        (int(bool(f & B)), int(bool(f & F)), int(bool(f & G))) for f in (0, B, F, B | F, G)}
