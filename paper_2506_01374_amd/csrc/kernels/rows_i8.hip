@@ -22,7 +22,9 @@
 // two 8-bit significands, 127 p has at most 23 bits, and the remainder 127 p
 // - q a of a trial q is exact in fp32, so q is the correctly rounded integer
 // whatever the order in which the row was read (see nearest).  The sum of
-// squares and both statistics are fp32.
+// squares is fp32, of one vector's at a time, and where a thread has many
+// vectors their sums carry what the additions drop: its error does not grow
+// with the row.
 // A row of zeros has scale 0 and q 0.  A row that holds a NaN or an infinity,
 // or (NORM) whose squares sum past fp32, has scale NaN and q 0: what is
 // computed from it is NaN, not a silent zero.
@@ -184,14 +186,27 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     float top = 0.f;
     u16x2 tops2 = {0, 0};
     float ss = 0.f;
+#if NORM && !HELD
+    float lost = 0.f;           // what the additions to ss have dropped
+#endif
     auto take = [&](const Vec &v, const Vec &wv) {
 #if NORM
+        float s = 0.f;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             top = __builtin_elementwise_maximum(top, __builtin_fabsf(product(v, wv, j)));
             const float h = v.at(j);
-            ss = __builtin_fmaf(h, h, ss);
+            s = __builtin_fmaf(h, h, s);
         }
+#if HELD
+        ss += s;
+#else
+        // (a row of 2^24 equal values: 1e-3 off without, in one wave)
+        s -= lost;
+        const float sum = ss + s;
+        lost = (sum - ss) - s;
+        ss = sum;
+#endif
 #else
 #pragma unroll
         for (int i = 0; i < WORDS; ++i)
