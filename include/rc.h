@@ -121,9 +121,10 @@ typedef enum rc_op_kind {
      *   scale = max |y| / 127,  q = y / scale rounded to the nearest integer
      *   (halves to the even one), so that q * scale is y in 8 bits.
      * q is the exactly rounded quotient (the norm's factor cancels from it),
-     * whatever the schedule.  A row of zeros has q 0 and scale 0; a row that
-     * holds a NaN or an infinity, or whose squares sum past fp32, has q 0 and
-     * scale NaN.
+     * whatever the schedule and wherever the products h * w lie.  A row of
+     * zeros has q 0 and scale 0; a row that holds a NaN or an infinity (in h
+     * or, with it, in w), or whose squares sum or whose scale is past fp32, has
+     * q 0 and scale NaN.  (A scale below fp32's least value is 0.)
      * dim = {T, Hd}; the descriptor's eps (1e-6 from rc_op_init) is finite
      * and at least 2^-100.  in[0] = x [T][Hd] bf16; in[1] = w [Hd] bf16;
      * in[2] = r [T][Hd] bf16 (RC_FLAG_RESIDUAL).  out[0] = q [T][Hd] int8;

@@ -21,13 +21,15 @@
 // The norm's factor cancels from q, which so needs no sum: p is a product of
 // two 8-bit significands, 127 p has at most 23 bits, and the remainder 127 p
 // - q a of a trial q is exact in fp32, so q is the correctly rounded integer
-// whatever the order in which the row was read (see nearest).  The sum of
+// whatever the order in which the row was read (see nearest).  A product's
+// exponent can leave fp32: a row whose a is not between 2^-63 and 2^64 takes
+// its products, a and the remainders in 64 bits (see WIDE).  The sum of
 // squares is fp32, of one vector's at a time, and where a thread has many
 // vectors their sums carry what the additions drop: its error does not grow
 // with the row.
 // A row of zeros has scale 0 and q 0.  A row that holds a NaN or an infinity,
-// or (NORM) whose squares sum past fp32, has scale NaN and q 0: what is
-// computed from it is NaN, not a silent zero.
+// or (NORM) whose squares sum or whose scale is past fp32, has scale NaN and q
+// 0: what is computed from it is NaN, not a silent zero.
 //
 // Bound by memory with many rows: 2048 x 14336 plain, 88 MB, 16.7 us (5.3
 // TB/s); the norm with the residual, 2048 x 4096, 59 MB, 12.4 us (4.7 TB/s),
@@ -186,8 +188,16 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     float top = 0.f;
     u16x2 tops2 = {0, 0};
     float ss = 0.f;
-#if NORM && !HELD
+#if NORM
+    u32 bits = 0;               // of h whose squares did not reach fp32, without their signs
+    auto gather = [&](const Vec &v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)             // (in C it is formed ahead of the branch around it)
+            asm("v_and_or_b32 %0, %1, %2, %0" : "+v"(bits) : "v"(v.w[i]), "s"(0x7FFF7FFFu));
+    };
+#if !HELD
     float lost = 0.f;           // what the additions to ss have dropped
+#endif
 #endif
     auto take = [&](const Vec &v, const Vec &wv) {
 #if NORM
@@ -199,6 +209,7 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
             s = __builtin_fmaf(h, h, s);
         }
 #if HELD
+        if (s == 0.f) gather(v);
         ss += s;
 #else
         // (a row of 2^24 equal values: 1e-3 off without, in one wave)
@@ -227,6 +238,38 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     }
 #endif
 
+    const auto put = [&](u32 (&q)[(VEC + 3) / 4], u32 keep, int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < (VEC + 3) / 4; ++i) q[i] &= keep;
+        store(a.q + base, q, c, cols);
+    };
+    // f(h, w, c) of each of the thread's vectors, read again
+    const auto again = [&](auto &&f) __attribute__((always_inline)) {
+        for (int c = part * VEC; c < cols; c += LANES * VEC) {
+            // RES: its own store, as x or r may be gone
+#if RES
+            const bf16_t *src = ho;
+#else
+            const bf16_t *src = x;
+#endif
+            Vec h = fetch(src, c, cols), wv = {};
+            ends(h, src, c, cols);
+#if NORM
+            wv = fetch(a.w, c, cols);
+            ends(wv, a.w, c, cols);
+#endif
+            f(h, wv, c);
+        }
+    };
+
+#if NORM
+    // squares of which none reached fp32: its least value instead of 0 (next to
+    // eps nothing), so that a row's 0 is the sum of zeros alone
+#if !HELD
+    if (ss == 0.f) again([&](const Vec &v, const Vec &, int) __attribute__((always_inline)) { gather(v); });
+#endif
+    if (ss == 0.f && bits) ss = 0x1p-149f;
+#endif
 #if !NORM
     top = __builtin_bit_cast(float, (u32)(tops2[0] > tops2[1] ? tops2[0] : tops2[1]) << 16);
 #endif
@@ -255,29 +298,93 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
     }
 #endif
 
-    bool bad = !(top < __builtin_inff());
-    float scale = top;
 #if NORM
-    // (the host keeps eps at 2^-100 or more, next to which a square that
-    // leaves fp32's normal range is nothing)
-    bad |= !(ss < __builtin_inff());
-    scale /= __builtin_sqrtf(ss / (float)a.cols + a.eps);
+    // The row in 64 bits, which hold every product of two bf16: where fp32 may
+    // have lost the end of a product that counts (a below 2^-126 does), or
+    // 1 / a and y could leave it; rows with a NaN or an infinity come here too.
+    // Not rows of zeros, which padding makes many.
+#define WIDE(top, ss) (!((top) >= 0x1p-63f && (top) < 0x1p64f) && !((top) == 0.f && (ss) == 0.f))
+    const bool wide = live && WIDE(top, ss);
+    bool any = wide;                                    // of the rows that share the barrier below
+#if ROWS > 1 && WAVES > 1
+    for (int s = 0; s < ROWS; ++s) {
+        float t = tops[s][0], sum = sums[s][0];
+        for (int i = 1; i < WAVES; ++i) {
+            t = __builtin_elementwise_maximum(t, tops[s][i]);
+            sum += sums[s][i];
+        }
+        any |= (long long)blockIdx.x * ROWS + s < a.rows && WIDE(t, sum);
+    }
 #endif
-    scale /= 127.f;             // last, so that a small one is rounded once
-    if (bad) scale = __builtin_nanf("");
-    if (live && part == 0) a.scale[row_at] = scale;
-
+    if (any) {
+        double most = 0;
+        // (with held vectors instead of a second reading 8192 x 4096 would take
+        // 73 registers, not 48, and leave room for fewer waves)
+        again([&](const Vec &v, const Vec &wv, int) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const double p = __builtin_fabs((double)v.at(j) * (double)wv.at(j));
+                most = __builtin_fmax(most, p < __builtin_inf() ? p : __builtin_inf());
+            }
+        });
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) most = __builtin_fmax(most, __shfl_xor(most, d));
+#if WAVES > 1
+        __shared__ double mosts[ROWS][WAVES];
+        if (part % 64 == 0) mosts[slot][part / 64] = most;
+        __syncthreads();
+        for (int i = 0; i < WAVES; ++i) most = __builtin_fmax(most, mosts[slot][i]);
+#endif
+        if (wide) {
+            float scale = (float)(most / __builtin_sqrt((double)(ss / (float)a.cols + a.eps)) / 127.);
+            const bool bad = !(most < __builtin_inf()) || !(ss < __builtin_inff()) || !(scale < __builtin_inff());
+            if (bad) scale = __builtin_nanf("");
+            if (part == 0) a.scale[row_at] = scale;
+            if (bad || most == 0) {
+                u32 q[(VEC + 3) / 4] = {};
+                for (int c = part * VEC; c < cols; c += LANES * VEC) put(q, 0u, c);
+                return;
+            }
+            const double inv = 1 / most;
+            again([&](const Vec &v, const Vec &wv, int c) __attribute__((always_inline)) {
+                u32 o[VEC], q[(VEC + 3) / 4];
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    // as in nearest; t is next to s / a by its last bits
+                    const double s = (double)v.at(j) * (double)wv.at(j) * 127.;
+                    const double t = __builtin_rint(s * inv), rem = __builtin_fma(-t, most, s), r = __builtin_fabs(rem);
+                    const int n = (int)t;
+                    const bool move = r > 0.5 * most || (r == 0.5 * most && (n & 1));
+                    o[j] = (u32)(move ? n + (rem > 0 ? 1 : -1) : n);
+                }
+                pack(q, o);
+                put(q, ~0u, c);
+            });
+            return;
+        }
+    }
+    const bool bad = !(ss < __builtin_inff());
+    float scale = top / __builtin_sqrtf(ss / (float)a.cols + a.eps);
+    const float up = 1.f;
+#else
+    const bool bad = !(top < __builtin_inff());
+    float scale = top;
     // a is brought near 1 by a power of two, and p with it (exact), so that no
     // product below leaves fp32's range
     float up = 1.f;
     if (top < 0x1p-63f) up = 0x1p64f;
     if (top >= 0x1p64f) up = 0x1p-64f;
+#endif
+    scale /= 127.f;             // last, so that a small one is rounded once
+    if (bad) scale = __builtin_nanf("");
+    if (live && part == 0) a.scale[row_at] = scale;
+
     const float as = bad || top == 0.f ? 1.f : top * up;
     // above 1 / a by its last bits: then the trial of p = a / 2, the one tie
     // that is met often, is 64, the even neighbour of 63.5
     const float inv = __builtin_amdgcn_rcpf(as) * 0x1.000004p0f;
     const u32 keep = bad ? 0u : ~0u;
-    auto emit = [&](const Vec &v, const Vec &wv, int c) {
+    const auto emit = [&](const Vec &v, const Vec &wv, int c) __attribute__((always_inline)) {
         // trials of all elements, and again where one of them is not nearest
         u32 o[VEC], q[(VEC + 3) / 4];
         float far = 0.f;
@@ -302,9 +409,7 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
             for (int j = 0; j < VEC; ++j) o[j] = (u32)nearest(product(v, wv, j) * (127.f * up), as, inv);
             pack(q, o);
         }
-#pragma unroll
-        for (int i = 0; i < (VEC + 3) / 4; ++i) q[i] &= keep;
-        store(a.q + base, q, c, cols);
+        put(q, keep, c);
     };
 #if HELD
 #pragma unroll
@@ -313,20 +418,6 @@ extern "C" __global__ __launch_bounds__(LANES * ROWS) void rc_rows_i8(RowsI8Args
         if (c < cols) emit(v[i], wv[i], c);
     }
 #else
-    for (int c = part * VEC; c < cols; c += LANES * VEC) {
-        // RES: its own store, as x or r may be gone
-#if RES
-        const bf16_t *src = ho;
-#else
-        const bf16_t *src = x;
-#endif
-        Vec v = fetch(src, c, cols), wv = {};
-        ends(v, src, c, cols);
-#if NORM
-        wv = fetch(a.w, c, cols);
-        ends(wv, a.w, c, cols);
-#endif
-        emit(v, wv, c);
-    }
+    again(emit);
 #endif
 }

@@ -36,6 +36,85 @@ def test_overlapping_buffers_are_refused():
 
 
 # ---------------------------------------------------------------------------
+# Products of a norm past fp32's range
+# ---------------------------------------------------------------------------
+
+def wide_reference(x, w, r, eps):
+    """rows_reference, with a scale past fp32 as NaN."""
+    q, scale, h = rows_reference(x, w, r, eps)
+    past = ~(scale < 2.0 ** 128 - 2.0 ** 103)           # (rounds to an infinity)
+    scale[past] = np.nan
+    q[past] = 0
+    return q, scale, h
+
+
+def check_wide(x, w, r, text, eps, alias=None):
+    x, w, r = (None if v is None else f64(bf16(v)) for v in (x, w, r))
+    q, scale, h = wide_reference(x, w, r, eps)
+    got = run_rows(rc.RC_OP_RMSNORM_I8, 0 if r is None else R, x, w, r, text, eps, alias)
+    assert np.array_equal(got[0].cpu().numpy(), q)
+    s, ok = f64(got[1]), ~np.isnan(scale)
+    assert np.array_equal(np.isnan(s), ~ok)
+    # as test_gpu_i8's; a scale below fp32's normal range has its absolute step
+    tol = ((-(-x.shape[1] // 64) + 21) / 2 + 5) * U
+    assert np.all(np.abs(s - scale)[ok] <= tol * scale[ok] + 2.0 ** -149)
+    if r is not None:
+        assert np.array_equal(f64(got[2]), h, equal_nan=True)
+    return q, scale
+
+
+@pytest.mark.parametrize("text", cases.WIDE_TEXTS)
+@pytest.mark.parametrize("hx,wx,eps", [(58, 70, 1e-5), (-75, -70, 1e-5), (-80, -75, 2.0 ** -100), (-120, 100, 1e-5), (50, 120, 1e-5),
+                                       (30, 125, 2.0 ** -100), (-130, -130, 2.0 ** -100), (0, -63, 1e-5), (-4, 66, 1e-5),
+                                       (-60, -66, 1e-5)])
+def test_products_past_fp32(text, hx, wx, eps):
+    # rows around the exponents hx of h and wx of w, next to ordinary ones, with
+    # zeros, NaN and an infinity among them
+    g = np.random.default_rng(1000 * (hx + 200) + wx + 200)
+    t, c = 12, cases.WIDE_COLS
+    x = g.standard_normal((t, c)) * 2.0 ** hx
+    x[3] = g.standard_normal(c)
+    x[5] = 0
+    x[6, 10], x[7, 699] = np.nan, np.inf
+    x[8, ::2] *= 2.0 ** -20
+    x[9] = np.where(np.arange(c) % 3 == 0, x[9], 0)
+    w = g.standard_normal(c) * 2.0 ** wx
+    w[5], w[11] = 0, 2.0 ** wx
+    q, scale = check_wide(x, w, None, text, eps)
+    assert np.abs(q[0]).max() == 127 and np.isnan(scale[6]) and scale[5] == 0
+    r = g.standard_normal((t, c)) * 2.0 ** hx
+    check_wide(x, w, r, text, eps)
+    check_wide(x, w, r, text, eps, alias=0)
+    check_wide(x, w, r, text, eps, alias=2)
+
+
+def test_products_of_all_exponents_in_one_row():
+    # each row's products span fp32's range and more: h and w from 2^-130 to
+    # 2^60 and 2^120, the largest product anywhere
+    g = np.random.default_rng(5)
+    t, c = 40, cases.WIDE_COLS
+    x = g.standard_normal((t, c)) * 2.0 ** g.integers(-130, 60, (t, c))
+    w = g.standard_normal(c) * 2.0 ** g.integers(-130, 120, c)
+    check_wide(x, w, None, None, 1e-5)
+    # and a few next to the largest, at and next to halves of its 127th
+    x = 2.0 ** -70 * f64(bf16(np.concatenate([np.full((t, 1), 127.0), (g.integers(-127, 127, (t, c - 1)) + 0.5)], axis=1)))
+    w = np.full(c, 2.0 ** -70)
+    check_wide(x, w, None, None, 1e-5)
+    w = 2.0 ** -70 * f64(bf16(1 + g.random(c)))
+    check_wide(x, w, None, None, 1e-5)
+
+
+def test_a_scale_past_fp32():
+    # one value in 2^17 columns: y is 2^8.5 times its weight
+    c = 1 << 17
+    x, w = np.zeros((3, c)), np.ones(c)
+    x[0, 7], x[1, 8], x[2, 9] = 1.0, -3.0, 5.0
+    w[7], w[8], w[9] = 2.0 ** 127, 1.0, 2.0 ** 125
+    q, scale = check_wide(x, w, None, None, 2.0 ** -100)
+    assert np.isnan(scale[0]) and q[0, 7] == 0 and q[1, 8] == -127 and q[2, 9] == 127
+
+
+# ---------------------------------------------------------------------------
 # Long rows
 # ---------------------------------------------------------------------------
 
