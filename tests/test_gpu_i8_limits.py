@@ -6,7 +6,8 @@ import pytest
 from paper_2506_01374_amd import rc
 
 import cases_i8_limits as cases
-from test_gpu_i8 import R, U, _gpu, bf16, f64, gemm_inputs, rows_reference, run_rows  # noqa: F401
+from test_gpu_i8 import (B, BF16, F, G, R, U, _gpu, bf16, check_rows, f64, gemm_inputs, rows_inputs,  # noqa: F401
+                         rows_reference, run_gemm, run_rows)
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -134,3 +135,43 @@ def test_the_sum_of_squares_of_a_long_row(cols, text, flags):
     assert np.all(np.abs(f64(got[1]) - scale) <= ((8 + 3 + 21) / 2 + 5) * U * scale)
     if flags:
         assert np.array_equal(f64(got[2]), h)
+
+
+# ---------------------------------------------------------------------------
+# Every suggested schedule
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind,flags", [(rc.RC_OP_QUANT_I8, 0), (rc.RC_OP_RMSNORM_I8, 0), (rc.RC_OP_RMSNORM_I8, R)])
+def test_every_suggested_schedule_of_rows(kind, flags):
+    for i, ((t, c), text) in enumerate(cases.suggested_rows(kind, flags)):
+        x, w, r = rows_inputs(t, c, 500 + i)
+        norm = kind == rc.RC_OP_RMSNORM_I8
+        check_rows(kind, flags, x, w if norm else None, r if flags else None, text=text)
+
+
+@pytest.mark.parametrize("stages", [1, 2, 3])
+@pytest.mark.parametrize("flags", [0, B, F, B | F, G])
+def test_every_suggested_product(flags, stages):
+    jobs = [(d, t) for d, t in cases.suggested_products(flags) if f"stages={stages}" in t]
+    assert jobs
+    for i, (dims, text) in enumerate(jobs):
+        ins = gemm_inputs(dims, flags, 1000 * flags + i)
+        dev = [t.cuda().double() for t in ins]
+
+        # the exact sums, as in gemm_reference (64 bits hold them), and its bounds
+        def product(b, s):
+            return torch.mm(dev[0], b.t().contiguous()).mul_(dev[1][:, None]).mul_(s[None, :])
+
+        want = product(dev[2], dev[3])
+        got = run_gemm(dims, flags, ins, text).double()
+        if flags & G:
+            y, u = want, product(dev[4], dev[5])
+            want = y / (1 + torch.exp(-y)) * u
+            tol = want.abs() * (BF16 + 2 * (4 * y.abs() + 9 + 3 * (1 + y.abs()) + 3 + 1) * U) + 2.0 ** -133
+        else:
+            tol = 3 * U * want.abs()
+            if flags & B:
+                want = want + dev[4][None, :]
+                tol = tol + U * want.abs()
+            tol = tol * 1.01 + (0 if flags & F else BF16) * want.abs() + 2.0 ** -133
+        assert bool(((got - want).abs() <= tol).all()), (dims, text)
