@@ -818,13 +818,23 @@ static void suggest_rows_i8(const rc_op_desc *d, rc_schedule *s) {
 struct RingTile {
     int tm, tn, tk, wm, wn;          // tn: weight rows (twice the columns when gated)
     double start, turn, pace;
+    // Share of a round's time that a last one of half-height tiles takes: the
+    // mean of an eighth to all of the CUs busy with them, K of 1024 to 8192,
+    // plain and gated.  256 x 256 tiles are bound by their MFMAs, of which a half
+    // tile has half (rounds of 1, 1 1/4, 1 1/2 and 2 for K of 4096: 60, 86, 95
+    // and 115 us; 0.40 to 0.66 over all); in the others the weight's bytes from
+    // L2 count, which it has all of (128 x 256: 36, 57, 59 and 68; 0.55 to 0.9).
+    double half;
 };
 static const RingTile RING_TILES[] = {
-    {256, 256, 64, 2, 4, 0.0, 7.6, 11.0}, {256, 128, 128, 4, 2, 0.0, 5.2, 7.0}, {128, 256, 128, 2, 4, 0.0, 5.2, 7.0},
-    {128, 128, 128, 2, 4, 0.0, 4.9, 3.5}, {64, 128, 128, 2, 2, 0.0, 4.2, 2.35}, {128, 64, 128, 2, 2, 0.0, 4.2, 2.35},
-    {64, 64, 256, 2, 2, 0.0, 3.9, 1.45},  {64, 32, 256, 2, 2, 0.0, 3.45, 1.1},  {32, 64, 256, 2, 2, 0.0, 3.45, 1.1},
-    {32, 32, 256, 1, 2, 1.5, 1.8, 1.06},  {32, 64, 128, 1, 2, 1.0, 2.6, 1.6},   {16, 32, 256, 1, 2, 1.6, 1.75, 0.87},
-    {16, 16, 256, 1, 1, 1.6, 1.6, 0.8},   {16, 64, 128, 1, 2, 1.6, 1.75, 1.15}, {16, 32, 128, 1, 1, 1.6, 1.7, 1.1}};
+    {256, 256, 64, 2, 4, 0.0, 7.6, 11.0, 0.51}, {256, 128, 128, 4, 2, 0.0, 5.2, 7.0, 0.68},
+    {128, 256, 128, 2, 4, 0.0, 5.2, 7.0, 0.74}, {128, 128, 128, 2, 4, 0.0, 4.9, 3.5, 0.63},
+    {64, 128, 128, 2, 2, 0.0, 4.2, 2.35, 0.76}, {128, 64, 128, 2, 2, 0.0, 4.2, 2.35, 0.70},
+    {64, 64, 256, 2, 2, 0.0, 3.9, 1.45, 0.77},  {64, 32, 256, 2, 2, 0.0, 3.45, 1.1, 0.76},
+    {32, 64, 256, 2, 2, 0.0, 3.45, 1.1, 1.0},   {32, 32, 256, 1, 2, 1.5, 1.8, 1.06, 0.73},
+    {32, 64, 128, 1, 2, 1.0, 2.6, 1.6, 0.75},   {16, 32, 256, 1, 2, 1.6, 1.75, 0.87, 1.0},
+    {16, 16, 256, 1, 1, 1.6, 1.6, 0.8, 1.0},    {16, 64, 128, 1, 2, 1.6, 1.75, 1.15, 1.0},
+    {16, 32, 128, 1, 1, 1.6, 1.7, 1.1, 1.0}};   // (1: no tile of half the height)
 
 // K that is no multiple of 16: the ring on rows copied to whole chunks (pad),
 // at 3.9 us and 4.2 TB/s for the copy, or the double buffer, whose workgroups
@@ -897,14 +907,11 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
         const int64_t lds = (int64_t)gemm_i8_ring_stages(t.tm, t.tn, t.tk, waves, 1) * (t.tm + t.tn) * t.tk;
         const int64_t slots = 256 * std::max<int64_t>(1, LDS_LIMIT / lds);
         const int64_t tiles = count(M, t.tm) * count(N, t.tn / nb);
-        // a round of half-height tiles (1536 x 8192 x 8192 in 256 x 128 tiles
-        // with such a round: 134 us, in 256 x 256 tiles 108)
-        const double half = t.tm * t.tn == 256 * 128 ? 0.6 : 0.5;
         for (int sp = 1; sp <= 16; sp *= 2) {
             const double kp = (double)gemm_i8_split_k(K, t.tk, sp) / 1000.0;
             for (int tail = 0; tail <= (sp == 1); ++tail) {
                 const int64_t w = tiles * sp;
-                const double rounds = tail ? (double)(w / slots) + half : (double)count(w, slots);
+                const double rounds = tail ? (double)(w / slots) + t.half : (double)count(w, slots);
                 double us = t.start + rounds * (t.turn + kp * t.pace);
                 us = std::max(us, 2.8 + bytes / std::min(5.6e6, (double)w * 4e4)) + copy + join(sp);
                 all.push_back({us, t.tm, t.tn / nb, t.tk, t.wm, t.wn, 2, sp, tail});
