@@ -819,19 +819,19 @@ struct RingTile {
     int tm, tn, tk, wm, wn;          // tn: weight rows (twice the columns when gated)
     double start, turn, pace;
     // Share of a round's time that a last one of half-height tiles takes: the
-    // mean of an eighth to all of the CUs busy with them, K of 1024 to 8192,
+    // mean of an eighth to all of the CUs busy with them, K of 4096 and 8192,
     // plain and gated.  256 x 256 tiles are bound by their MFMAs, of which a half
     // tile has half (rounds of 1, 1 1/4, 1 1/2 and 2 for K of 4096: 60, 86, 95
     // and 115 us; 0.40 to 0.66 over all); in the others the weight's bytes from
-    // L2 count, which it has all of (128 x 256: 36, 57, 59 and 68; 0.55 to 0.9).
+    // L2 count, which it has all of (128 x 256: 36, 57, 59 and 68; 0.53 to 0.84).
     double half;
 };
 static const RingTile RING_TILES[] = {
-    {256, 256, 64, 2, 4, 0.0, 7.6, 11.0, 0.51}, {256, 128, 128, 4, 2, 0.0, 5.2, 7.0, 0.68},
-    {128, 256, 128, 2, 4, 0.0, 5.2, 7.0, 0.74}, {128, 128, 128, 2, 4, 0.0, 4.9, 3.5, 0.63},
-    {64, 128, 128, 2, 2, 0.0, 4.2, 2.35, 0.76}, {128, 64, 128, 2, 2, 0.0, 4.2, 2.35, 0.70},
-    {64, 64, 256, 2, 2, 0.0, 3.9, 1.45, 0.77},  {64, 32, 256, 2, 2, 0.0, 3.45, 1.1, 0.76},
-    {32, 64, 256, 2, 2, 0.0, 3.45, 1.1, 1.0},   {32, 32, 256, 1, 2, 1.5, 1.8, 1.06, 0.73},
+    {256, 256, 64, 2, 4, 0.0, 7.6, 11.0, 0.50}, {256, 128, 128, 4, 2, 0.0, 5.2, 7.0, 0.66},
+    {128, 256, 128, 2, 4, 0.0, 5.2, 7.0, 0.75}, {128, 128, 128, 2, 4, 0.0, 4.9, 3.5, 0.57},
+    {64, 128, 128, 2, 2, 0.0, 4.2, 2.35, 0.75}, {128, 64, 128, 2, 2, 0.0, 4.2, 2.35, 0.66},
+    {64, 64, 256, 2, 2, 0.0, 3.9, 1.45, 0.77},  {64, 32, 256, 2, 2, 0.0, 3.45, 1.1, 0.79},
+    {32, 64, 256, 2, 2, 0.0, 3.45, 1.1, 1.0},   {32, 32, 256, 1, 2, 1.5, 1.8, 1.06, 0.74},
     {32, 64, 128, 1, 2, 1.0, 2.6, 1.6, 0.75},   {16, 32, 256, 1, 2, 1.6, 1.75, 0.87, 1.0},
     {16, 16, 256, 1, 1, 1.6, 1.6, 0.8, 1.0},    {16, 64, 128, 1, 2, 1.6, 1.75, 1.15, 1.0},
     {16, 32, 128, 1, 1, 1.6, 1.7, 1.1, 1.0}};   // (1: no tile of half the height)
