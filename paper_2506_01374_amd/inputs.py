@@ -182,3 +182,31 @@ def conv_inputs(N, H, W, C, K, R, S, seed=0):
     return {"x": normal_bf16(seed, 41, (N, H, W, C)),
             "w": normal_bf16(seed, 42, (K, R, S, C), 1.0 / np.sqrt(R * S * C)),
             "bias": normal_f32(seed, 43, (K,))}
+
+
+def int_i8(seed: int, tid: int, shape, sigma: float = 32.0) -> np.ndarray:
+    """int8 values as row quantisation leaves them: a rounded normal, its ends
+    at -127 and 127."""
+    return np.clip(np.rint(normal_f32(seed, tid, shape, sigma)), -127, 127).astype(np.int8)
+
+
+def rows_i8_inputs(T, Hd, norm=False, residual=False, seed=0):
+    out = {"x": normal_bf16(seed, 51, (T, Hd))}
+    if norm:
+        out["w"] = f32_to_bf16_bits(1 + normal_f32(seed, 52, (Hd,), 0.2))
+    if residual:
+        out["r"] = normal_bf16(seed, 53, (T, Hd))
+    return out
+
+
+def gemm_i8_inputs(M, N, K, bias=False, gated=False, seed=0):
+    # the sums of K products of two rounded normals come out near one
+    scale = 1.0 / (32.0 * 32.0 * np.sqrt(K))
+    out = {"A": int_i8(seed, 61, (M, K)), "sa": uniform_f32(seed, 62, (M,), 0.5, 1.5),
+           "B": int_i8(seed, 63, (N, K)), "sb": uniform_f32(seed, 64, (N,), 0.5 * scale, 1.5 * scale)}
+    if bias:
+        out["bias"] = normal_f32(seed, 65, (N,))
+    if gated:
+        out["Bu"] = int_i8(seed, 66, (N, K))
+        out["su"] = uniform_f32(seed, 67, (N,), 0.5 * scale, 1.5 * scale)
+    return out

@@ -49,6 +49,14 @@ def reward_of(op: rc.Op, ms: float) -> float:
     return op.flops() / sec / op.peak_flops()
 
 
+def reference_schedule(name: str) -> str:
+    """A workload's tuned schedule, or an 8-bit one's suggested one."""
+    if name in W.I8_WORKLOADS:
+        return str(W.workload_op(name).suggest())
+    with open(os.path.join(HERE, "tuned.json")) as f:
+        return json.load(f)[name]
+
+
 def legal_space(op: rc.Op, limit: Optional[int] = None) -> List[rc.Schedule]:
     """Every legal schedule (cartesian product of knob values, filtered)."""
     names = op.knob_names()
@@ -412,7 +420,7 @@ def run_campaign(op: rc.Op, name: str, policies: List[str], seeds: List[int], bu
                            (f"cold: a 512 MiB buffer overwritten before each timed launch; median of "
                             if flush else "warm: back-to-back launches on the same inputs; median of ")
                            + f"{repeat} launches (one launch when it exceeds {slow_ms:g} ms)"),
-           "reward": "fraction of the binding roofline (bf16 MFMA peak or HBM bandwidth) at the median",
+           "reward": "fraction of the binding roofline (MFMA peak or HBM bandwidth) at the median",
            "reference_schedule": reference,
            "reference_reward": ref_reward, "reference_us": [ref0.get("ms", 0) * 1e3, ref1.get("ms", 0) * 1e3],
            "distinct_schedules": len(ev.order),
@@ -764,6 +772,20 @@ def schedule_features(op: rc.Op, sched: rc.Schedule) -> List[float]:
         nq = -(-S // bm)
         items = B * H * nq * (1 if ch == 0 else -(-nkt // ch))
         f += [bm / w, w * sp, chain, items / CUS, bm * bn / (64.0 * w), d["stages"] * 1.0]
+    elif op.kind == rc.RC_OP_GEMM_I8:
+        M, N, K = D
+        nb = 2 if op.flags & rc.RC_FLAG_GATED else 1
+        tm, tn, tk = d["tile_m"], nb * d["tile_n"], d["tile_k"]
+        waves = d["waves_m"] * d["waves_n"] * d["waves_k"]
+        acc = tm * tn / (64.0 * d["waves_m"] * d["waves_n"])
+        n_wg = -(-M // tm) * -(-N // d["tile_n"]) * d["splits"]
+        rounds = n_wg / CUS
+        f += [waves, acc, (tm + tn) * tk / 1024.0, rounds, rounds / -(-n_wg // CUS), (tm + tn) / (tm * tn),
+              K / d["splits"] / (tk * d["waves_k"])]
+    elif op.kind in (rc.RC_OP_RMSNORM_I8, rc.RC_OP_QUANT_I8):
+        T, C = D
+        step = 64 * d["waves"] * d["vec"]
+        f += [step, -(-C // step), -(-C // step) * step / C, -(-T // d["rows"]) / CUS, d["held"] * d["vec"]]
     return f
 
 
@@ -931,7 +953,7 @@ def _parse_seeds(text: str) -> List[int]:
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("--workload", required=True, choices=list(W.WORKLOADS))
+    ap.add_argument("--workload", required=True, choices=list(W.WORKLOADS) + list(W.I8_WORKLOADS))
     ap.add_argument("--policy", default="uct", choices=list(POLICIES) + ["list"])
     ap.add_argument("--budget", type=int, default=64)
     ap.add_argument("--seeds", default="0")
@@ -994,8 +1016,7 @@ def main(argv=None):
         return
 
     if args.p0:
-        tuned = json.load(open(os.path.join(HERE, "tuned.json")))
-        rec = time_p0_and_tuned(op, args.workload, tuned[args.workload], repeat=args.repeat)
+        rec = time_p0_and_tuned(op, args.workload, reference_schedule(args.workload), repeat=args.repeat)
         with open(os.path.join(args.out, f"{args.workload}.p0.json"), "w") as f:
             json.dump(rec, f, indent=1)
         print(json.dumps({k: rec[k] for k in ("workload", "p0_us", "tuned_us", "tuned_speedup_over_p0")}),
@@ -1003,12 +1024,11 @@ def main(argv=None):
         return
 
     if args.campaign:
-        tuned = json.load(open(os.path.join(HERE, "tuned.json")))
         pols = [p for p in args.campaign.split(",") if p]
         path = os.path.join(args.out, f"{args.workload}.campaign.json")
         log = open(os.path.join(args.out, f"{args.workload}.campaign.jsonl"), "a")
         rec = run_campaign(op, args.workload, pols, _parse_seeds(args.seeds), args.budget,
-                           tuned[args.workload], args.jobs, path, args.cache_dir, repeat=args.repeat,
+                           reference_schedule(args.workload), args.jobs, path, args.cache_dir, repeat=args.repeat,
                            slow_ms=args.slow_ms, log=log, horizon=args.horizon, flush=not args.warm,
                            rotate=args.bench_timing)
         print(json.dumps({k: rec[k] for k in ("workload", "reference_reward", "distinct_schedules",

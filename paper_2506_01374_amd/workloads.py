@@ -33,12 +33,24 @@ WORKLOADS: Dict[str, Tuple[int, Tuple[int, ...], int]] = {
 }
 
 
+# The dense layers in 8-bit integers (Llama-3-8B-style sizes: a prefill of 2048
+# tokens and a decode batch of 16).  Their suggested schedules stand where the
+# others have a tuned one.
+I8_WORKLOADS: Dict[str, Tuple[int, Tuple[int, ...], int]] = {
+    "rmsnorm_i8_t2048_h4096_res": (rc.RC_OP_RMSNORM_I8, (2048, 4096), rc.RC_FLAG_RESIDUAL),
+    "quant_i8_t2048_h14336": (rc.RC_OP_QUANT_I8, (2048, 14336), 0),
+    "gemm_i8_m2048_n4096_k14336": (rc.RC_OP_GEMM_I8, (2048, 4096, 14336), 0),
+    "gemm_i8_m16_n4096_k4096": (rc.RC_OP_GEMM_I8, (16, 4096, 4096), 0),
+    "gated_i8_m2048_n14336_k4096": (rc.RC_OP_GEMM_I8, (2048, 14336, 4096), rc.RC_FLAG_GATED),
+}
+
+
 def op_for(kind: int, dims, flags: int = 0) -> rc.Op:
     return rc.Op(kind, dims, flags)
 
 
 def workload_op(name: str) -> rc.Op:
-    kind, dims, flags = WORKLOADS[name]
+    kind, dims, flags = WORKLOADS[name] if name in WORKLOADS else I8_WORKLOADS[name]
     return rc.Op(kind, dims, flags)
 
 
@@ -56,7 +68,22 @@ def host_inputs(op: rc.Op, seed: int = 0) -> Dict[str, np.ndarray]:
     if op.kind == rc.RC_OP_CONV2D:
         N, H, W, C, K, R, S, _ = d
         return gen.conv_inputs(N, H, W, C, K, R, S, seed)
+    if op.kind in (rc.RC_OP_RMSNORM_I8, rc.RC_OP_QUANT_I8):
+        return gen.rows_i8_inputs(*d, norm=op.kind == rc.RC_OP_RMSNORM_I8, residual=bool(op.flags & rc.RC_FLAG_RESIDUAL),
+                                  seed=seed)
+    if op.kind == rc.RC_OP_GEMM_I8:
+        return gen.gemm_i8_inputs(*d, bias=bool(op.flags & rc.RC_FLAG_BIAS), gated=bool(op.flags & rc.RC_FLAG_GATED),
+                                  seed=seed)
     raise ValueError(op.kind)
+
+
+def output_shapes(op: rc.Op) -> List[Tuple[Tuple[int, ...], str]]:
+    """Shape and type of each output."""
+    d = op.dims
+    if op.kind in (rc.RC_OP_RMSNORM_I8, rc.RC_OP_QUANT_I8):
+        outs = [(tuple(d), "int8"), ((d[0],), "float32")]
+        return outs + [(tuple(d), "bfloat16")] if op.flags & rc.RC_FLAG_RESIDUAL else outs
+    return [output_shape(op)]
 
 
 def output_shape(op: rc.Op) -> Tuple[Tuple[int, ...], str]:
@@ -69,6 +96,10 @@ def output_shape(op: rc.Op) -> Tuple[Tuple[int, ...], str]:
         return (d[0], d[1]), "bfloat16"
     if op.kind == rc.RC_OP_MOE:
         return (d[0], d[1]), "bfloat16"
+    if op.kind == rc.RC_OP_GEMM_I8:
+        return (d[0], d[1]), "float32" if op.flags & rc.RC_FLAG_OUT_F32 else "bfloat16"
+    if op.kind != rc.RC_OP_CONV2D:
+        raise ValueError("an operator of several outputs: see output_shapes")
     N, H, W, C, K, R, S, pad = d
     return (N, H + 2 * pad - R + 1, W + 2 * pad - S + 1, K), "bfloat16"
 
@@ -96,6 +127,10 @@ def stored_inputs(op: rc.Op, sched: rc.Schedule, host: Dict[str, np.ndarray]) ->
         if k["layout"] == 0:
             w = np.ascontiguousarray(np.transpose(w, (1, 2, 3, 0)))   # [R][S][C][K]
         return [host["x"], w, host["bias"]]
+    if op.kind in (rc.RC_OP_RMSNORM_I8, rc.RC_OP_QUANT_I8):
+        return [host[n] for n in ("x", "w", "r") if n in host]
+    if op.kind == rc.RC_OP_GEMM_I8:
+        return [host[n] for n in ("A", "sa", "B", "sb", "bias", "Bu", "su") if n in host]
     raise ValueError(op.kind)
 
 
@@ -111,17 +146,23 @@ def to_device(arrs: List[np.ndarray], device="cuda"):
 
 
 def empty_output(op: rc.Op, device="cuda", fill_nan=True):
+    """The output, or a tuple of an operator's several outputs (integers are
+    filled with -128, which no quantised row holds)."""
     import torch
-    shape, dt = output_shape(op)
-    dtype = torch.float32 if dt == "float32" else torch.bfloat16
-    t = torch.empty(shape, dtype=dtype, device=device)
-    if fill_nan:
-        t.fill_(float("nan"))
-    return t
+    outs = []
+    for shape, dt in output_shapes(op):
+        t = torch.empty(shape, dtype=getattr(torch, dt), device=device)
+        if fill_nan:
+            t.fill_(-128 if dt == "int8" else float("nan"))
+        outs.append(t)
+    return outs[0] if len(outs) == 1 else tuple(outs)
 
 
-def output_to_f64(op: rc.Op, t) -> np.ndarray:
+def output_to_f64(op: rc.Op, t):
+    """The output as a float64 array, or the arrays of several outputs."""
     import torch
+    if isinstance(t, (tuple, list)):
+        return [output_to_f64(op, x) for x in t]
     a = t.detach().cpu()
     if a.dtype == torch.bfloat16:
         return gen.bf16_bits_to_f32(a.view(torch.int16).numpy().view(np.uint16)).astype(np.float64)
