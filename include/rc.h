@@ -141,7 +141,9 @@ typedef enum rc_op_kind {
     /* Matrix product in 8-bit integers with a scale for each row of A (token)
      * and of the weight (channel), int32 sums, which are exact:
      *   out[m][n] = (sum_k A[m][k] B[n][k]) * sa[m] * sb[n] (+ bias[n]),
-     * in bf16, or in fp32 with RC_FLAG_OUT_F32; bias with RC_FLAG_BIAS.
+     * in bf16, or in fp32 with RC_FLAG_OUT_F32; bias with RC_FLAG_BIAS.  The
+     * products are formed in fp32 from left to right: acc * sa[m] is to stay
+     * below fp32's largest value (any scale below 2^97 keeps it there).
      * With RC_FLAG_GATED (alone) two weights share A, and
      *   out = bf16(SiLU(g) * u),  g and u the two products.
      * dim = {M, N, K}, K at most 131071 (the sums of 128 * 128 stay in 32

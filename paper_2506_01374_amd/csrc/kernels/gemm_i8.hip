@@ -1,6 +1,8 @@
 // int8 x int8 -> int32 MFMA matrix product for gfx950 with a fused epilogue:
 //   acc[m][n] = sum_k A[m][k] B[n][k]              (int32, exact)
-//   out[m][n] = acc * (sa[m] * sb[n]) (+ bias[n])  (fp32, rounded once)
+//   out[m][n] = acc * sa[m] * sb[n] (+ bias[n])    (fp32, then the output's type)
+// (the sum is converted, multiplied by sa and then by sb, each rounded in fp32:
+// sa * sb first would leave fp32's range where the output does not)
 // and the gated form, two products of one A:
 //   out[m][n] = bf16(SiLU(g) * u).
 // Both operands have K contiguous, the layout the matrix instructions take:
@@ -201,9 +203,9 @@ __device__ __forceinline__ void finish(const GemmI8Args &a, long long m, int n, 
 #endif
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        float y = (float)g[r] * (sa * c.s[r]);
+        float y = (float)g[r] * sa * c.s[r];
 #if GATED
-        y = silu(y) * ((float)u[r] * (sa * c.u[r]));
+        y = silu(y) * ((float)u[r] * sa * c.u[r]);
 #endif
 #if BIAS
         y += c.b[r];

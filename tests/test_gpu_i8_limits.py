@@ -6,8 +6,8 @@ import pytest
 from paper_2506_01374_amd import rc
 
 import cases_i8_limits as cases
-from test_gpu_i8 import (B, BF16, F, G, R, U, _gpu, bf16, check_rows, f64, gemm_inputs, rows_inputs,  # noqa: F401
-                         rows_reference, run_gemm, run_rows)
+from test_gpu_i8 import (B, BF16, F, G, R, U, _gpu, bf16, check_rows, f64, gemm_inputs, gemm_reference,  # noqa: F401
+                         rows_inputs, rows_reference, run_gemm, run_rows)
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -175,3 +175,33 @@ def test_every_suggested_product(flags, stages):
                 tol = tol + U * want.abs()
             tol = tol * 1.01 + (0 if flags & F else BF16) * want.abs() + 2.0 ** -133
         assert bool(((got - want).abs() <= tol).all()), (dims, text)
+
+
+# ---------------------------------------------------------------------------
+# Scales whose product leaves fp32's range
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("text", ["tile_m=16,tile_n=16,tile_k=64,stages=1", "tile_m=32,tile_n=32,tile_k=128,stages=2",
+                                  "tile_m=16,tile_n=16,tile_k=64,stages=3,waves_k=2", "tile_m=32,tile_n=32,tile_k=64,stages=1,splits=2"])
+@pytest.mark.parametrize("flags", [F, G])
+def test_scales_whose_product_leaves_fp32(flags, text):
+    dims = (40, 70, 512)
+    ins = gemm_inputs(dims, flags, 17)
+    ins[0][5], ins[0][6] = 0, 0                                     # sums of 0
+    low = ins[1] * 2.0 ** -70
+    high = ins[1] * 2.0 ** 90
+    for sa, sb, whole in ((low, 2.0 ** -55, 0), (high, 2.0 ** 60, 1), (high, 2.0 ** -100, 0)):
+        if flags & G:
+            sets = [ins[0], sa, ins[2], ins[3] * sb, ins[4], ins[5] * sb]
+        else:
+            sets = [ins[0], sa, ins[2], ins[3] * sb]
+        got = f64(run_gemm(dims, flags, sets, text))
+        want, tol = gemm_reference(sets, flags)
+        if whole:
+            # past fp32 but for the rows of zeros (gated: 0 times anything finite)
+            assert np.all(got[5:7] == 0) and not np.isfinite(got[0]).all()
+            continue
+        # (below the types' normal range a step is absolute)
+        least = 2.0 ** -149 if flags & F else 2.0 ** -133
+        assert np.all(np.abs(got - want) <= tol + least), np.max(np.abs(got - want) - tol)
+        assert np.abs(want).max() > 2.0 ** -126 or flags & G       # (a normal number)
