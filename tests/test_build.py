@@ -52,3 +52,15 @@ def test_build_compiles_what_the_package_launches():
     op = rc.Op(rc.RC_OP_GEMM_I8, (20, 4668, 1188), rc.RC_FLAG_BIAS | rc.RC_FLAG_OUT_F32)
     assert str(op.suggest()).replace("pad=1", "pad=0") in {text for kind, _, flags, text in jobs
                                                           if (kind, flags) == (op.kind, op.flags)}
+
+
+def test_compilation_says_how_far_it_is_and_what_failed(tmp_path, capfd):
+    import __graft_entry__ as g
+    import pytest
+    op = rc.Op(rc.RC_OP_QUANT_I8, (3, 100))
+    good, bad = [op.schedule(vec=2), op.default()], op.schedule(waves=16, rows=8)
+    g.compile_kernels([(op, good + good)], [(op, [bad])], str(tmp_path))
+    assert "build: kernels of 3 of 3 schedules" in capfd.readouterr().out
+    assert sum(f.endswith(".hsaco") for f in os.listdir(tmp_path)) == 2
+    with pytest.raises(RuntimeError, match="failed for 1 schedules"):
+        g.compile_kernels([(op, [bad])], [], str(tmp_path))
