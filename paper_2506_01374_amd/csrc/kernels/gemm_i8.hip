@@ -152,7 +152,9 @@ __device__ __forceinline__ i32x4 bytes16(const i8 *p, int left) {
 
 __device__ __forceinline__ float silu(float x) {
     // x * sigmoid(x); exp(-x) as 2^(-x log2 e) and the reciprocal on the
-    // hardware's units, one step of fp32 off each
+    // hardware's units, one step of fp32 off each, which a rounding to bf16
+    // follows.  The reciprocal's results end at 2^-126: below x = -87.3, where
+    // the value is under 10^-36, this is 0.
     return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * 1.4426950408889634f));
 }
 

@@ -32,9 +32,10 @@
 // 0: what is computed from it is NaN, not a silent zero.
 //
 // Bound by memory with many rows: 2048 x 14336 plain, 88 MB, 16.7 us (5.3
-// TB/s); the norm with the residual, 2048 x 4096, 59 MB, 12.4 us (4.7 TB/s),
-// 8192 x 4096 43.3 us (5.4).  A row stays in registers between the passes:
-// reading it again takes 18.8 us in the first of these.
+// TB/s); the norm with the residual, 2048 x 4096, 59 MB, 12.6 us (4.7 TB/s),
+// 8192 x 4096 43.4 us (5.4).  A row stays in registers between the passes:
+// reading it again takes 18.8 us in the first of these.  Rows in 64 bits are
+// read twice more: 2048 x 4096 of them, with the residual, take 21.3 us for 12.6.
 // Bound by the way to memory and back with few rows: one row of 4096 takes 3.0
 // us, of which an empty kernel takes 2.2, so that its waves are many and their
 // loads all under way at once.
