@@ -10,7 +10,9 @@
  *     (attention, MoE, convolution, gated MLP) plus the fp32 contraction of
  *     the App. A example module; or one of the operators of the dense layers
  *     in 8-bit integers (the matrix product with its scales, and the
- *     quantisation of its rows, with or without a norm in front);
+ *     quantisation of its rows, with or without a norm in front); or one of
+ *     the operators of attention in serving (a paged cache of keys and values,
+ *     attention over it, and attention over prompts packed behind each other);
  *   - a program variant is a schedule (rc_schedule): one integer per knob;
  *   - a transformation (rc_transform) sets one knob, named after the
  *     transformation classes of App. A (TileSize, Parallel,
@@ -155,15 +157,71 @@ typedef enum rc_op_kind {
      * are the gate's).  out[0] = [M][N].  No size need be a multiple of
      * anything.  Weights are stored [N][K] only: 16 consecutive k are what a
      * lane of the matrix cores takes. */
-    RC_OP_GEMM_I8 = 8
+    RC_OP_GEMM_I8 = 8,
+    /* Attention in serving: sequences of different lengths, which the
+     * descriptor does not hold.  B sequences; sequence b owns the packed rows
+     * offsets[b] .. offsets[b + 1] - 1 (offsets [B + 1] int32, not decreasing;
+     * a sequence may have none), its newest tokens, and has lens[b] tokens (lens
+     * [B] int32), these among them and last.  The cache holds K and V
+     * [pages][Hkv][page][D] each: position p of sequence b is slot p % page of
+     * page table[b][p / page] (table [B][width] int32).  It holds bf16, or with
+     * RC_FLAG_I8_CACHE int8 and for each token and head an fp32 scale, Ks and
+     * Vs [pages][Hkv][page].
+     * Offsets, lengths and the table are read on the device, so that a captured
+     * launch serves the lengths it then finds.  Whatever they hold, no access
+     * leaves its buffer: a position has no page where p / page >= width or the
+     * table's entry is not one of 0 .. pages - 1 (-1 marks a page that is not
+     * held).  Rows of out[] that are no sequence's are left as they were.
+     * D is 64, 128 or 256; page 16, 32, 64, 128 or 256; width * page at most
+     * 2^30, pages * Hkv * page at most 2^40, T * H and T * Hkv at most 2^30,
+     * Hkv * D at most 2^20, and B at most 2^24.
+     *
+     * New tokens' K and V into the cache:
+     *   bf16: as they are;
+     *   int8: scale = max |x| / 127 over a token's head, q = x / scale rounded
+     *   as in RC_OP_QUANT_I8 (zeros, NaN and infinities as there).
+     * dim = {T, B, Hkv, D, page, pages, width}.  in[0] = k, in[1] = v
+     * [T][Hkv][D] bf16; in[2] = offsets; in[3] = lens; in[4] = table.  out[0] =
+     * K, out[1] = V, out[2] = Ks and out[3] = Vs (RC_FLAG_I8_CACHE), of which
+     * the new tokens' slots are written and no other.  A token without a page is
+     * not written.  Two tokens of a launch must not have the same slot. */
+    RC_OP_KV_WRITE = 9,
+    /* Rows of the cache back into packed rows: bf16(q * scale), or as they are.
+     * dim = {T, B, Hkv, D, page, pages, width}.  in[0] = K, in[1] = V, in[2] =
+     * Ks and in[3] = Vs (RC_FLAG_I8_CACHE), then offsets, lens and table;
+     * out[0] = k, out[1] = v [T][Hkv][D] bf16: the newest tokens of each
+     * sequence, all of them where its rows are as many.  A token without a
+     * page is 0. */
+    RC_OP_KV_READ = 10,
+    /* Attention of new tokens (one, some, many: another number a sequence)
+     * over the cache, scale 1 / sqrt(D), fp32 scores and softmax:
+     *   O[row][h] = sum_j p_j V_j / sum_j p_j,  p_j = exp(q . K_j / sqrt(D) - max)
+     * over the positions j < lens[b], with RC_FLAG_CAUSAL up to the row's own,
+     * lens[b] - rows of b + row - offsets[b].  Query head h reads K/V head h /
+     * (H / Hkv).  Keys without a page are not seen.  A row that sees no key, or
+     * whose scores all are -infinity, is 0; what a row does not see does not
+     * count, a NaN there neither.  Probabilities are rounded to bf16 for the
+     * second product, int8 values with their scale multiplied in.
+     * dim = {T, B, H, Hkv, D, page, pages, width}, H a multiple of Hkv.  in[0] =
+     * Q [T][H][D] bf16; in[1] = K, in[2] = V, in[3] = Ks and in[4] = Vs
+     * (RC_FLAG_I8_CACHE), then offsets, lens and table; out[0] = O [T][H][D]. */
+    RC_OP_ATTENTION_PAGED = 11,
+    /* The same over K and V rows that are packed behind each other as the
+     * queries are: sequence b has the rows koffsets[b] .. koffsets[b + 1] - 1 of
+     * K and V, its queries are the last of them.
+     * dim = {T, TK, B, H, Hkv, D}.  in[0] = Q [T][H][D]; in[1] = K, in[2] = V
+     * [TK][Hkv][D]; in[3] = offsets; in[4] = koffsets [B + 1] (for whole prompts
+     * the same buffer); out[0] = O [T][H][D].  TK * Hkv at most 2^30. */
+    RC_OP_ATTENTION_PACKED = 12
 } rc_op_kind;
 
-#define RC_FLAG_CAUSAL 1   /* RC_OP_ATTENTION only */
+#define RC_FLAG_CAUSAL 1   /* the attention kinds only */
 #define RC_FLAG_NO_ACT 2   /* RC_OP_CONV2D only: bias, no SiLU */
 #define RC_FLAG_RESIDUAL 4 /* RC_OP_RMSNORM_I8 only: h = bf16(x + r), stored */
 #define RC_FLAG_BIAS 8     /* RC_OP_GEMM_I8 only: + bias[n] */
 #define RC_FLAG_OUT_F32 16 /* RC_OP_GEMM_I8 only: fp32 output */
 #define RC_FLAG_GATED 32   /* RC_OP_GEMM_I8 only: SiLU(g) * u, two weights */
+#define RC_FLAG_I8_CACHE 64 /* the kinds with a paged cache only: int8 and scales */
 #define RC_MAX_DIMS 8
 
 typedef struct rc_op_desc {
@@ -177,8 +235,8 @@ typedef struct rc_op_desc {
 /* Fill *d for `kind` with `ndims` dimensions.  Checks the kind, the number
  * of dimensions, that every dimension is positive (pad may be 0) and that
  * `flags` holds only flags defined for the kind; RC_ERR_INVALID_ARGUMENT
- * otherwise.  Sizes past the limits stated for the 8-bit kinds are
- * RC_ERR_UNSUPPORTED. */
+ * otherwise.  Sizes past the limits stated for the 8-bit kinds and those of
+ * attention in serving are RC_ERR_UNSUPPORTED. */
 rc_status rc_op_init(rc_op_desc *d, int32_t kind, const int64_t *dims, int32_t ndims,
                      int32_t flags);
 
@@ -186,7 +244,10 @@ rc_status rc_op_init(rc_op_desc *d, int32_t kind, const int64_t *dims, int32_t n
  * FLOPs count 2 per multiply-add of the contraction only (for causal
  * attention only visible query/key pairs; for MoE only routed rows);
  * bytes count compulsory HBM traffic: each input read once and each output
- * written once.  Negative on an invalid descriptor. */
+ * written once.  Negative on an invalid descriptor.
+ * (The attention kinds in serving, whose lengths are on the device, are counted
+ * for B sequences that share the rows evenly and fill their part of the table,
+ * or of K's rows.) */
 double rc_op_flops(const rc_op_desc *d);
 double rc_op_bytes(const rc_op_desc *d);
 /* Published MI355X peak that bounds the operator: fp32 MFMA (157.3 TFLOP/s)
@@ -231,7 +292,9 @@ rc_status rc_knob_values(const rc_op_desc *d, int32_t knob, int32_t *vals, int32
 rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out);
 
 /* A legal schedule for an 8-bit kind (RC_OP_RMSNORM_I8, RC_OP_QUANT_I8,
- * RC_OP_GEMM_I8) at the descriptor's sizes, by rules on sizes: for a caller
+ * RC_OP_GEMM_I8) or one of attention in serving (RC_OP_KV_WRITE, RC_OP_KV_READ,
+ * RC_OP_ATTENTION_PAGED, RC_OP_ATTENTION_PACKED) at the descriptor's sizes, by
+ * rules on sizes: for a caller
  * that has not searched, whose sizes change from call to call (the kernels of
  * these kinds take sizes as arguments, so that plans of all sizes share the
  * code objects that rc_suggestions lists).  RC_ERR_UNSUPPORTED for the other kinds. */
@@ -338,7 +401,9 @@ rc_status rc_plan_kernel_flops(const rc_plan *p, int32_t kernel, double *flops);
  *   stage with splits > 1: "splitk.partials"; RC_OP_GEMM_I8 with splits > 1:
  *   "splitk.partials" int32 [splits][M][1, or 2 gated][N rounded up to 4], and
  *   with pad 1 "padded.rows" int8 [M + N, or M + 2 N gated][K rounded up to
- *   16] (A, then the weights).
+ *   16] (A, then the weights);
+ *   RC_OP_ATTENTION_PAGED and RC_OP_ATTENTION_PACKED with splits > 0:
+ *   "partials" fp32, the states of a block's pieces.
  * RC_ERR_INVALID_ARGUMENT if the plan has no part of that name.  (The
  * routing preparation of the MoE layer of Sec. 4.1 is integer index work:
  * these parts let it be checked exactly.) */
@@ -383,7 +448,8 @@ typedef struct rc_args {
 
 /* Enqueue one execution of the operator on `stream`.  Checks pointers
  * (non-NULL, 16-byte aligned) and the workspace size; never synchronises.
- * The plan of an 8-bit kind is launched with the device current that it was
+ * The plan of an 8-bit kind or one of attention in serving is launched with the
+ * device current that it was
  * created on, and what it writes (outputs, workspace) overlaps none of its
  * other buffers but for RC_OP_RMSNORM_I8's h, as stated there
  * (RC_ERR_INVALID_ARGUMENT otherwise). */
@@ -391,7 +457,7 @@ rc_status rc_launch(const rc_plan *p, const rc_args *a, void *workspace, size_t 
                     void *stream);
 
 /* rc_launch's checks of the pointers, host only: NULL, alignment and, for the
- * 8-bit kinds, overlap, with a workspace of `ws_bytes` bytes in use (NULL and 0
+ * 8-bit kinds and those of attention in serving, overlap, with a workspace of `ws_bytes` bytes in use (NULL and 0
  * for none). */
 rc_status rc_check_args(const rc_op_desc *d, const rc_args *a, const void *workspace, size_t ws_bytes);
 

@@ -153,6 +153,23 @@ static std::vector<KnobDef> gemm_i8_knobs() {
     };
 }
 
+static std::vector<KnobDef> kv_cache_knobs() {
+    return {
+        {"waves", "Parallel", {1, 2, 4, 8}, 1},               // waves of a workgroup, a token each
+        {"vec", "Vectorize", {4, 8}, 4},                      // bf16 per global load
+    };
+}
+
+static std::vector<KnobDef> attention_seqs_knobs() {
+    return {
+        {"block_m", "TileSize", {16, 32, 64, 128}, 16},       // rows (tokens x heads of a K/V head) of an item
+        {"waves", "Parallel", {1, 2, 4, 8}, 1},               // waves of a workgroup
+        {"stages", "ComputeLocation", {1, 2}, 1},             // a tile after the other / the next one's loads under way
+        // workgroups a CU for which the keys are cut into pieces (0: they are not)
+        {"splits", "Parallel", {0, 1, 2, 4}, 0},
+    };
+}
+
 const std::vector<KnobDef> &knobs_for(int32_t kind) {
     static const std::vector<KnobDef> empty;
     static const std::vector<KnobDef> g = gemm_f32_knobs();
@@ -162,6 +179,8 @@ const std::vector<KnobDef> &knobs_for(int32_t kind) {
     static const std::vector<KnobDef> c = conv_knobs();
     static const std::vector<KnobDef> ri = rows_i8_knobs();
     static const std::vector<KnobDef> gi = gemm_i8_knobs();
+    static const std::vector<KnobDef> kc = kv_cache_knobs();
+    static const std::vector<KnobDef> as = attention_seqs_knobs();
     switch (kind) {
         case RC_OP_GEMM_F32: return g;
         case RC_OP_ATTENTION: return a;
@@ -171,6 +190,10 @@ const std::vector<KnobDef> &knobs_for(int32_t kind) {
         case RC_OP_RMSNORM_I8:
         case RC_OP_QUANT_I8: return ri;
         case RC_OP_GEMM_I8: return gi;
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return kc;
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: return as;
         default: return empty;
     }
 }
@@ -182,7 +205,7 @@ int knob_index(int32_t kind, const char *name) {
     return -1;
 }
 
-static int expected_dims(int32_t kind) {
+int expected_dims(int32_t kind) {
     switch (kind) {
         case RC_OP_GEMM_F32: return 3;
         case RC_OP_ATTENTION: return 4;
@@ -192,6 +215,10 @@ static int expected_dims(int32_t kind) {
         case RC_OP_RMSNORM_I8:
         case RC_OP_QUANT_I8: return 2;
         case RC_OP_GEMM_I8: return 3;
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return 7;
+        case RC_OP_ATTENTION_PAGED: return 8;
+        case RC_OP_ATTENTION_PACKED: return 6;
         default: return -1;
     }
 }
@@ -413,17 +440,55 @@ static int32_t allowed_flags(int32_t kind) {
         case RC_OP_CONV2D: return RC_FLAG_NO_ACT;
         case RC_OP_RMSNORM_I8: return RC_FLAG_RESIDUAL;
         case RC_OP_GEMM_I8: return RC_FLAG_BIAS | RC_FLAG_OUT_F32 | RC_FLAG_GATED;
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return RC_FLAG_I8_CACHE;
+        case RC_OP_ATTENTION_PAGED: return RC_FLAG_CAUSAL | RC_FLAG_I8_CACHE;
+        case RC_OP_ATTENTION_PACKED: return RC_FLAG_CAUSAL;
         default: return 0;
     }
 }
 
-// What a descriptor of an 8-bit kind must keep to beyond positive
+SeqDims seq_dims(const rc_op_desc *d) {
+    const int64_t *D = d->dim;
+    switch (d->kind) {
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return {D[0], 0, D[1], D[2], D[2], D[3], D[4], D[5], D[6]};
+        case RC_OP_ATTENTION_PAGED: return {D[0], 0, D[1], D[2], D[3], D[4], D[5], D[6], D[7]};
+        default: return {D[0], D[1], D[2], D[3], D[4], D[5], 0, 0, 0};
+    }
+}
+
+// The limits of attention in serving, which keep every index of a row, key or
+// page in 32 bits and every offset in 64.
+static std::string check_seqs_desc(const rc_op_desc *d, bool *size) {
+    const SeqDims s = seq_dims(d);
+    if (s.H % s.Hkv) return fmt("H = %lld is not a multiple of Hkv = %lld", (long long)s.H, (long long)s.Hkv);
+    *size = true;
+    const int64_t most = 1LL << 30;
+    if (s.D != 64 && s.D != 128 && s.D != 256) return fmt("D = %lld: head dimensions are 64, 128 and 256", (long long)s.D);
+    if (s.T > most || s.TK > most || s.H > most || s.T * s.H > most || s.TK * s.Hkv > most) return "rows x heads exceed 2^30";
+    if (s.Hkv > (1 << 20) / s.D) return fmt("Hkv x D = %lld x %lld exceeds 2^20", (long long)s.Hkv, (long long)s.D);
+    if (s.B > (1 << 24)) return fmt("B = %lld exceeds 2^24", (long long)s.B);
+    if (d->kind == RC_OP_ATTENTION_PACKED) return "";
+    if (s.page != 16 && s.page != 32 && s.page != 64 && s.page != 128 && s.page != 256)
+        return fmt("page = %lld: pages hold 16, 32, 64, 128 or 256 tokens", (long long)s.page);
+    if (s.width > most / s.page) return fmt("width x page = %lld x %lld exceeds 2^30", (long long)s.width, (long long)s.page);
+    if (s.pages > INT32_MAX || s.pages * s.Hkv > (1LL << 40) / s.page) return "pages x Hkv x page exceed 2^40";
+    return "";
+}
+
+// What a descriptor of an 8-bit kind, or one of attention in serving, must keep
+// to beyond positive
 // dimensions: "" or the first violated rule.  `size`: the rule is a limit of
 // the kernels, not a wrong argument.
 static std::string check_i8_desc(const rc_op_desc *d, bool *size) {
     *size = false;
     const int64_t *D = d->dim;
     switch (d->kind) {
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ:
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: return check_seqs_desc(d, size);
         case RC_OP_RMSNORM_I8:
             // (squares below fp32's normal range are nothing next to it)
             if (!(d->eps >= 0x1p-100f) || !std::isfinite(d->eps)) return "eps must be finite and at least 2^-100";
@@ -536,6 +601,37 @@ static std::string check_gemm_i8(const rc_op_desc *d, const rc_schedule *s) {
     const int64_t per_simd = std::max<int64_t>(occ, (waves + 3) / 4);
     if (regs + 24 > 512 / per_simd)
         return fmt("%lld accumulator and operand registers per lane leave too few at %lld waves/SIMD", (long long)regs, (long long)per_simd);
+    return "";
+}
+
+static std::string check_kv_cache(const rc_op_desc *d, const rc_schedule *s) {
+    const SeqDims q = seq_dims(d);
+    const int w = kv(d, s, "waves"), vec = kv(d, s, "vec");
+    if (redundant_tile(d, "waves", w, q.T)) return fmt("waves %d: waves %d already cover T = %lld", w, w / 2, (long long)q.T);
+    if ((q.T + w - 1) / w * 64 * w > MAX_GRID_THREADS) return "tokens of a wave each exceed the grid's 2^32 - 1 threads";
+    (void)vec;
+    return "";
+}
+
+int64_t seqs_items(const rc_op_desc *d, int bm, int splits) {
+    const SeqDims q = seq_dims(d);
+    return q.Hkv * (q.T * (q.H / q.Hkv) / bm + std::min(q.B, q.T)) + 256 * splits;
+}
+
+int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits) {
+    return std::min<int64_t>(256 * splits, seqs_items(d, bm, 0));
+}
+
+static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *s) {
+    const SeqDims q = seq_dims(d);
+    const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
+    if (redundant_tile(d, "block_m", bm, q.T * (q.H / q.Hkv)))
+        return fmt("block_m %d: block_m %d already covers all rows of a K/V head", bm, bm / 2);
+    const int64_t lds = (int64_t)w * bm * (q.D + 6) * 4;
+    if (lds > LDS_LIMIT) return fmt("the states of %d waves take %lld B of LDS, more than %lld", w, (long long)lds, (long long)LDS_LIMIT);
+    const int64_t regs = bm * q.D / 64 + bm / 4 * q.D / 32;
+    if (regs > 160) return fmt("%lld registers per lane for O and Q exceed 160", (long long)regs);
+    if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     return "";
 }
 
@@ -753,6 +849,10 @@ std::string check_schedule(const rc_op_desc *d, const rc_schedule *s) {
         case RC_OP_RMSNORM_I8:
         case RC_OP_QUANT_I8: return check_rows_i8(d, s);
         case RC_OP_GEMM_I8: return check_gemm_i8(d, s);
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return check_kv_cache(d, s);
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: return check_attention_seqs(d, s);
     }
     return "unknown operator kind";
 }
@@ -944,6 +1044,18 @@ static void suggest_gemm_i8(const rc_op_desc *d, rc_schedule *s) {
                     if (tile(tm, 16, tk, tm / 16, 1, 1, 1, sp, 0)) return;
 }
 
+static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
+    const SeqDims q = seq_dims(d);
+    set_knob(d, s, "vec", 8);
+    set_knob(d, s, "waves", q.T > 4 ? 4 : q.T > 1 ? 2 : 1);
+}
+
+static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
+    const SeqDims q = seq_dims(d);
+    (void)q;
+    set_knob(d, s, "waves", 4);
+}
+
 typedef std::vector<std::pair<rc_op_desc, rc_schedule>> Suggestions;
 
 static void list_once(Suggestions *out, const rc_op_desc &d, const rc_schedule &s) {
@@ -1025,6 +1137,23 @@ static void all_rows_i8(const rc_op_desc *kind, Suggestions *out) {
         }
 }
 
+// The same of the kinds of attention in serving.
+static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
+    const bool cache = kind->kind == RC_OP_KV_WRITE || kind->kind == RC_OP_KV_READ;
+    for (int64_t D : {64, 128, 256}) {         // (a definition of the kernels)
+        Suggestions once;
+        for (int64_t T : {1, 2, 3, 5, 1 << 20}) {
+            rc_op_desc d = *kind;
+            const int64_t dims[8] = {T, 1, 1, cache ? D : 1, cache ? 16 : d.kind == RC_OP_ATTENTION_PAGED ? D : 1,
+                                     cache || d.kind == RC_OP_ATTENTION_PAGED ? 16 : D, 1 << 16, 1 << 16};
+            for (int i = 0; i < expected_dims(d.kind); ++i) d.dim[i] = dims[i];
+            rc_schedule s;
+            if (rc_suggest_schedule(&d, &s) == RC_OK) list_once(&once, d, s);
+        }
+        out->insert(out->end(), once.begin(), once.end());
+    }
+}
+
 }  // namespace rc
 
 using namespace rc;
@@ -1092,6 +1221,16 @@ double rc_op_flops(const rc_op_desc *d) {
         case RC_OP_RMSNORM_I8:
         case RC_OP_QUANT_I8: return 0.0;     // no contraction
         case RC_OP_GEMM_I8: return ((d->flags & RC_FLAG_GATED) ? 4.0 : 2.0) * D[0] * D[1] * D[2];
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: return 0.0;
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: {
+            const SeqDims q = seq_dims(d);
+            const double n = (double)q.T / q.B, m = q.page ? (double)q.width * q.page : (double)q.TK / q.B;
+            // rows n of m keys each, or up to their own positions m - n .. m - 1
+            const double pairs = !(d->flags & RC_FLAG_CAUSAL) ? n * m : n <= m ? n * m - n * (n - 1) / 2 : m * (m + 1) / 2;
+            return 4.0 * q.D * q.H * q.B * pairs;
+        }
     }
     return -1.0;
 }
@@ -1118,6 +1257,18 @@ double rc_op_bytes(const rc_op_desc *d) {
             return (double)D[0] * D[2] + 4.0 * D[0] + nb * ((double)D[1] * D[2] + 4.0 * D[1]) +
                    ((d->flags & RC_FLAG_BIAS) ? 4.0 * D[1] : 0.0) +
                    ((d->flags & RC_FLAG_OUT_F32) ? 4.0 : 2.0) * D[0] * D[1];
+        }
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ:
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: {
+            const SeqDims q = seq_dims(d);
+            // K and V of a token, in the cache or packed; offsets, and lengths with the table
+            const double token = q.Hkv * ((d->flags & RC_FLAG_I8_CACHE) ? 2.0 * q.D + 8 : 4.0 * q.D);
+            const double where = 4.0 * (q.B + 1) + (q.page ? 4.0 * q.B * (1 + q.width) : 4.0 * (q.B + 1));
+            if (d->kind == RC_OP_ATTENTION_PACKED) return 4.0 * q.T * q.H * q.D + token * q.TK + where;
+            if (d->kind == RC_OP_ATTENTION_PAGED) return 4.0 * q.T * q.H * q.D + token * q.B * q.width * q.page + where;
+            return q.T * (token + 4.0 * q.Hkv * q.D) + where;
         }
     }
     return -1.0;
@@ -1187,6 +1338,10 @@ rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) try {
         suggest_rows_i8(d, &s);
     else if (d->kind == RC_OP_GEMM_I8)
         suggest_gemm_i8(d, &s);
+    else if (d->kind == RC_OP_KV_WRITE || d->kind == RC_OP_KV_READ)
+        suggest_kv_cache(d, &s);
+    else if (d->kind == RC_OP_ATTENTION_PAGED || d->kind == RC_OP_ATTENTION_PACKED)
+        suggest_attention_seqs(d, &s);
     else
         return fail(RC_ERR_UNSUPPORTED, "schedules of this kind are found by search, not suggested");
     std::string why = check_schedule(d, &s);
@@ -1199,14 +1354,23 @@ rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out) try {
 
 rc_status rc_suggestions(int32_t kind, int32_t flags, rc_op_desc *descs, rc_schedule *out, int32_t cap, int32_t *n) try {
     if (!n || cap < 0 || (cap > 0 && (!descs || !out))) return fail(RC_ERR_INVALID_ARGUMENT, "bad arguments");
-    if (kind != RC_OP_RMSNORM_I8 && kind != RC_OP_QUANT_I8 && kind != RC_OP_GEMM_I8)
+    if (kind < RC_OP_RMSNORM_I8 || kind > RC_OP_ATTENTION_PACKED)
         return fail(RC_ERR_UNSUPPORTED, "schedules of this kind are found by search, not suggested");
-    const int64_t one[] = {1, 1, 1};
+    const bool seqs = kind >= RC_OP_KV_WRITE;
+    int64_t least[RC_MAX_DIMS] = {1, 1, 1, 1, 1, 1, 1, 1};
+    if (seqs) {
+        const int64_t cache[] = {1, 1, 1, 64, 16, 1, 1}, paged[] = {1, 1, 1, 1, 64, 16, 1, 1}, packed[] = {1, 1, 1, 1, 1, 64};
+        if (kind == RC_OP_ATTENTION_PAGED) std::copy(paged, paged + 8, least);
+        else if (kind == RC_OP_ATTENTION_PACKED) std::copy(packed, packed + 6, least);
+        else std::copy(cache, cache + 7, least);
+    }
     rc_op_desc d;
-    rc_status r = rc_op_init(&d, kind, one, kind == RC_OP_GEMM_I8 ? 3 : 2, flags);
+    rc_status r = rc_op_init(&d, kind, least, expected_dims(kind), flags);
     if (r != RC_OK) return r;
     Suggestions all;
-    if (kind == RC_OP_GEMM_I8)
+    if (seqs)
+        all_seqs(&d, &all);
+    else if (kind == RC_OP_GEMM_I8)
         all_gemm_i8(&d, &all);
     else
         all_rows_i8(&d, &all);

@@ -41,6 +41,17 @@ int64_t gemm_i8_tail_tiles(int64_t tiles, int tm, int tn, int tk, int waves, int
 bool gemm_tail_split(int tm, int tn, int tk, int nb, int waves, int occ, int st, int64_t M, int64_t N,
                      int64_t *main_cols, int64_t *tail_cols);
 
+// Sizes of a kind of attention in serving (0 where it has none).
+struct SeqDims {
+    int64_t T, TK, B, H, Hkv, D, page, pages, width;
+};
+SeqDims seq_dims(const rc_op_desc *d);
+int expected_dims(int32_t kind);
+// Work items that an attention over sequences has at most, and blocks of rows of
+// which it cuts the keys (at most 2 pieces a workgroup that it cuts them for).
+int64_t seqs_items(const rc_op_desc *d, int bm, int splits);
+int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits);
+
 // Legality with a reason; "" when legal.
 std::string check_schedule(const rc_op_desc *d, const rc_schedule *s);
 

@@ -80,6 +80,15 @@ struct GemmI8Args {
     long long M;
     int N, K, KP, tail;
 };
+struct CacheArgs {
+    const void *k, *v, *K, *V, *Ks, *Vs, *offsets, *lens, *table;
+    int T, B, HKV, shift, pages, width;
+};
+struct SeqsArgs {
+    const void *Q, *K, *V, *Ks, *Vs, *offsets, *lens, *table;
+    void *O, *P;
+    int T, TK, B, G, HKV, shift, pages, width, causal, slots;
+};
 struct PadI8Args {
     const void *A, *B0, *B1;
     void *out;
@@ -90,7 +99,7 @@ struct PadI8Args {
 // A kernel's by-value argument block (fixed storage: launching allocates
 // nothing on the host).
 struct ArgBlob {
-    alignas(16) char data[128];
+    alignas(16) char data[160];
     size_t size = 0;
 };
 
@@ -934,6 +943,65 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             }
             break;
         }
+        case RC_OP_KV_WRITE:
+        case RC_OP_KV_READ: {
+            const SeqDims q = seq_dims(d);
+            const bool i8 = d->flags & RC_FLAG_I8_CACHE, write = d->kind == RC_OP_KV_WRITE;
+            const int w = kv(d, s, "waves");
+            Kern k;
+            k.src = Source{SRC_kv_cache, write ? "rc_kv_write" : "rc_kv_read",
+                           def("WAVES", w) + def("VEC", kv(d, s, "vec")) + def("HD", q.D) + def("I8", i8)};
+            k.grid = dim3((unsigned)((q.T + w - 1) / w), 1, 1);
+            k.block = dim3(64 * w, 1, 1);
+            k.bind = [=](const rc_args *a, char *, ArgBlob &b) {
+                const void *const *cache = write ? (const void *const *)a->out : a->in;
+                const void *const *rows = write ? a->in : (const void *const *)a->out;
+                const void *const *at = a->in + (write ? 2 : i8 ? 4 : 2);
+                put(b, CacheArgs{rows[0], rows[1], cache[0], cache[1], i8 ? cache[2] : nullptr, i8 ? cache[3] : nullptr,
+                                 at[0], at[1], at[2], (int)q.T, (int)q.B, (int)q.Hkv, __builtin_ctzll(q.page), (int)q.pages,
+                                 (int)q.width});
+            };
+            p.kerns.push_back(k);
+            p.dominant = 0;
+            break;
+        }
+        case RC_OP_ATTENTION_PAGED:
+        case RC_OP_ATTENTION_PACKED: {
+            const SeqDims q = seq_dims(d);
+            const bool paged = d->kind == RC_OP_ATTENTION_PAGED, i8 = d->flags & RC_FLAG_I8_CACHE;
+            const int causal = (d->flags & RC_FLAG_CAUSAL) != 0;
+            const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
+            // states of the pieces of cut blocks: fewer than two a workgroup that
+            // the keys are cut for
+            const size_t offP = sp ? ws.add((size_t)512 * sp * bm * (q.D + 2) * 4, "partials") : 0;
+            char scale[64];
+            snprintf(scale, sizeof scale, "#define SCALE_LOG2 %.17gf\n", 1.4426950408889634 / std::sqrt((double)q.D));
+            Kern k;
+            k.src = Source{SRC_attention_seqs, "rc_attention_seqs",
+                           def("BM", bm) + def("NW", w) + def("STAGES", kv(d, s, "stages")) + def("SPLIT", sp > 0) + def("HD", q.D) + def("PAGED", paged) +
+                               def("I8", i8) + def("LEAST", 2 * w) + scale};
+            k.grid = dim3((unsigned)seqs_items(d, bm, sp), 1, 1);
+            k.block = dim3(64 * w, 1, 1);
+            k.flops = rc_op_flops(d);
+            k.bind = [=](const rc_args *a, char *wsp, ArgBlob &b) {
+                const int at = i8 ? 5 : 3;
+                put(b, SeqsArgs{a->in[0], a->in[1], a->in[2], i8 ? a->in[3] : nullptr, i8 ? a->in[4] : nullptr, a->in[at],
+                                a->in[at + 1], paged ? a->in[at + 2] : nullptr, a->out[0], sp ? wsp + offP : nullptr,
+                                (int)q.T, (int)q.TK, (int)q.B, (int)(q.H / q.Hkv), (int)q.Hkv,
+                                paged ? __builtin_ctzll(q.page) : 0, (int)q.pages, (int)q.width, causal, 256 * sp});
+            };
+            p.kerns.push_back(k);
+            if (sp) {
+                Kern kj = k;
+                kj.flops = 0;
+                kj.src.entry = "rc_attention_seqs_join";
+                kj.grid = dim3((unsigned)(seqs_cut_blocks(d, bm, sp) * bm / 4), 1, 1);
+                kj.block = dim3(256, 1, 1);
+                p.kerns.push_back(kj);
+            }
+            p.dominant = 0;
+            break;
+        }
         default: return fail(RC_ERR_UNSUPPORTED, "unknown operator kind");
     }
     for (auto &k : p.kerns) {
@@ -957,6 +1025,10 @@ int n_inputs(const rc_op_desc &d) {
         case RC_OP_RMSNORM_I8: return (d.flags & RC_FLAG_RESIDUAL) ? 3 : 2;
         case RC_OP_QUANT_I8: return 1;
         case RC_OP_GEMM_I8: return (d.flags & RC_FLAG_GATED) ? 6 : (d.flags & RC_FLAG_BIAS) ? 5 : 4;
+        case RC_OP_KV_WRITE: return 5;
+        case RC_OP_KV_READ: return (d.flags & RC_FLAG_I8_CACHE) ? 7 : 5;
+        case RC_OP_ATTENTION_PAGED: return (d.flags & RC_FLAG_I8_CACHE) ? 8 : 6;
+        case RC_OP_ATTENTION_PACKED: return 5;
     }
     return 0;
 }
@@ -965,6 +1037,8 @@ int n_outputs(const rc_op_desc &d) {
     switch (d.kind) {
         case RC_OP_RMSNORM_I8: return (d.flags & RC_FLAG_RESIDUAL) ? 3 : 2;
         case RC_OP_QUANT_I8: return 2;
+        case RC_OP_KV_WRITE: return (d.flags & RC_FLAG_I8_CACHE) ? 4 : 2;
+        case RC_OP_KV_READ: return 2;
     }
     return 1;
 }
@@ -1199,8 +1273,38 @@ rc_status rc_time_release(void) {
     return r;
 }
 
-// Bytes of the operands of an 8-bit kind.
+// Bytes of the operands of a kind of attention in serving.
+static void seqs_operand_bytes(const rc_op_desc &d, size_t (&in)[8], size_t (&out)[4]) {
+    const SeqDims q = seq_dims(&d);
+    const bool i8 = d.flags & RC_FLAG_I8_CACHE;
+    const size_t slots = (size_t)q.pages * q.Hkv * q.page, rows = 2 * (size_t)q.T * q.Hkv * q.D;
+    const size_t at[3] = {4 * ((size_t)q.B + 1), 4 * (size_t)q.B, 4 * (size_t)q.B * q.width};
+    size_t cache[4] = {slots * q.D * (i8 ? 1 : 2)}, n = i8 ? 4 : 2;
+    cache[1] = cache[0];
+    cache[2] = cache[3] = 4 * slots;
+    if (d.kind == RC_OP_KV_WRITE) {
+        in[0] = in[1] = rows;
+        std::copy(at, at + 3, in + 2);
+        std::copy(cache, cache + n, out);
+    } else if (d.kind == RC_OP_KV_READ) {
+        std::copy(cache, cache + n, in);
+        std::copy(at, at + 3, in + n);
+        out[0] = out[1] = rows;
+    } else {
+        in[0] = out[0] = 2 * (size_t)q.T * q.H * q.D;
+        if (d.kind == RC_OP_ATTENTION_PAGED) {
+            std::copy(cache, cache + n, in + 1);
+            std::copy(at, at + 3, in + 1 + n);
+        } else {
+            in[1] = in[2] = 2 * (size_t)q.TK * q.Hkv * q.D;
+            in[3] = in[4] = at[0];
+        }
+    }
+}
+
+// Bytes of the operands of an 8-bit kind, or one of attention in serving.
 static void i8_operand_bytes(const rc_op_desc &d, size_t (&in)[8], size_t (&out)[4]) {
+    if (d.kind >= RC_OP_KV_WRITE) return seqs_operand_bytes(d, in, out);
     const size_t r = (size_t)d.dim[0], c = (size_t)d.dim[1], k = (size_t)d.dim[2];
     if (d.kind == RC_OP_GEMM_I8) {
         const size_t v[] = {r * k, 4 * r, c * k, 4 * c, (d.flags & RC_FLAG_GATED) ? c * k : 4 * c, 4 * c};
@@ -1214,7 +1318,7 @@ static void i8_operand_bytes(const rc_op_desc &d, size_t (&in)[8], size_t (&out)
     }
 }
 
-// The first overlap of what a launch of an 8-bit kind writes (outputs and
+// The first overlap of what a launch of such a kind writes (outputs and
 // workspace) with anything else it is given, "" if none.  Workgroups read
 // their inputs while others write: an overlap would give wrong results
 // without an error.

@@ -24,9 +24,11 @@ STATUS = {0: "RC_OK", 1: "RC_ERR_INVALID_ARGUMENT", 2: "RC_ERR_ILLEGAL_SCHEDULE"
 
 RC_OP_GEMM_F32, RC_OP_ATTENTION, RC_OP_GATED_MLP, RC_OP_MOE, RC_OP_CONV2D = 1, 2, 3, 4, 5
 RC_OP_RMSNORM_I8, RC_OP_QUANT_I8, RC_OP_GEMM_I8 = 6, 7, 8
+RC_OP_KV_WRITE, RC_OP_KV_READ, RC_OP_ATTENTION_PAGED, RC_OP_ATTENTION_PACKED = 9, 10, 11, 12
 RC_FLAG_CAUSAL = 1
 RC_FLAG_NO_ACT = 2
 RC_FLAG_RESIDUAL, RC_FLAG_BIAS, RC_FLAG_OUT_F32, RC_FLAG_GATED = 4, 8, 16, 32
+RC_FLAG_I8_CACHE = 64
 RC_POLICY_RANDOM, RC_POLICY_UCT, RC_POLICY_EXHAUSTIVE = 0, 1, 2
 MAX_DIMS, MAX_KNOBS = 8, 32
 
@@ -289,7 +291,8 @@ class Op:
         return Schedule(self, s)
 
     def suggest(self) -> "Schedule":
-        """A legal schedule by rules on the sizes (the 8-bit kinds)."""
+        """A legal schedule by rules on the sizes (the 8-bit kinds and those of
+        attention in serving)."""
         s = rc_schedule()
         _check(lib().rc_suggest_schedule(self.ref, ctypes.byref(s)), "rc_suggest_schedule")
         return Schedule(self, s)
@@ -367,12 +370,14 @@ class Schedule:
 
 def suggestions(kind: int, flags: int = 0) -> List[tuple]:
     """(Op, Schedule) of every schedule that Op.suggest may return for a kind
-    and flags (the 8-bit kinds), each at sizes where it is legal."""
+    and flags (the 8-bit kinds and those of attention in serving), each at sizes
+    where it is legal."""
     n = ctypes.c_int32()
     _check(lib().rc_suggestions(kind, flags, None, None, 0, ctypes.byref(n)), "rc_suggestions")
     descs, scheds = (rc_op_desc * n.value)(), (rc_schedule * n.value)()
     _check(lib().rc_suggestions(kind, flags, descs, scheds, n, ctypes.byref(n)), "rc_suggestions")
-    nd = 3 if kind == RC_OP_GEMM_I8 else 2
+    nd = {RC_OP_GEMM_I8: 3, RC_OP_KV_WRITE: 7, RC_OP_KV_READ: 7, RC_OP_ATTENTION_PAGED: 8,
+          RC_OP_ATTENTION_PACKED: 6}.get(kind, 2)
     ops = [Op(kind, list(d.dim)[:nd], flags) for d in descs]
     return [(op, Schedule(op, s).copy()) for op, s in zip(ops, scheds)]
 
@@ -491,10 +496,12 @@ def _pack_args(inputs: Iterable, output) -> bytes:
 
 def _i8_tensors(op: Op):
     """(name, dtype, shape) of the inputs and of the outputs of an 8-bit
-    operator, which Plan checks at each launch: a wrong type or size would
-    read or write past a buffer."""
+    operator or one of attention in serving, which Plan checks at each launch: a
+    wrong type or size would read or write past a buffer."""
     import torch
     bf16, f32, i8 = torch.bfloat16, torch.float32, torch.int8
+    if op.kind >= RC_OP_KV_WRITE:
+        return _seqs_tensors(op)
     if op.kind == RC_OP_GEMM_I8:
         m, n, k = op.dims
         ins = [("A", i8, (m, k)), ("sa", f32, (m,)), ("B", i8, (n, k)), ("sb", f32, (n,))]
@@ -511,6 +518,30 @@ def _i8_tensors(op: Op):
             ins.append(("r", bf16, (t, c)))
             outs.append(("h", bf16, (t, c)))
     return ins, outs
+
+
+def _seqs_tensors(op: Op):
+    """_i8_tensors of the operators of attention in serving."""
+    import torch
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    if op.kind == RC_OP_ATTENTION_PACKED:
+        t, tk, b, h, hkv, d = op.dims
+        kv = [(name, bf16, (tk, hkv, d)) for name in ("K", "V")]
+        return ([("Q", bf16, (t, h, d))] + kv + [("offsets", i32, (b + 1,)), ("koffsets", i32, (b + 1,))],
+                [("O", bf16, (t, h, d))])
+    if op.kind == RC_OP_ATTENTION_PAGED:
+        t, b, h, hkv, d, page, pages, width = op.dims
+    else:
+        t, b, hkv, d, page, pages, width = op.dims
+    i8 = op.flags & RC_FLAG_I8_CACHE
+    cache = [(name, torch.int8 if i8 else bf16, (pages, hkv, page, d)) for name in ("K", "V")]
+    if i8:
+        cache += [(name, f32, (pages, hkv, page)) for name in ("Ks", "Vs")]
+    where = [("offsets", i32, (b + 1,)), ("lens", i32, (b,)), ("table", i32, (b, width))]
+    if op.kind == RC_OP_ATTENTION_PAGED:
+        return [("Q", bf16, (t, h, d))] + cache + where, [("O", bf16, (t, h, d))]
+    rows = [(name, bf16, (t, hkv, d)) for name in ("k", "v")]
+    return (rows + where, cache) if op.kind == RC_OP_KV_WRITE else (cache + where, rows)
 
 
 def _check_tensors(tensors, device: int, inputs, output, workspace, stream):
@@ -656,7 +687,8 @@ class Plan:
 
     def launch(self, inputs, output, workspace=None, stream=None) -> None:
         """rc_launch.  ``output``: a tensor, or a tuple of an operator's
-        several outputs.  Tensors of the 8-bit kinds are checked."""
+        several outputs.  Tensors of the 8-bit kinds and those of attention in
+        serving are checked."""
         wsz = 0 if workspace is None else workspace.numel() * workspace.element_size()
         if self._tensors:
             block, stream = self._pack(inputs, output, workspace, stream)
