@@ -7,7 +7,10 @@
 //   BM      rows of a work item (TileSize), see below
 //   NW      waves that share an item's keys (Parallel)
 //   STAGES  1: a tile is loaded, then computed; 2: the next tile's loads are
-//           under way meanwhile (ComputeLocation)
+//           under way meanwhile; 3: tiles go through a ring in shared memory,
+//           and two halves of the waves take turns on the matrix cores
+//           (ComputeLocation)
+//   OCC     waves per SIMD the register allocation must leave room for
 //   SPLIT   1: the keys of a sequence are cut into pieces for several
 //           workgroups, whose states rc_attention_seqs_join puts together
 //   HD      head dimension: 64, 128 or 256
@@ -37,8 +40,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
 typedef u32 u32x4 __attribute__((ext_vector_type(4)));
 
-#define QB (BM / 16)               // blocks of 16 rows
-#define BN 32                      // keys of a tile
+#if STAGES == 3
+#define QB (BM / 64)               // blocks of 16 rows of a wave
+#define BN (HD == 256 ? 32 : 64)   // keys of a tile
+#else
+#define QB (BM / 16)
+#define BN 32
+#endif
 #define NKS (HD / 32)              // MFMA steps of the score product
 #define DE (HD / 16)               // elements of V that a lane takes of a key
 #define ELT (I8 ? 1 : 2)           // bytes of an element of K and V
@@ -162,8 +170,18 @@ template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int
     return false;
 }
 
+// -inf (no key seen yet) as a finite number: what is -inf relative to it stays so
+__device__ __forceinline__ float least_finite(float m) { return fmaxf(m, -0x1.fffffep127f); }
+
 // State of a piece: m and l of its rows, then their sums of p V
 #define STATE (BM * (HD + 2))
+
+__device__ __forceinline__ u32 pack2(float a, float b) {
+    return __builtin_bit_cast(u32, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
+__device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
 // ---------------------------------------------------------------------------
 // Keys and values straight to registers
@@ -178,12 +196,41 @@ template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int
 // DE i + e as its 16 rows.  The keys of a lane are those of its scores (4 (lane
 // / 16) + r of each 16), so that P^T stays where it is.
 
-__device__ __forceinline__ u32 pack2(float a, float b) {
-    return __builtin_bit_cast(u32, __builtin_convertvector((f32x2){a, b}, bf16x2));
+// Values that are not finite, in a tile that some row does not see whole: 0 times
+// one is a NaN.  O += V^T P^T takes them as 0, and +-1 in their place (a NaN both)
+// times the keys that a row sees (1, or 0) says which of its sums are infinite.
+__device__ __forceinline__ bool far(u32 half) { return (half & 0x7F80u) == 0x7F80u; }
+__device__ __forceinline__ bf16x8 ones(const u32x4 &v, u32 but) {
+    u32x4 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const u32 lo = v[j] & 0xFFFFu, hi = v[j] >> 16;
+        f[j] = (far(lo) && lo != but ? 0x3F80u : 0u) | (far(hi) && hi != but ? 0x3F800000u : 0u);
+    }
+    return __builtin_bit_cast(bf16x8, f);
 }
-__device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+__device__ __forceinline__ bf16x8 seen(const f32x4 &s0, const f32x4 &s1) {
+    const float none = -__builtin_inff();
+    u32x4 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f32x4 &s = j < 2 ? s0 : s1;
+        f[j] = (s[2 * (j % 2)] == none ? 0u : 0x3F80u) | (s[2 * (j % 2) + 1] == none ? 0u : 0x3F800000u);
+    }
+    return __builtin_bit_cast(bf16x8, f);
 }
+__device__ __forceinline__ f32x4 add_far(const u32x4 &v, const bf16x8 &p, const bf16x8 &see, const f32x4 &o) {
+    u32x4 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = v[j] & ~((far(v[j]) ? 0xFFFFu : 0u) | (far(v[j] >> 16) ? 0xFFFF0000u : 0u));
+    f32x4 x = mfma(__builtin_bit_cast(bf16x8, f), p, o);
+    const f32x4 up = mfma(ones(v, 0xFF80u), see, f32x4{}), down = mfma(ones(v, 0x7F80u), see, f32x4{});
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] += (up[r] > 0.f ? __builtin_inff() : 0.f) - (down[r] > 0.f ? __builtin_inff() : 0.f);
+    return x;
+}
+
+#if STAGES < 3
 // byte e of w as a float
 __device__ __forceinline__ float byte(u32 w, int e) { return (float)(signed char)(w >> (8 * e)); }
 
@@ -196,7 +243,7 @@ struct Tile {
     int held;          // of the two 16-key blocks
 };
 
-extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs a) {
+extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OCC, 8))) void rc_attention_seqs(SeqsArgs a) {
     __shared__ __attribute__((aligned(16))) float osum[NW][BM][HD + 4];
     __shared__ float om[NW][BM], ol[NW][BM];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -235,11 +282,11 @@ extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs
     const int nt = __builtin_amdgcn_readfirstlane(t1 > t0 ? (t1 - t0 + NW - 1) / NW : 0);
 
     f32x4 o[QB][DE];
-    float m[QB], minus[QB], l[QB];         // minus: -m, or 0 while no key was seen
+    float m[QB], l[QB];
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         m[b] = -__builtin_inff();
-        minus[b] = l[b] = 0.f;
+        l[b] = 0.f;
 #pragma unroll
         for (int e = 0; e < DE; ++e) o[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -341,14 +388,14 @@ extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs
 #if I8
                     if (!there) x.vs[c][r] = 0.f;
 #else
-                    u32 far = 0;
+                    bool some = false;
 #pragma unroll
                     for (int e = 0; e < DE * ELT / 4; ++e) {
                         u32 &v = x.v[4 * c + r][e];
                         v = there ? v : 0;
-                        far |= ((v & 0x7F80u) == 0x7F80u) | ((v & 0x7F800000u) == 0x7F800000u);
+                        some |= far(v) | far(v >> 16);
                     }
-                    apart |= far != 0;
+                    apart |= some;
 #endif
                 }
         }
@@ -368,14 +415,14 @@ extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs
 #pragma unroll
                 for (int e = 0; e < DE; ++e) o[b][e] *= by;
                 m[b] = now;
-                minus[b] = now == -__builtin_inff() ? 0.f : -now;
             }
+            const float minus = -least_finite(m[b]);
             float pr[2][4];
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    pr[c][r] = pow2(__builtin_fmaf(sc[b][c][r], SCALE_LOG2, minus[b]));
+                    pr[c][r] = pow2(__builtin_fmaf(sc[b][c][r], SCALE_LOG2, minus));
                     l[b] += pr[c][r];
 #if I8
                     // V's scale goes into p; a key that the row does not see has none
@@ -403,28 +450,12 @@ extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs
             return f;
         };
         if (!I8 && __builtin_amdgcn_ballot_w64(apart) != 0) {
-            // Key by key, so that a row leaves out what it does not see (0 times
-            // an infinity or a NaN is a NaN)
-#pragma nounroll
-            for (int k = 0; k < BN; ++k) {
-                // (what is formed from V is formed anew: held, it takes as many registers again)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+            for (int e = 0; e < DE; ++e) {
+                const u32x4 v = values(e);
 #pragma unroll
-                    for (int e = 0; e < DE * ELT / 4; ++e) asm volatile("" : "+v"(x.v[j][e]));
-                const int at = k / 16 * 4 + k % 4;      // its place among the 8 of the lanes g = k % 16 / 4
-                u32x4 only;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) only[j] = g == k % 16 / 4 && at / 2 == j ? (at % 2 ? 0xFFFF0000u : 0xFFFFu) : 0u;
-#pragma unroll
-                for (int b = 0; b < QB; ++b)
-#pragma unroll
-                    for (int e = 0; e < DE; ++e) {
-                        const f32x4 t = mfma(__builtin_bit_cast(bf16x8, values(e) & only),
-                                             __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, p[b]) & only), f32x4{0.f, 0.f, 0.f, 0.f});
-                        if (key0 + k <= vis[b]) o[b][e] += t;
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                for (int b = 0; b < QB; ++b) o[b][e] = add_far(v, p[b], seen(sc[b][0], sc[b][1]), o[b][e]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             return;
         }
@@ -498,6 +529,452 @@ extern "C" __global__ __launch_bounds__(64 * NW) void rc_attention_seqs(SeqsArgs
         }
     }
 }
+
+#endif
+
+// ---------------------------------------------------------------------------
+// Keys and values through shared memory, in turns (STAGES 3)
+// ---------------------------------------------------------------------------
+//
+// Eight waves: four of 16 QB rows each for the even key tiles of the piece, and
+// four for the odd ones, with their own softmax states, put together at the
+// end.  Waves w and w + 4 share a SIMD and take turns on its matrix cores: while
+// one multiplies (O^T += V^T P^T of its tile, then S^T = K Q^T of its next),
+// the other does its softmax (vector work); a barrier ends each turn.  K and V
+// go straight from memory to shared memory, into a ring of two tiles for each
+// operand and half of the waves; the softmax turn issues the loads between its
+// exponentials, K of the tile after the next and V of the next, into the places
+// that the matrix turn before it has read, and waits for those of the softmax
+// turn before.  16-byte chunks of a row are XOR-ed with the row's number (KSWZ,
+// VSWZ), by the choice of what a lane fetches, so that fragment reads have no
+// bank conflicts; V's are transposed by the reading instruction.
+
+#if STAGES == 3
+#define ROWG 4                     // groups of rows
+#define BNW (BN / ROWG)            // keys that a wave loads of a tile
+#define KB (BN / 16)
+#define DB (HD / 16)
+#define CPR (HD / 8)               // 16-byte chunks of a row
+#define RPL ((16 / CPR) > 0 ? (16 / CPR) : 1)
+#define KSWZ(r) (((r) / RPL) % (CPR < 16 ? CPR : 16))
+#define VSWZ(r) ((2 * (r)) & (CPR - 1))
+#define TILE (BN * HD)
+#define NPJ (BN / 32)              // MFMA steps of P V
+#define NKF (KB * NKS)             // fragments of K and of V
+#define NVF (NPJ * DB)
+#define AHEAD 8                    // of them read ahead of their MFMAs
+#define WL (TILE / 512 / ROWG)     // 1 KiB loads of a wave for a tile
+#define RPI (512 / HD)             // rows of one
+
+template <int V> struct IntC { static constexpr int value = V; };
+// seq<A, B>(f): f(IntC<A>), ... f(IntC<B - 1>), every index a constant
+template <class T, T... I> struct ISeq {};
+template <int A, class F, int... I> __device__ __forceinline__ void seq_calls(F &f, ISeq<int, I...>) {
+    (f(IntC<A + I>{}), ...);
+}
+template <int A, int B, class F> __device__ __forceinline__ void seq(F &&f) {
+    if constexpr (B > A) seq_calls<A>(f, __make_integer_seq<ISeq, int, B - A>{});
+}
+// at most n loads of this wave are left in flight
+#define WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | ((((n) >> 4) & 3) << 14) | (7 << 4) | (15 << 8))
+
+extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void rc_attention_seqs(SeqsArgs a) {
+    __shared__ __attribute__((aligned(16))) bf16_t ring[8][TILE];      // K of each half's two tiles, then V
+    __shared__ int again;
+    if (threadIdx.x == 0) again = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = lane % 16, g = lane / 16, rg = wave % ROWG, sp = wave / ROWG;
+    Item item;
+    if (!find<false>(a, blockIdx.x, item)) return;
+    const Seq s = item.s;
+    const int rows = s.n * a.G, r0 = item.block * BM, r0w = r0 + 16 * QB * rg;
+
+    // tiles of the block's last row, of the piece
+    const int last_vis = s.vis((min(rows, r0 + BM) - 1) / a.G, a.causal);
+    const int all = (max(last_vis + 1, 0) + BN - 1) / BN, share = (all + item.pieces - 1) / item.pieces;
+    const int kt0 = item.piece * share, n_kt = max(0, min(all, kt0 + share) - kt0);
+    const int n_it = (n_kt + 1) / 2, n_loc = (n_kt + 1 - sp) / 2;      // turns; tiles of this half
+
+    // loads: lane's byte offsets within the wave's rows of a tile
+#if PAGED
+    constexpr u32 step = HD * 2;
+#else
+    const u32 step = (u32)a.HKV * (HD * 2);
+#endif
+    u32 k_src[WL], v_src[WL];
+#pragma unroll
+    for (int j = 0; j < WL; ++j) {
+        const int r = j * RPI + lane / CPR, row = rg * BNW + r, c = lane % CPR;
+        k_src[j] = r * step + 16 * (c ^ KSWZ(row));
+        v_src[j] = r * step + 16 * (c ^ VSWZ(row));
+    }
+    typedef __attribute__((address_space(3))) bf16_t *lds_p;
+    const u32 lds0 = (u32)(size_t)(lds_p)ring[0] + rg * (WL * 1024u);
+    // K or V (v) of this half's slot b
+    auto slot = [&](int v, int b) { return lds0 + (u32)(4 * v + 2 * sp + b) * (TILE * 2u); };
+    // (issued from inline assembly, which the compiler's own waits do not see:
+    // it would drain them before every read of shared memory)
+    auto dma = [&](const char *base, u32 off, u32 lds) {
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+    };
+    // Where the wave's rows of the half's tile `it` start, and the last of them
+    // that is a key (past the sequence's last key: that one, which is there).
+    // Past the half's last tile: that one again, which nothing reads.
+    struct From {
+        size_t at;
+        int end;
+    };
+    const int last_key = s.keys - 1;
+    int ids = 0;                           // pages of the wave's rows of 64 tiles
+    auto first_key = [&](int it) { return min((kt0 + 2 * it + sp) * BN + BNW * rg, last_key & ~(BNW - 1)); };
+    auto rows_of = [&](int it) {
+        it = min(it, max(n_loc - 1, 0));
+        const int key = first_key(it);
+        From f;
+        f.end = last_key - key;
+#if PAGED
+        if (it % 64 == 0) {
+            const int x = first_key(it + lane);
+            ids = a.table[(size_t)s.k0 * a.width + (x >> a.shift)];
+        }
+        const int id = __builtin_amdgcn_readlane(ids, it % 64);
+        f.at = (((size_t)((u32)id < (u32)a.pages ? id : 0) * a.HKV + item.h) << a.shift) + (key & ((1 << a.shift) - 1));
+#else
+        f.at = (size_t)(s.k0 + key) * a.HKV + item.h;
+#endif
+        f.at *= HD * 2;
+        return f;
+    };
+    // loads j0 .. j1 - 1 of a tile; `edge`: rows past the last key fetch that one
+    auto load = [&](const char *src, const u32 (&off)[WL], const From &f, u32 lds, int j0, int j1, auto edge) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = j0; j < j1; ++j) {
+            u32 o = off[j];
+            if constexpr (decltype(edge)::value) o -= (u32)max(j * RPI + lane / CPR - f.end, 0) * step;
+            dma(src + f.at, o, lds + j * 1024u);
+        }
+    };
+    auto load_whole = [&](const char *src, const u32 (&off)[WL], const From &f, u32 lds) __attribute__((always_inline)) {
+        if (f.end < BNW - 1) load(src, off, f, lds, 0, WL, IntC<1>{});
+        else load(src, off, f, lds, 0, WL, IntC<0>{});
+    };
+
+    // (nothing to see: the states below stay empty)
+    From next = {0, BNW};
+    if (n_kt > 0) {
+        const From f = rows_of(0);
+        next = rows_of(1);
+        load_whole(a.K, k_src, f, slot(0, 0));
+        load_whole(a.V, v_src, f, slot(1, 0));
+        load_whole(a.K, k_src, next, slot(0, 1));
+    }
+    // is a page of the piece not held?
+    bool gaps = false;
+#if PAGED
+    for (int p = (kt0 * BN >> a.shift) + lane; n_kt > 0 && p <= min(last_key, (kt0 + n_kt) * BN - 1) >> a.shift; p += 64)
+        gaps |= (u32)a.table[(size_t)s.k0 * a.width + p] >= (u32)a.pages;
+    gaps = __builtin_amdgcn_ballot_w64(gaps) != 0;
+#endif
+    auto held = [&](int key) {
+        if (!PAGED || !gaps) return true;
+        return (u32)a.table[(size_t)s.k0 * a.width + (min(key, last_key) >> a.shift)] < (u32)a.pages;
+    };
+
+    bf16x8 qf[QB][NKS];
+    int vis[QB], least = 1 << 30, most = -1;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int r = r0w + 16 * b + i, token = r / a.G;
+        vis[b] = 1 << 30;          // (rows that there are not)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) qf[b][ks] = bf16x8{};
+        if (r < rows) {
+            vis[b] = s.vis(token, a.causal);
+            least = min(least, vis[b]);
+            most = max(most, vis[b]);
+            const bf16_t *p = a.Q + ((size_t)(s.q0 + token) * a.HKV * a.G + item.h * a.G + r % a.G) * HD;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) qf[b][ks] = *(const bf16x8 *)(p + 32 * ks + 8 * g);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        least = min(least, __shfl_xor(least, d));
+        most = max(most, __shfl_xor(most, d));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    most = __builtin_amdgcn_readfirstlane(most);
+    // (their loads end before the loop, whose waits count the ring's alone)
+#pragma unroll
+    for (int b = 0; b < QB; ++b)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) asm volatile("" ::"v"(qf[b][ks]));
+    WAIT_VM(0);
+    __syncthreads();
+
+    f32x4 o[QB][DB];
+    float m[QB], l[QB];
+    auto clear = [&] {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            m[b] = -__builtin_inff();
+            l[b] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    clear();
+
+    typedef short v4i16 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4i16 *lds_v4p;
+    // Fragments, at an element of shared memory: of K at k0 + its tile's, with
+    // the chunk 4 ks + g XOR-ed as above, which is an XOR of the whole index (a
+    // tile starts at a multiple of HD); of V likewise
+    const int k0 = 2 * sp * TILE + i * HD + 8 * (g ^ KSWZ(i));
+    const int vr = 4 * g + i / 4, v0 = (4 + 2 * sp) * TILE + vr * HD + 8 * ((lane & 3) / 2 ^ VSWZ(vr)) + (lane & 1) * 4;
+    auto read_kf = [&](auto fc, int k) __attribute__((always_inline)) {
+        constexpr int f = decltype(fc)::value;
+        return *(const bf16x8 *)(ring[0] + (k ^ 32 * (f % NKS)) + (f / NKS) * 16 * HD);
+    };
+    auto read_v = [&](int v, int d, int j) __attribute__((always_inline)) {
+        const bf16_t *const p = ring[0] + (v ^ 16 * d) + 32 * j * HD;
+        const v4i16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4p)(p));
+        const v4i16 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4p)(p + 16 * HD));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto read_vf = [&](auto fc, int v) __attribute__((always_inline)) {
+        constexpr int f = decltype(fc)::value;
+        return read_v(v, f % DB, f / DB);
+    };
+    static_assert(NVF % AHEAD == 0 && NKF >= AHEAD, "fragment ring");
+    f32x4 sc[QB][KB];
+    bf16x8 pf[NPJ][QB], fr[AHEAD];
+    // S^T of a tile: its first AHEAD fragments are in fr
+    auto qk = [&](int k) __attribute__((always_inline)) {
+        seq<0, NKF>([&](auto fc) __attribute__((always_inline)) {
+            constexpr int f = decltype(fc)::value, kb = f / NKS, ks = f % NKS;
+            const bf16x8 x = fr[f % AHEAD];
+            if constexpr (f + AHEAD < NKF) fr[f % AHEAD] = read_kf(IntC<f + AHEAD>{}, k);
+            seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
+                constexpr int b = decltype(bc)::value;
+                sc[b][kb] = mfma(x, qf[b][ks], ks == 0 ? f32x4{} : sc[b][kb]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // O^T += V^T P^T of a tile, its first AHEAD fragments in fr, reading the
+    // first fragments of the next K tile
+    auto pv = [&](int v, int kn) __attribute__((always_inline)) {
+        seq<0, NVF>([&](auto fc) __attribute__((always_inline)) {
+            constexpr int f = decltype(fc)::value, j = f / DB, d = f % DB;
+            const bf16x8 x = fr[f % AHEAD];
+            if constexpr (f + AHEAD < NVF) fr[f % AHEAD] = read_vf(IntC<f + AHEAD>{}, v);
+            else fr[f % AHEAD] = read_kf(IntC<f + AHEAD - NVF>{}, kn);
+            seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
+                constexpr int b = decltype(bc)::value;
+                o[b][d] = mfma(x, pf[j][b], o[b][d]);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    auto key_of = [&](int it) { return (kt0 + 2 * it + sp) * BN; };
+    auto live = [&](int it) { return it < n_loc && key_of(it) <= most; };
+    auto mask = [&](int it) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int key = key_of(it) + 16 * kb;
+            const bool there = held(key);
+#pragma unroll
+            for (int b = 0; b < QB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (!there || key + 4 * g + r > vis[b]) sc[b][kb][r] = -__builtin_inff();
+        }
+    };
+    // moves the running maximum where a score is past the limit (see STALE)
+    auto maximum = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
+            if (__builtin_amdgcn_ballot_w64(top * SCALE_LOG2 > m[b] + STALE) != 0) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(m[b], top * SCALE_LOG2);
+                // (all -inf so far: nothing to rescale)
+                const float by = m[b] == now ? 1.f : pow2(m[b] - now);
+                l[b] *= by;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[b][d] *= by;
+                m[b] = now;
+            }
+        }
+    };
+    auto masked = [&](int it) { return key_of(it) + BN - 1 > least || gaps; };
+    // A tile that some row does not see whole is looked through for values that
+    // are not finite: 0 times each of them.  Where there are any, the piece is
+    // done again (see below): a second way through the turns would leave too few
+    // registers for the first.
+    bool far_seen = false;
+    auto far_values = [&](int v) __attribute__((always_inline)) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        seq<0, NVF>([&](auto f) __attribute__((always_inline)) { x = mfma(read_vf(f, v), bf16x8{}, x); });
+        const float y = (x[0] + x[1]) + (x[2] + x[3]);
+        return __builtin_amdgcn_ballot_w64(y != y) != 0;
+    };
+    // The softmax turn of tile `it` after its row maximum, in KB x QB groups of
+    // exponentials with a share of the loads in each; a turn that loads the
+    // sequence's last, partial tile issues its loads first
+    auto exps = [&](int it, auto act) __attribute__((always_inline)) {
+        const From kn = rows_of(it + 2), vn = next;
+        next = kn;
+        const u32 lk = slot(0, it & 1), lv = slot(1, (it + 1) & 1);
+        auto groups = [&](auto loads) __attribute__((always_inline)) {
+            seq<0, KB * QB>([&](auto gc) __attribute__((always_inline)) {
+                constexpr int n = decltype(gc)::value, kb = n / QB, b = n % QB;
+                constexpr int d0 = n * 2 * WL / (KB * QB), d1 = (n + 1) * 2 * WL / (KB * QB);
+                if constexpr (decltype(loads)::value && d0 < WL && d1 > d0)
+                    load(a.K, k_src, kn, lk, d0, d1 < WL ? d1 : WL, IntC<0>{});
+                if constexpr (decltype(loads)::value && d1 > WL)
+                    load(a.V, v_src, vn, lv, d0 > WL ? d0 - WL : 0, d1 - WL, IntC<0>{});
+                if constexpr (decltype(act)::value) {
+                    float p[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[r] = pow2(__builtin_fmaf(sc[b][kb][r], SCALE_LOG2, -least_finite(m[b])));
+                    l[b] += (p[0] + p[1]) + (p[2] + p[3]);
+                    u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
+                    w[2 * (kb % 2)] = pack2(p[0], p[1]);
+                    w[2 * (kb % 2) + 1] = pack2(p[2], p[3]);
+                    pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        if (min(kn.end, vn.end) < BNW - 1) {
+            load_whole(a.K, k_src, kn, lk);
+            load_whole(a.V, v_src, vn, lv);
+            groups(IntC<0>{});
+        } else {
+            groups(IntC<1>{});
+        }
+    };
+    auto turn_end = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0): this wave's reads of shared memory are done
+        asm volatile("s_barrier" ::: "memory");
+    };
+    if (sp == 1) turn_end();
+    if (live(0)) {
+        seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_kf(f, k0); });
+        qk(k0);
+    }
+    turn_end();
+#pragma nounroll
+    for (int it = 0; it < n_it; ++it) {
+        const int at = (it & 1) * TILE, to = ((it + 1) & 1) * TILE;
+        const bool act = live(it), some = act && masked(it);
+        if (act) {
+            if (some) mask(it);
+            maximum();
+            exps(it, IntC<1>{});
+        } else {
+            exps(it, IntC<0>{});
+        }
+        WAIT_VM(2 * WL);           // the loads of the softmax turn before this one have landed
+        turn_end();
+        // matrix turn: its waves go first at the issue port
+        __builtin_amdgcn_s_setprio(2);
+        if (act) {
+            if (some && !far_seen) far_seen = far_values(v0 + at);
+            seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_vf(f, v0 + at); });
+            pv(v0 + at, k0 + to);
+            if (live(it + 1)) qk(k0 + to);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        turn_end();
+    }
+    WAIT_VM(0);
+    if (sp == 0) turn_end();
+    if (far_seen) again = 1;
+    __syncthreads();           // every wave is done with the ring (used again below)
+    if (again) {
+        // a tile after the other, with care for the values
+        clear();
+        for (int it = 0; it < n_it; ++it) {
+            const From f = rows_of(it);
+            load_whole(a.K, k_src, f, slot(0, 0));
+            load_whole(a.V, v_src, f, slot(1, 0));
+            WAIT_VM(0);
+            __syncthreads();
+            if (live(it)) {
+                seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_kf(f, k0); });
+                qk(k0);
+                if (masked(it)) mask(it);
+                maximum();
+#pragma unroll
+                for (int kb = 0; kb < KB; kb += 2)
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) {
+                        const bf16x8 see = seen(sc[b][kb], sc[b][kb + 1]);
+                        u32x4 w;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            float p[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) l[b] += p[r] = pow2(__builtin_fmaf(sc[b][kb + c][r], SCALE_LOG2, -least_finite(m[b])));
+                            w[2 * c] = pack2(p[0], p[1]);
+                            w[2 * c + 1] = pack2(p[2], p[3]);
+                        }
+#pragma unroll
+                        for (int d = 0; d < DB; ++d) {
+                            o[b][d] = add_far(__builtin_bit_cast(u32x4, read_v(v0, d, kb / 2)), __builtin_bit_cast(bf16x8, w), see, o[b][d]);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+    }
+
+    // the two halves' states
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+    }
+    float *const other = (float *)ring[0] + rg * (QB * (32 + DB * 256));
+    if (sp == 1) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            if (g == 0) other[b * 32 + i] = m[b], other[b * 32 + 16 + i] = l[b];
+#pragma unroll
+            for (int d = 0; d < DB; ++d) *(f32x4 *)(other + QB * 32 + ((b * DB + d) * 64 + lane) * 4) = o[b][d];
+        }
+    }
+    __syncthreads();
+    if (sp == 1) return;
+    float *state = a.P + (SPLIT ? (size_t)item.slot * STATE : 0);
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const float mo = other[b * 32 + i], lo = other[b * 32 + 16 + i], top = fmaxf(m[b], mo);
+        const float by = m[b] == top ? 1.f : pow2(m[b] - top), byo = mo == top ? 1.f : pow2(mo - top);
+        const float sum = l[b] * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int row = r0w + 16 * b + i, r = row - r0;
+        if (row >= rows) continue;
+        if (SPLIT && item.pieces > 1 && g == 0) state[r] = top, state[BM + r] = sum;
+        bf16_t *p = a.O + ((size_t)(s.q0 + row / a.G) * a.HKV * a.G + item.h * a.G + row % a.G) * HD;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const f32x4 x = o[b][d] * by + *(const f32x4 *)(other + QB * 32 + ((b * DB + d) * 64 + lane) * 4) * byo;
+            if (SPLIT && item.pieces > 1) *(f32x4 *)(state + 2 * BM + r * HD + 16 * d + 4 * g) = x;
+            else *(u32x2 *)(p + 16 * d + 4 * g) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
+        }
+    }
+}
+#endif
 
 // ---------------------------------------------------------------------------
 // Rows of sequences that were cut: a wave takes a row.

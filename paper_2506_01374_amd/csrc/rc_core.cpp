@@ -164,7 +164,9 @@ static std::vector<KnobDef> attention_seqs_knobs() {
     return {
         {"block_m", "TileSize", {16, 32, 64, 128}, 16},       // rows (tokens x heads of a K/V head) of an item
         {"waves", "Parallel", {1, 2, 4, 8}, 1},               // waves of a workgroup
-        {"stages", "ComputeLocation", {1, 2}, 1},             // a tile after the other / the next one's loads under way
+        // a tile after the other / the next one's loads under way / a ring in LDS, in turns
+        {"stages", "ComputeLocation", {1, 2, 3}, 1},
+        {"occ", "Parallel", {1, 2, 4}, 1},                    // waves per SIMD to budget registers for
         // workgroups a CU for which the keys are cut into pieces (0: they are not)
         {"splits", "Parallel", {0, 1, 2, 4}, 0},
     };
@@ -627,11 +629,23 @@ static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *
     const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
     if (redundant_tile(d, "block_m", bm, q.T * (q.H / q.Hkv)))
         return fmt("block_m %d: block_m %d already covers all rows of a K/V head", bm, bm / 2);
+    if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
+    if (kv(d, s, "stages") == 3) {
+        if (w != 8 || kv(d, s, "occ") != 2) return "the ring in turns (stages 3) takes 8 waves, two a SIMD (occ 2)";
+        if (d->flags & RC_FLAG_I8_CACHE) return "the ring in turns (stages 3) moves bf16";
+        if (bm != 64 && !(bm == 128 && q.D < 256)) return fmt("the ring in turns (stages 3) takes blocks of 64 rows, or 128 with D < 256 (%d, %lld)", bm, (long long)q.D);
+        return "";
+    }
     const int64_t lds = (int64_t)w * bm * (q.D + 6) * 4;
     if (lds > LDS_LIMIT) return fmt("the states of %d waves take %lld B of LDS, more than %lld", w, (long long)lds, (long long)LDS_LIMIT);
-    const int64_t regs = bm * q.D / 64 + bm / 4 * q.D / 32;
-    if (regs > 160) return fmt("%lld registers per lane for O and Q exceed 160", (long long)regs);
-    if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
+    // registers of a lane: Q, the tiles (with int8 also their scales) and what a
+    // tile's scores take; O, which may be in accumulation registers where a SIMD
+    // has one wave
+    const int occ = kv(d, s, "occ"), tiles = kv(d, s, "stages");
+    const int64_t tile = (d->flags & RC_FLAG_I8_CACHE) ? q.D / 4 + 16 : q.D / 2;
+    const int64_t regs = bm / 4 * q.D / 32 + tiles * tile + 70 + 20 * (bm / 16), o = bm * q.D / 64;
+    if (occ == 1 ? regs > 256 || o > 192 : regs + o > 512 / occ)
+        return fmt("%lld registers per lane and %lld for O are too many at %d waves/SIMD", (long long)regs, (long long)o, occ);
     return "";
 }
 
@@ -1052,8 +1066,21 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
-    (void)q;
-    set_knob(d, s, "waves", 4);
+    const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
+    auto set = [&](int bm, int waves, int stages, int occ, int splits) {
+        set_knob(d, s, "block_m", bm), set_knob(d, s, "waves", waves), set_knob(d, s, "stages", stages);
+        set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
+        return check_schedule(d, s).empty();
+    };
+    const bool i8 = d->flags & RC_FLAG_I8_CACHE;
+    if (!i8 && rows > 32 * q.B && rows > 256) {
+        const int bm = q.D == 256 ? 64 : 128, splits = seqs_items(d, bm, 0) < 512 ? 1 : 0;
+        if (set(bm, 8, 3, 2, splits)) return;
+    }
+    for (int sp : {2, 0})
+        for (int occ : {2, 1})
+            if (set(16, 4, 1, occ, sp)) return;
+    set(16, 1, 1, 1, 0);
 }
 
 typedef std::vector<std::pair<rc_op_desc, rc_schedule>> Suggestions;
@@ -1142,7 +1169,7 @@ static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
     const bool cache = kind->kind == RC_OP_KV_WRITE || kind->kind == RC_OP_KV_READ;
     for (int64_t D : {64, 128, 256}) {         // (a definition of the kernels)
         Suggestions once;
-        for (int64_t T : {1, 2, 3, 5, 1 << 20}) {
+        for (int64_t T : {1, 2, 3, 5, 300, 1 << 20}) {
             rc_op_desc d = *kind;
             const int64_t dims[8] = {T, 1, 1, cache ? D : 1, cache ? 16 : d.kind == RC_OP_ATTENTION_PAGED ? D : 1,
                                      cache || d.kind == RC_OP_ATTENTION_PAGED ? 16 : D, 1 << 16, 1 << 16};

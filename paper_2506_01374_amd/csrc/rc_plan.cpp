@@ -978,7 +978,7 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             snprintf(scale, sizeof scale, "#define SCALE_LOG2 %.17gf\n", 1.4426950408889634 / std::sqrt((double)q.D));
             Kern k;
             k.src = Source{SRC_attention_seqs, "rc_attention_seqs",
-                           def("BM", bm) + def("NW", w) + def("STAGES", kv(d, s, "stages")) + def("SPLIT", sp > 0) + def("HD", q.D) + def("PAGED", paged) +
+                           def("BM", bm) + def("NW", w) + def("STAGES", kv(d, s, "stages")) + def("OCC", kv(d, s, "occ")) + def("SPLIT", sp > 0) + def("HD", q.D) + def("PAGED", paged) +
                                def("I8", i8) + def("LEAST", 2 * w) + scale};
             k.grid = dim3((unsigned)seqs_items(d, bm, sp), 1, 1);
             k.block = dim3(64 * w, 1, 1);

@@ -19,16 +19,18 @@ PAGED_CASES = [
     ([1], [1], 1, 1, 64, 16), ([1], [40], 1, 4, 128, 16), ([1, 1, 1, 1], [1, 31, 32, 33], 2, 4, 128, 16),
     ([1, 0, 1], [500, 77, 0], 2, 7, 64, 32), ([5, 3, 1], [5, 300, 64], 1, 5, 128, 64), ([17], [17], 2, 3, 64, 16),
     ([1, 16, 2], [700, 16, 129], 1, 8, 256, 32), ([70, 1], [70, 333], 2, 4, 128, 128), ([3, 4], [2, 300], 1, 16, 64, 256),
-    ([130], [1000], 1, 4, 128, 16), ([1] * 70, [1 + 13 * i % 200 for i in range(70)], 1, 2, 64, 16), ([9], [4], 1, 1, 256, 16)]
+    ([130], [1000], 1, 4, 128, 16), ([40, 3], [1500, 900], 2, 4, 128, 16), ([33, 64], [64, 640], 2, 2, 64, 32), ([70], [400], 1, 3, 256, 64), ([1] * 70, [1 + 13 * i % 200 for i in range(70)], 1, 2, 64, 16), ([9], [4], 1, 1, 256, 16)]
 
 # (rows of Q of each sequence, of K, K/V heads, query heads for each, head dimension)
 PACKED_CASES = [
     ([1], [1], 1, 1, 64), ([1, 37, 200], [1, 37, 200], 2, 4, 128), ([33, 0, 5], [33, 0, 5], 1, 3, 256),
     ([16, 32, 64], [16, 32, 64], 2, 1, 64), ([10, 1, 7], [100, 64, 3], 1, 8, 128), ([300], [300], 1, 4, 128),
-    ([0, 2, 129], [5, 2, 129], 1, 5, 64), ([65], [257], 2, 2, 256)]
+    ([0, 2, 129], [5, 2, 129], 1, 5, 64), ([65], [257], 2, 2, 256), ([700, 3, 129], [700, 3, 129], 2, 4, 128), ([257], [600], 3, 1, 64)]
 
 CACHE_TEXTS = ["", "vec=8", "waves=4,vec=8"]
-ATTENTION_TEXTS = ["", "block_m=32", "waves=4", "block_m=32,waves=2,splits=1", "waves=4,splits=2"]
+ATTENTION_TEXTS = ["", "block_m=32", "waves=4", "block_m=32,waves=2,splits=1", "waves=4,splits=2",
+                   "block_m=64,waves=8,stages=3,occ=2", "block_m=128,waves=8,stages=3,occ=2,splits=1", "block_m=64,waves=8,stages=3,occ=2,splits=4",
+                   "stages=2,waves=2,occ=1,splits=1", "stages=1,waves=4,occ=2,splits=2"]
 
 
 def cache_op(kind, case, flags, pages=None):

@@ -78,8 +78,8 @@ def test_legality():
     assert "already covers" in op.schedule(block_m=32).validate()
     op = rc.Op(PG, (100, 1, 16, 1, 128, 16, 9, 5))
     assert op.schedule(block_m=32).validate() == ""
-    assert "LDS" in op.schedule(block_m=64, waves=8).validate()
-    assert "registers" in rc.Op(PG, (100, 1, 16, 1, 256, 16, 9, 5)).schedule(block_m=64).validate()
+    assert "LDS" in rc.Op(PG, (100, 1, 16, 1, 64, 16, 9, 5)).schedule(block_m=128, waves=8).validate()
+    assert "registers" in rc.Op(PG, (100, 1, 16, 1, 256, 16, 9, 5)).schedule(block_m=32).validate()
     huge = rc.Op(PG, (2 ** 26 - 64, 1, 16, 16, 64, 16, 9, 5))
     assert huge.default().validate() == "" and "2^32 - 1 threads" in huge.schedule(waves=2).validate()
     assert "already cover" in rc.Op(W, (1, 1, 1, 64, 16, 9, 5)).schedule(waves=2).validate()
