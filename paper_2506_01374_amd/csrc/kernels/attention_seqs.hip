@@ -64,6 +64,7 @@ struct SeqsArgs {
     bf16_t *O;
     float *P;                      // states of pieces (SPLIT)
     int T, TK, B, G, HKV, shift, pages, width, causal, slots;
+    int share;                     // the join: four waves a row
 };
 
 __device__ __forceinline__ int limit(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -106,66 +107,74 @@ struct Item {
     int h, block, piece, pieces, slot;
 };
 
+// x + that of all lanes before, by moves between lanes without shared memory
+__device__ __forceinline__ int scan(int x) {
+#define FROM(how, rows) x += __builtin_amdgcn_update_dpp(0, x, how, rows, 0xF, false)
+    FROM(0x111, 0xF);              // within rows of 16: 1, 2, 4, 8 lanes to the right
+    FROM(0x112, 0xF);
+    FROM(0x114, 0xF);
+    FROM(0x118, 0xF);
+    FROM(0x142, 0xA);              // the last lane of rows 0 and 2 to the next row
+    FROM(0x143, 0xC);              // lane 31 to the two rows behind it
+#undef FROM
+    return x;
+}
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
 // A sequence's rows are cut into blocks of BM, and with SPLIT its keys into
 // pieces of at most `most` tiles, the same number for each block.  `most` is
 // the work of all sequences over the workgroups that it is cut for (a.slots), so
 // that pieces of blocks that are cut are at most 2 a.slots: each takes more than
-// half of it.  Item j is piece by piece, the sequence's last block (the one that
-// sees most keys) first, head by head; JOIN: block by block of what is cut.
+// half of it.  The pieces' states are in this order too: sequence by sequence,
+// its last block (the one that sees most keys) first, piece by piece, head by
+// head.  Item `index` of that order, or (JOIN) the first piece's of what row
+// `index` of Q is in.
 template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int index, Item &item) {
     const int lane = threadIdx.x & 63;
-    item.h = index % a.HKV;
-    int j = index / a.HKV;
+    item.h = JOIN ? 0 : index % a.HKV;
+    int j = JOIN ? index : index / a.HKV;
     int most = 1 << 30;
+    Seq first = {};                // of the first 64 sequences
+    if (lane < a.B) first = sequence(a, lane);
 #if SPLIT
     unsigned long long work = 0;
     for (int c = 0; c < a.B; c += 64) {
-        unsigned long long w = 0;
-        if (c + lane < a.B) {
-            const Seq s = sequence(a, c + lane);
-            w = (unsigned long long)blocks_of(a, s) * tiles_of(s);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) w += __shfl_xor(w, d);
-        work += w;
+        const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
+        // (all of it is below 2^51, 24 bits at a time)
+        const unsigned long long w = c + lane < a.B ? (unsigned long long)blocks_of(a, s) * tiles_of(s) : 0;
+        work += (u32)from_lane(scan((int)(w & 0xFFFFFF)), 63) + ((unsigned long long)(u32)from_lane(scan((int)(w >> 24)), 63) << 24);
     }
     work = (work * a.HKV + a.slots - 1) / a.slots;
     most = work < LEAST ? LEAST : work > (1 << 30) ? 1 << 30 : (int)work;
 #endif
     int slot = 0;
     for (int c = 0; c < a.B; c += 64) {
-        Seq s = {};
-        int blocks = 0, pieces = 1;
-        if (c + lane < a.B) {
-            s = sequence(a, c + lane);
-            blocks = blocks_of(a, s);
-            if (SPLIT) pieces = max(1, (tiles_of(s) + most - 1) / most);
-        }
+        const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
+        const int blocks = c + lane < a.B ? blocks_of(a, s) : 0, pieces = SPLIT ? max(1, (tiles_of(s) + most - 1) / most) : 1;
         const int cut = pieces > 1 ? blocks * pieces : 0;      // states that the sequence leaves
-        const int items = JOIN ? (pieces > 1 ? blocks : 0) : blocks * pieces;
-        int sum = items, sums = cut;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(sum, d), y = __shfl_up(sums, d);
-            if (lane >= d) sum += x, sums += y;
-        }
-        const unsigned long long past = __builtin_amdgcn_ballot_w64(sum > j);
+        const int items = blocks * pieces, sum = JOIN ? 0 : scan(items), sums = SPLIT ? scan(cut) : 0;
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(JOIN ? blocks > 0 && s.q0 <= j && j < s.q0 + s.n : sum > j);
         if (past) {
             const int at = __builtin_ctzll(past);
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-            item.s.q0 = of(s.q0), item.s.n = of(s.n), item.s.k0 = of(s.k0), item.s.len = of(s.len), item.s.keys = of(s.keys);
-            const int i = j - of(sum - items), k = of(blocks);
-            item.pieces = of(pieces);
-            const int order = JOIN ? i : i / item.pieces;
-            item.block = k - 1 - order;
-            item.piece = JOIN ? 0 : i % item.pieces;
-            item.slot = ((slot + of(sums - cut)) + order * item.pieces + item.piece) * a.HKV + item.h;
-            // (for readlane's sake: which sequence, to find its row of the table)
-            item.s.k0 = PAGED ? c + at : item.s.k0;
+            item.s.q0 = from_lane(s.q0, at), item.s.n = from_lane(s.n, at), item.s.len = from_lane(s.len, at);
+            item.s.keys = from_lane(s.keys, at);
+            // (PAGED: which sequence, to find its row of the table)
+            item.s.k0 = PAGED ? c + at : from_lane(s.k0, at);
+            item.pieces = from_lane(pieces, at);
+            slot += from_lane(sums - cut, at);
+            if (JOIN) {
+                item.slot = slot;
+                item.block = from_lane(blocks, at);            // how many there are
+                return true;
+            }
+            const int i = j - from_lane(sum - items, at), order = i / item.pieces;
+            item.block = from_lane(blocks, at) - 1 - order;
+            item.piece = i % item.pieces;
+            item.slot = (slot + i) * a.HKV + item.h;
             return true;
         }
-        j -= __builtin_amdgcn_readlane(sum, 63);
-        slot += __builtin_amdgcn_readlane(sums, 63);
+        if (!JOIN) j -= from_lane(sum, 63);
+        slot += from_lane(sums, 63);
     }
     return false;
 }
@@ -977,35 +986,63 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
 #endif
 
 // ---------------------------------------------------------------------------
-// Rows of sequences that were cut: a wave takes a row.
+// Rows of sequences that were cut: a wave takes a row, or a workgroup (`share`)
 // ---------------------------------------------------------------------------
+//
+// A lane takes 4 channels of every 256 / HD-th piece (of every 1024 / HD-th with
+// four waves a row), eight pieces at once: the time is that of the way to memory
+// and back.
 #if SPLIT
 extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long at = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ f32x4 po[4][HD / 4];
+    __shared__ float pm[4], pl[4];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.HKV * a.G;
+    const long long at = a.share ? blockIdx.x : (long long)blockIdx.x * 4 + w;
+    if (at >= (long long)a.T * H) return;
+    const int token = (int)(at / H), head = (int)(at % H);
     Item item;
-    if (!find<true>(a, (int)(at / BM), item)) return;
-    const int r = (int)(at % BM), row = item.block * BM + r;
-    if (row >= item.s.n * a.G) return;
-    const float *state = a.P + (size_t)item.slot * STATE;
+    if (!find<true>(a, token, item) || item.pieces == 1) return;
+    const int row = (token - item.s.q0) * a.G + head % a.G, r = row % BM;
+    const float *state = a.P + ((size_t)(item.slot + (item.block - 1 - row / BM) * item.pieces) * a.HKV + head / a.G) * STATE;
     const size_t next = (size_t)a.HKV * STATE;          // of the block's next piece
-    float top = -__builtin_inff();
-    for (int p = lane; p < item.pieces; p += 64) top = fmaxf(top, state[p * next + r]);
+    constexpr int LANES = HD / 4, PAR = 64 / LANES;
+    const int part = lane / LANES, d = lane % LANES * 4;
+    const int step = a.share ? 4 * PAR : PAR;
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float mp, float lp, const f32x4 &op) {
+        const float top = fmaxf(m, mp), x = m == top ? 1.f : pow2(m - top), y = mp == top ? 1.f : pow2(mp - top);
+        l = l * x + lp * y;
+        o = o * x + op * y;
+        m = top;
+    };
+    for (int p0 = a.share ? w * PAR + part : part; p0 - part < item.pieces; p0 += 8 * step) {
+        float mp[8], lp[8];
+        f32x4 op[8];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    constexpr int PER = HD / 64;
-    float sum = 0.f, out[PER] = {};
-#pragma unroll 8
-    for (int p = 0; p < item.pieces; ++p) {
-        const float *x = state + p * next;
-        const float by = x[r] == top ? 1.f : pow2(x[r] - top);
-        sum += x[BM + r] * by;
+        for (int i = 0; i < 8; ++i) {
+            const float *x = state + (size_t)min(p0 + i * step, item.pieces - 1) * next;
+            mp[i] = x[r], lp[i] = x[BM + r];
+            op[i] = *(const f32x4 *)(x + 2 * BM + r * HD + d);
+        }
 #pragma unroll
-        for (int e = 0; e < PER; ++e) out[e] += x[2 * BM + r * HD + lane * PER + e] * by;
+        for (int i = 0; i < 8; ++i)
+            if (p0 + i * step < item.pieces) add(mp[i], lp[i], op[i]);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    bf16_t *o = a.O + ((size_t)(item.s.q0 + row / a.G) * a.HKV * a.G + item.h * a.G + row % a.G) * HD + lane * PER;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = __builtin_bit_cast(bf16_t, (__bf16)(out[e] * inv));
+    for (int x = LANES; x < 64; x <<= 1) {
+        const f32x4 other = {__shfl_xor(o[0], x), __shfl_xor(o[1], x), __shfl_xor(o[2], x), __shfl_xor(o[3], x)};
+        add(__shfl_xor(m, x), __shfl_xor(l, x), other);
+    }
+    if (a.share) {
+        if (part == 0) po[w][d / 4] = o;
+        if (lane == 0) pm[w] = m, pl[w] = l;
+        __syncthreads();
+        if (w) return;
+#pragma unroll
+        for (int x = 1; x < 4; ++x) add(pm[x], pl[x], po[x][d / 4]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (part == 0) *(u32x2 *)(a.O + (size_t)at * HD + d) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
 }
 #endif

@@ -35,11 +35,17 @@ struct CacheArgs {
     int T, B, HKV, shift, pages, width;
 };
 
-struct Vec { u32 w[WORDS]; };
-struct Bytes { u32 w[VEC / 4]; };
+typedef u32 Vec __attribute__((ext_vector_type(WORDS)));
+#if VEC == 8
+typedef u32 Bytes __attribute__((ext_vector_type(2)));
+#define WORD(q, i) q[i]
+#else
+typedef u32 Bytes;
+#define WORD(q, i) q
+#endif
 
 __device__ __forceinline__ float element(const Vec &x, int j) {
-    return __builtin_bit_cast(float, j % 2 ? x.w[j / 2] & 0xFFFF0000u : x.w[j / 2] << 16);
+    return __builtin_bit_cast(float, j % 2 ? x[j / 2] & 0xFFFF0000u : x[j / 2] << 16);
 }
 
 // (row of the cache's slots, or -1 if the token has none; whether the row is a
@@ -77,57 +83,98 @@ __device__ __forceinline__ Place place(const CacheArgs &a, int row) {
     return p;
 }
 
+// Integers near s / a, |s| <= 127 a, as SHIFT + t: the last bit of a float there
+// is 1, so that the addition rounds to an integer, which the low bits then are.
+#define SHIFT 12582912.f           // 1.5 * 2^23
+
+// VEC of a head's elements x, the head's largest magnitude `as` after the factor
+// `up`, as integers.  Trials of all, within one of the result, whose remainders s
+// - t a are exact (127 x has 15 bits, a 8); again where one of them is not the
+// nearest, or at a half and odd: an odd trial's last bit makes a remainder of a
+// half larger (a / 2 has 8 bits, their last one is 0), and no smaller one as large.
+__device__ __forceinline__ Bytes quantise(const Vec &x, float as, float up) {
+    // above 1 / a by its last bits: the trial of a / 2, the one tie that is met
+    // often, is 64 then, the even neighbour of 63.5
+    const float inv = __builtin_amdgcn_rcpf(as) * 0x1.000004p0f;
+    u32 t[VEC];
+    float far = 0.f;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        const float s = element(x, j) * (127.f * up), n = __builtin_fmaf(s, inv, SHIFT);
+        t[j] = __builtin_bit_cast(u32, n);
+        const float rem = __builtin_fmaf(-(n - SHIFT), as, s);
+        far = fmaxf(far, __builtin_fabsf(__builtin_bit_cast(float, __builtin_bit_cast(u32, rem) | (t[j] & 1))));
+    }
+    if (far > 0.5f * as) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float s = element(x, j) * (127.f * up), n = __builtin_bit_cast(float, t[j]);
+            const float rem = __builtin_fmaf(-(n - SHIFT), as, s), r = __builtin_fabsf(rem);
+            if (r > 0.5f * as || (r == 0.5f * as && (t[j] & 1))) t[j] += rem > 0.f ? 1 : -1;
+        }
+    }
+    Bytes q;
+#pragma unroll
+    for (int i = 0; i < VEC / 4; ++i) {
+        const u32 lo = __builtin_amdgcn_perm(t[4 * i + 1], t[4 * i], 0x0C0C0400u);
+        const u32 hi = __builtin_amdgcn_perm(t[4 * i + 3], t[4 * i + 2], 0x0C0C0400u);
+        WORD(q, i) = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+    }
+    return q;
+}
+
+// K's chunks of VEC elements, then V's; four of a lane at once
+#define AT_ONCE 4
+
 extern "C" __global__ __launch_bounds__(64 * WAVES) void rc_kv_write(CacheArgs a) {
     const int lane = threadIdx.x & 63, row = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.T) return;
-    const int chunks = a.HKV * LANES;                  // of K's row, then of V's
+    const int chunks = a.HKV * LANES;
     const bf16_t *k = a.k + (size_t)row * a.HKV * HD, *v = a.v + (size_t)row * a.HKV * HD;
-    auto fetch = [&](int c) {
-        Vec x = {};
-        const bool isv = c >= chunks;
-        if (c < 2 * chunks) __builtin_memcpy(&x, (isv ? v : k) + (size_t)(isv ? c - chunks : c) * VEC, sizeof x);
-        return x;
+    Vec x[AT_ONCE];
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int c = from + 64 * j;
+            x[j] = Vec{};
+            if (c < 2 * chunks) x[j] = *(const Vec *)((c >= chunks ? v - (size_t)chunks * VEC : k) + (size_t)c * VEC);
+        }
     };
-    Vec x = fetch(lane);                               // on its way while the place is found
+    fetch(lane);                                       // on their way while the place is found
     const Place p = place(a, row);
     if (p.slot < 0) return;
-    for (int c = lane; c - lane < 2 * chunks; c += 64) {
-        const Vec next = fetch(c + 64);
-        const bool isv = c >= chunks, live = c < 2 * chunks;
-        const int cc = isv ? c - chunks : c, h = cc / LANES, d = cc % LANES * VEC;
-        const long long slot = p.slot + ((long long)h << a.shift);
+    for (int from = lane;;) {
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int c = from + 64 * j;
+            const bool isv = c >= chunks, live = c < 2 * chunks;
+            const int cc = isv ? c - chunks : c, h = cc / LANES, d = cc % LANES * VEC;
+            const long long slot = p.slot + ((long long)h << a.shift);
 #if I8
-        // magnitudes as bits: above all others a NaN
-        u32 top = 0;
+            // magnitudes as bits: above all others a NaN
+            u32 bits = 0;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) top = max(top, __builtin_bit_cast(u32, element(x, j)) & 0x7FFFFFFFu);
+            for (int e = 0; e < WORDS; ++e) bits = max(bits, max(x[j][e] & 0x7FFF0000u, x[j][e] << 16 & 0x7FFF0000u));
 #pragma unroll
-        for (int s = 1; s < LANES; s <<= 1) top = max(top, (u32)__shfl_xor((int)top, s));
-        const float most = __builtin_bit_cast(float, top);
-        const bool bad = !(most < __builtin_inff());
-        // near 1 by a power of two, exactly, so that 127 x and its remainders
-        // stay in fp32's range
-        const float up = most < 0x1p-63f ? 0x1p64f : most >= 0x1p64f ? 0x1p-64f : 1.f;
-        const float as = bad || most == 0.f ? 1.f : most * up, inv = 1.f / as;
-        Bytes q = {};
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            // s - t a is exact (127 x has 15 bits, a 8), and t within one of the result
-            const float s = element(x, j) * (127.f * up);
-            const float t = __builtin_rintf(s * inv), rem = __builtin_fmaf(-t, as, s), r = __builtin_fabsf(rem);
-            const int n = (int)t;
-            const bool move = r > 0.5f * as || (r == 0.5f * as && (n & 1));
-            const int e = bad ? 0 : move ? n + (rem > 0.f ? 1 : -1) : n;
-            q.w[j / 4] |= (u32)(e & 255) << (8 * (j % 4));
-        }
-        if (live) {
-            __builtin_memcpy((isv ? a.V : a.K) + slot * HD + d, &q, sizeof q);
-            if (d == 0) (isv ? a.Vs : a.Ks)[slot] = bad ? __builtin_nanf("") : most / 127.f;
-        }
+            for (int s = 1; s < LANES; s <<= 1) bits = max(bits, (u32)__shfl_xor((int)bits, s));
+            const float top = __builtin_bit_cast(float, bits);
+            const bool bad = !(top < __builtin_inff());
+            // brought near 1 by a power of two, exactly, so that 127 x and its
+            // remainders stay in fp32's range
+            const float up = top < 0x1p-63f ? 0x1p64f : top >= 0x1p64f ? 0x1p-64f : 1.f;
+            Bytes q = quantise(x[j], bad || top == 0.f ? 1.f : top * up, up);
+            if (bad) q = Bytes{};
+            if (live) {
+                *(Bytes *)((isv ? a.V : a.K) + slot * HD + d) = q;
+                if (d == 0) (isv ? a.Vs : a.Ks)[slot] = bad ? __builtin_nanf("") : top / 127.f;
+            }
 #else
-        if (live) __builtin_memcpy((isv ? a.V : a.K) + (slot * HD + d) * 2, &x, sizeof x);
+            if (live) *(Vec *)((isv ? a.V : a.K) + (slot * HD + d) * 2) = x[j];
 #endif
-        x = next;
+        }
+        from += 64 * AT_ONCE;
+        if (from - lane >= 2 * chunks) break;
+        fetch(from);
     }
 }
 
@@ -138,25 +185,43 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void rc_kv_read(CacheArgs a)
     bf16_t *k = a.k + (size_t)row * a.HKV * HD, *v = a.v + (size_t)row * a.HKV * HD;
     const Place p = place(a, row);
     if (!p.row) return;
-    for (int c = lane; c < 2 * chunks; c += 64) {
-        const bool isv = c >= chunks;
-        const int cc = isv ? c - chunks : c, h = cc / LANES, d = cc % LANES * VEC;
-        const long long slot = p.slot + ((long long)h << a.shift);
-        Vec x = {};
-        if (p.slot >= 0) {
+    const long long slot0 = p.slot < 0 ? 0 : p.slot;
+    for (int from = lane; from - lane < 2 * chunks; from += 64 * AT_ONCE) {
+        Vec x[AT_ONCE];
 #if I8
-            Bytes q;
-            __builtin_memcpy(&q, (isv ? a.V : a.K) + slot * HD + d, sizeof q);
-            const float s = (isv ? a.Vs : a.Ks)[slot];
+        Bytes q[AT_ONCE];
+        float s[AT_ONCE];
+#endif
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const __bf16 y = (__bf16)((float)(signed char)(q.w[j / 4] >> (8 * (j % 4))) * s);
-                x.w[j / 2] |= (u32)__builtin_bit_cast(bf16_t, y) << (16 * (j % 2));
-            }
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int c = min(from + 64 * j, 2 * chunks - 1), isv = c >= chunks, cc = isv ? c - chunks : c;
+            const long long slot = slot0 + ((long long)(cc / LANES) << a.shift);
+            const long long at = slot * HD + cc % LANES * VEC;
+#if I8
+            q[j] = *(const Bytes *)((isv ? a.V : a.K) + at);
+            s[j] = (isv ? a.Vs : a.Ks)[slot];
 #else
-            __builtin_memcpy(&x, (isv ? a.V : a.K) + (slot * HD + d) * 2, sizeof x);
+            x[j] = *(const Vec *)((isv ? a.V : a.K) + 2 * at);
 #endif
         }
-        __builtin_memcpy((isv ? v : k) + (size_t)cc * VEC, &x, sizeof x);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int c = from + 64 * j;
+#if I8
+#pragma unroll
+            for (int e = 0; e < WORDS; ++e) {
+                u32 y = 0;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int n = 2 * e + b;
+                    const float f = (float)(signed char)(WORD(q[j], n / 4) >> (8 * (n % 4))) * s[j];
+                    y |= (u32)__builtin_bit_cast(bf16_t, (__bf16)f) << (16 * b);
+                }
+                x[j][e] = y;
+            }
+#endif
+            if (p.slot < 0) x[j] = Vec{};
+            if (c < 2 * chunks) *(Vec *)((c >= chunks ? v - (size_t)chunks * VEC : k) + (size_t)c * VEC) = x[j];
+        }
     }
 }

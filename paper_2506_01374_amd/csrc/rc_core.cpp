@@ -620,15 +620,12 @@ int64_t seqs_items(const rc_op_desc *d, int bm, int splits) {
     return q.Hkv * (q.T * (q.H / q.Hkv) / bm + std::min(q.B, q.T)) + 256 * splits;
 }
 
-int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits) {
-    return std::min<int64_t>(256 * splits, seqs_items(d, bm, 0));
-}
-
 static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
     if (redundant_tile(d, "block_m", bm, q.T * (q.H / q.Hkv)))
         return fmt("block_m %d: block_m %d already covers all rows of a K/V head", bm, bm / 2);
+    if (sp && q.T * q.H * 64 + 192 > MAX_GRID_THREADS) return "splits: the rows exceed the joining launch's grid";
     if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     if (kv(d, s, "stages") == 3) {
         if (w != 8 || kv(d, s, "occ") != 2) return "the ring in turns (stages 3) takes 8 waves, two a SIMD (occ 2)";

@@ -47,10 +47,8 @@ struct SeqDims {
 };
 SeqDims seq_dims(const rc_op_desc *d);
 int expected_dims(int32_t kind);
-// Work items that an attention over sequences has at most, and blocks of rows of
-// which it cuts the keys (at most 2 pieces a workgroup that it cuts them for).
+// Work items that an attention over sequences has at most.
 int64_t seqs_items(const rc_op_desc *d, int bm, int splits);
-int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits);
 
 // Legality with a reason; "" when legal.
 std::string check_schedule(const rc_op_desc *d, const rc_schedule *s);
