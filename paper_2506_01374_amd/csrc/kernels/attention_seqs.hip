@@ -68,6 +68,8 @@ struct SeqsArgs {
 };
 
 __device__ __forceinline__ int limit(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+// byte e of w as a float
+__device__ __forceinline__ float byte(u32 w, int e) { return (float)(signed char)(w >> (8 * e)); }
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---------------------------------------------------------------------------
@@ -240,8 +242,6 @@ __device__ __forceinline__ f32x4 add_far(const u32x4 &v, const bf16x8 &p, const 
 }
 
 #if STAGES < 3
-// byte e of w as a float
-__device__ __forceinline__ float byte(u32 w, int e) { return (float)(signed char)(w >> (8 * e)); }
 
 struct Tile {
     u32x4 k[2][I8 ? NKS / 2 : NKS];
@@ -557,6 +557,10 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // turn before.  16-byte chunks of a row are XOR-ed with the row's number (KSWZ,
 // VSWZ), by the choice of what a lane fetches, so that fragment reads have no
 // bank conflicts; V's are transposed by the reading instruction.
+// An int8 tile goes through registers: a softmax turn widens what the one before
+// has loaded to bf16 (exactly) and writes it, K of the next tile and V of this
+// one, so that one place for each is enough.  K's scale is multiplied into the
+// scores, V's into the probabilities.
 
 #if STAGES == 3
 #define ROWG 4                     // groups of rows
@@ -571,9 +575,10 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 #define NPJ (BN / 32)              // MFMA steps of P V
 #define NKF (KB * NKS)             // fragments of K and of V
 #define NVF (NPJ * DB)
-#define AHEAD 8                    // of them read ahead of their MFMAs
+#define AHEAD (I8 ? 4 : 8)         // of them read ahead of their MFMAs (int8: the registers allow 4)
 #define WL (TILE / 512 / ROWG)     // 1 KiB loads of a wave for a tile
 #define RPI (512 / HD)             // rows of one
+#define NL (TILE / 1024 / ROWG)    // 16-byte loads of a lane for a tile of int8
 
 template <int V> struct IntC { static constexpr int value = V; };
 // seq<A, B>(f): f(IntC<A>), ... f(IntC<B - 1>), every index a constant
@@ -588,9 +593,15 @@ template <int A, int B, class F> __device__ __forceinline__ void seq(F &&f) {
 #define WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | ((((n) >> 4) & 3) << 14) | (7 << 4) | (15 << 8))
 
 extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void rc_attention_seqs(SeqsArgs a) {
+#if I8
+    // K of each half's tile, then V; the last for the halves' states
+    __shared__ __attribute__((aligned(16))) bf16_t ring[5][TILE];
+    __shared__ __attribute__((aligned(16))) float scales[2][2][2][BN];        // of each half: two tiles' Ks and Vs
+#else
     __shared__ __attribute__((aligned(16))) bf16_t ring[8][TILE];      // K of each half's two tiles, then V
     __shared__ int again;
     if (threadIdx.x == 0) again = 0;
+#endif
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane % 16, g = lane / 16, rg = wave % ROWG, sp = wave / ROWG;
     Item item;
@@ -605,6 +616,13 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     const int n_it = (n_kt + 1) / 2, n_loc = (n_kt + 1 - sp) / 2;      // turns; tiles of this half
 
     // loads: lane's byte offsets within the wave's rows of a tile
+#if I8
+    // (16 int8, two chunks in shared memory)
+    const int row = lane / (HD / 16), chunk = lane % (HD / 16), rw = rg * BNW + row;
+    // (elements of the first of them; 1024 / HD rows on the XOR-ed part changes
+    // by a constant)
+    const int k_to = sp * TILE + rw * HD + 8 * ((2 * chunk) ^ KSWZ(rw)), v_to = (2 + sp) * TILE + rw * HD + 8 * ((2 * chunk) ^ VSWZ(rw));
+#else
 #if PAGED
     constexpr u32 step = HD * 2;
 #else
@@ -626,11 +644,12 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     auto dma = [&](const char *base, u32 off, u32 lds) {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
     };
+#endif
     // Where the wave's rows of the half's tile `it` start, and the last of them
     // that is a key (past the sequence's last key: that one, which is there).
     // Past the half's last tile: that one again, which nothing reads.
     struct From {
-        size_t at;
+        size_t at;                         // bytes; of the scales elements
         int end;
     };
     const int last_key = s.keys - 1;
@@ -651,9 +670,55 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
 #else
         f.at = (size_t)(s.k0 + key) * a.HKV + item.h;
 #endif
-        f.at *= HD * 2;
+        if (!I8) f.at *= HD * 2;
         return f;
     };
+#if I8
+    // A tile on its way through registers: loaded in one softmax turn, widened
+    // to bf16 and written to shared memory in the next
+    u32x4 kx[NL], vx[NL];
+    float sx = 0.f, sy = 0.f;
+    auto fetch = [&](const char *src, const From &f, u32x4 (&x)[NL]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j) x[j] = *(const u32x4 *)(src + f.at * HD + (u32)(min(row + j * (1024 / HD), f.end) * HD + 16 * chunk));
+    };
+    auto fetch_scales = [&](const From &f) __attribute__((always_inline)) {
+        const u32 at = 4 * min(lane % BNW, f.end);
+        sx = *(const float *)((const char *)(a.Ks + f.at) + at);
+        sy = *(const float *)((const char *)(a.Vs + f.at) + at);
+    };
+    auto widen = [&](const u32x4 (&x)[NL], int to, int swz) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 y;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32 t = x[j][2 * h + e];
+                    y[2 * e] = pack2(byte(t, 0), byte(t, 1));
+                    y[2 * e + 1] = pack2(byte(t, 2), byte(t, 3));
+                }
+                *(u32x4 *)(ring[0] + ((to + 1024 * j) ^ (8 * swz * j) ^ 8 * h)) = y;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    auto put_scales = [&](int b) __attribute__((always_inline)) {
+        if (lane < 2 * BNW) scales[sp][b][lane / BNW][rg * BNW + lane % BNW] = lane < BNW ? sx : sy;
+    };
+    From next = {0, BNW};
+    if (n_kt > 0) {
+        From f = rows_of(0);
+        fetch(a.K, f, kx);
+        fetch(a.V, f, vx);
+        fetch_scales(f);
+        next = rows_of(1);
+        widen(kx, k_to, KSWZ(1024 / HD));
+        put_scales(0);
+        fetch(a.K, next, kx);
+        fetch_scales(next);
+    }
+#else
     // loads j0 .. j1 - 1 of a tile; `edge`: rows past the last key fetch that one
     auto load = [&](const char *src, const u32 (&off)[WL], const From &f, u32 lds, int j0, int j1, auto edge) __attribute__((always_inline)) {
 #pragma unroll
@@ -677,6 +742,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         load_whole(a.V, v_src, f, slot(1, 0));
         load_whole(a.K, k_src, next, slot(0, 1));
     }
+#endif
     // is a page of the piece not held?
     bool gaps = false;
 #if PAGED
@@ -739,8 +805,9 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     // Fragments, at an element of shared memory: of K at k0 + its tile's, with
     // the chunk 4 ks + g XOR-ed as above, which is an XOR of the whole index (a
     // tile starts at a multiple of HD); of V likewise
-    const int k0 = 2 * sp * TILE + i * HD + 8 * (g ^ KSWZ(i));
-    const int vr = 4 * g + i / 4, v0 = (4 + 2 * sp) * TILE + vr * HD + 8 * ((lane & 3) / 2 ^ VSWZ(vr)) + (lane & 1) * 4;
+    constexpr int SLOTS = I8 ? 1 : 2;      // of a half's operand
+    const int k0 = SLOTS * sp * TILE + i * HD + 8 * (g ^ KSWZ(i));
+    const int vr = 4 * g + i / 4, v0 = SLOTS * (2 + sp) * TILE + vr * HD + 8 * ((lane & 3) / 2 ^ VSWZ(vr)) + (lane & 1) * 4;
     auto read_kf = [&](auto fc, int k) __attribute__((always_inline)) {
         constexpr int f = decltype(fc)::value;
         return *(const bf16x8 *)(ring[0] + (k ^ 32 * (f % NKS)) + (f / NKS) * 16 * HD);
@@ -757,9 +824,12 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     };
     static_assert(NVF % AHEAD == 0 && NKF >= AHEAD, "fragment ring");
     f32x4 sc[QB][KB];
-    bf16x8 pf[NPJ][QB], fr[AHEAD];
+    // (P^T and the fragments under way are arguments: variables of the whole loop
+    // would hold their registers through both turns)
+    typedef bf16x8 Probs[NPJ][QB];
+    typedef bf16x8 Frags[AHEAD];
     // S^T of a tile: its first AHEAD fragments are in fr
-    auto qk = [&](int k) __attribute__((always_inline)) {
+    auto qk = [&](int k, Frags &fr) __attribute__((always_inline)) {
         seq<0, NKF>([&](auto fc) __attribute__((always_inline)) {
             constexpr int f = decltype(fc)::value, kb = f / NKS, ks = f % NKS;
             const bf16x8 x = fr[f % AHEAD];
@@ -773,7 +843,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     };
     // O^T += V^T P^T of a tile, its first AHEAD fragments in fr, reading the
     // first fragments of the next K tile
-    auto pv = [&](int v, int kn) __attribute__((always_inline)) {
+    auto pv = [&](int v, int kn, const Probs &pf, Frags &fr) __attribute__((always_inline)) {
         seq<0, NVF>([&](auto fc) __attribute__((always_inline)) {
             constexpr int f = decltype(fc)::value, j = f / DB, d = f % DB;
             const bf16x8 x = fr[f % AHEAD];
@@ -783,7 +853,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                 constexpr int b = decltype(bc)::value;
                 o[b][d] = mfma(x, pf[j][b], o[b][d]);
             });
-            __builtin_amdgcn_sched_barrier(0);
+            if (!I8) __builtin_amdgcn_sched_barrier(0);        // (int8: the order pinned here would spill)
         });
     };
     auto key_of = [&](int it) { return (kt0 + 2 * it + sp) * BN; };
@@ -837,7 +907,36 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     // The softmax turn of tile `it` after its row maximum, in KB x QB groups of
     // exponentials with a share of the loads in each; a turn that loads the
     // sequence's last, partial tile issues its loads first
-    auto exps = [&](int it, auto act) __attribute__((always_inline)) {
+#if I8
+    // (int8: the values' scales are multiplied in; where some row does not see a
+    // key, its scale may be anything)
+    auto scaled = [&](int it, bool some, Probs &pf) __attribute__((always_inline)) {
+        seq<0, KB>([&](auto kc) __attribute__((always_inline)) {
+            constexpr int kb = decltype(kc)::value;
+            const f32x4 vs = *(const f32x4 *)&scales[sp][it & 1][1][16 * kb + 4 * g];
+            seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
+                constexpr int b = decltype(bc)::value;
+                const float minus = -least_finite(m[b]);
+                float p[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] = pow2(__builtin_fmaf(sc[b][kb][r], SCALE_LOG2, minus));
+                l[b] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] *= vs[r];
+                if (some) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[r] = sc[b][kb][r] == -__builtin_inff() ? 0.f : p[r];
+                }
+                u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
+                w[2 * (kb % 2)] = pack2(p[0], p[1]);
+                w[2 * (kb % 2) + 1] = pack2(p[2], p[3]);
+                pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+#else
+    auto exps = [&](int it, auto act, Probs &pf) __attribute__((always_inline)) {
         const From kn = rows_of(it + 2), vn = next;
         next = kn;
         const u32 lk = slot(0, it & 1), lv = slot(1, (it + 1) & 1);
@@ -870,6 +969,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             groups(IntC<1>{});
         }
     };
+#endif
     auto turn_end = [&] {
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0): this wave's reads of shared memory are done
@@ -877,38 +977,77 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     };
     if (sp == 1) turn_end();
     if (live(0)) {
+        Frags fr;
         seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_kf(f, k0); });
-        qk(k0);
+        qk(k0, fr);
     }
     turn_end();
 #pragma nounroll
     for (int it = 0; it < n_it; ++it) {
-        const int at = (it & 1) * TILE, to = ((it + 1) & 1) * TILE;
+        int v = v0 + (I8 ? 0 : (it & 1) * TILE), k = k0 + (I8 ? 0 : ((it + 1) & 1) * TILE);
+#if I8
+        // (what is formed from them is formed in each turn: held, it takes too
+        // many registers)
+        int kt = k_to, vt = v_to;
+        asm volatile("" : "+v"(v), "+v"(k), "+v"(kt), "+v"(vt));
+#endif
+        Probs pf;
         const bool act = live(it), some = act && masked(it);
+#if I8
+        // K of the next tile and V of this one, which the matrix turn reads next,
+        // and the scales that the next softmax turn reads
+        widen(kx, kt, KSWZ(1024 / HD));
+        widen(vx, vt, VSWZ(1024 / HD));
+        put_scales((it + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const From kn = rows_of(it + 2);
+        fetch(a.K, kn, kx);
+        fetch(a.V, next, vx);
+        fetch_scales(kn);
+        next = kn;
+        __builtin_amdgcn_sched_barrier(0);
+        if (act) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const f32x4 ks = *(const f32x4 *)&scales[sp][it & 1][0][16 * kb + 4 * g];
+#pragma unroll
+                for (int b = 0; b < QB; ++b) sc[b][kb] *= ks;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (some) mask(it);
+            maximum();
+            scaled(it, some, pf);
+        }
+#else
         if (act) {
             if (some) mask(it);
             maximum();
-            exps(it, IntC<1>{});
+            exps(it, IntC<1>{}, pf);
         } else {
-            exps(it, IntC<0>{});
+            exps(it, IntC<0>{}, pf);
         }
         WAIT_VM(2 * WL);           // the loads of the softmax turn before this one have landed
+#endif
         turn_end();
         // matrix turn: its waves go first at the issue port
         __builtin_amdgcn_s_setprio(2);
         if (act) {
-            if (some && !far_seen) far_seen = far_values(v0 + at);
-            seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_vf(f, v0 + at); });
-            pv(v0 + at, k0 + to);
-            if (live(it + 1)) qk(k0 + to);
+            if (!I8 && some && !far_seen) far_seen = far_values(v);
+            Frags fr;
+            seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_vf(f, v); });
+            pv(v, k, pf, fr);
+            if (live(it + 1)) qk(k, fr);
         }
         __builtin_amdgcn_s_setprio(0);
         turn_end();
     }
     WAIT_VM(0);
     if (sp == 0) turn_end();
+#if !I8
     if (far_seen) again = 1;
+#endif
     __syncthreads();           // every wave is done with the ring (used again below)
+#if !I8
     if (again) {
         // a tile after the other, with care for the values
         clear();
@@ -919,8 +1058,9 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             WAIT_VM(0);
             __syncthreads();
             if (live(it)) {
+                Frags fr;
                 seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_kf(f, k0); });
-                qk(k0);
+                qk(k0, fr);
                 if (masked(it)) mask(it);
                 maximum();
 #pragma unroll
@@ -947,6 +1087,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             __syncthreads();
         }
     }
+#endif
 
     // the two halves' states
 #pragma unroll
@@ -971,7 +1112,11 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         const float mo = other[b * 32 + i], lo = other[b * 32 + 16 + i], top = fmaxf(m[b], mo);
         const float by = m[b] == top ? 1.f : pow2(m[b] - top), byo = mo == top ? 1.f : pow2(mo - top);
         const float sum = l[b] * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int row = r0w + 16 * b + i, r = row - r0;
+        // (the row's token and head are formed anew: held, they take registers
+        // that the turns need)
+        int row = r0w + 16 * b + i;
+        asm volatile("" : "+v"(row));
+        const int r = row - r0;
         if (row >= rows) continue;
         if (SPLIT && item.pieces > 1 && g == 0) state[r] = top, state[BM + r] = sum;
         bf16_t *p = a.O + ((size_t)(s.q0 + row / a.G) * a.HKV * a.G + item.h * a.G + row % a.G) * HD;

@@ -629,7 +629,6 @@ static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *
     if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     if (kv(d, s, "stages") == 3) {
         if (w != 8 || kv(d, s, "occ") != 2) return "the ring in turns (stages 3) takes 8 waves, two a SIMD (occ 2)";
-        if (d->flags & RC_FLAG_I8_CACHE) return "the ring in turns (stages 3) moves bf16";
         if (bm != 64 && !(bm == 128 && q.D < 256)) return fmt("the ring in turns (stages 3) takes blocks of 64 rows, or 128 with D < 256 (%d, %lld)", bm, (long long)q.D);
         return "";
     }
@@ -1069,8 +1068,7 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
         set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
         return check_schedule(d, s).empty();
     };
-    const bool i8 = d->flags & RC_FLAG_I8_CACHE;
-    if (!i8 && rows > 32 * q.B && rows > 256) {
+    if (rows > 32 * q.B && rows > 256) {
         const int bm = q.D == 256 ? 64 : 128, splits = seqs_items(d, bm, 0) < 512 ? 1 : 0;
         if (set(bm, 8, 3, 2, splits)) return;
     }
