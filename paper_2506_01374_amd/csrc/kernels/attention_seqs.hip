@@ -575,7 +575,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 #define NPJ (BN / 32)              // MFMA steps of P V
 #define NKF (KB * NKS)             // fragments of K and of V
 #define NVF (NPJ * DB)
-#define AHEAD (I8 ? 4 : 8)         // of them read ahead of their MFMAs (int8: the registers allow 4)
+#define AHEAD 8                    // of them read ahead of their MFMAs
 #define WL (TILE / 512 / ROWG)     // 1 KiB loads of a wave for a tile
 #define RPI (512 / HD)             // rows of one
 #define NL (TILE / 1024 / ROWG)    // 16-byte loads of a lane for a tile of int8
@@ -788,12 +788,19 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     __syncthreads();
 
     f32x4 o[QB][DB];
-    float m[QB], l[QB];
+    float m[QB];
+#if I8
+    float l[QB];                   // of a lane's own keys
+#define SUM(b) l[b]
+#else
+    f32x4 l[QB];                   // of all keys, in each element
+#define SUM(b) l[b][0]
+#endif
     auto clear = [&] {
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
             m[b] = -__builtin_inff();
-            l[b] = 0.f;
+            l[b] = {};
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[b][d] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -838,9 +845,12 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                 constexpr int b = decltype(bc)::value;
                 sc[b][kb] = mfma(x, qf[b][ks], ks == 0 ? f32x4{} : sc[b][kb]);
             });
-            __builtin_amdgcn_sched_barrier(0);
+            if (!I8) __builtin_amdgcn_sched_barrier(0);        // (int8: the order pinned here would spill)
         });
     };
+#if !I8
+    const bf16x8 ones_row = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u});
+#endif
     // O^T += V^T P^T of a tile, its first AHEAD fragments in fr, reading the
     // first fragments of the next K tile
     auto pv = [&](int v, int kn, const Probs &pf, Frags &fr) __attribute__((always_inline)) {
@@ -852,6 +862,11 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
                 constexpr int b = decltype(bc)::value;
                 o[b][d] = mfma(x, pf[j][b], o[b][d]);
+                // the sums of the probabilities, a product with ones: two
+                // instructions of the matrix cores for 16 additions
+#if !I8
+                if constexpr (d == 0) l[b] = mfma(ones_row, pf[j][b], l[b]);
+#endif
             });
             if (!I8) __builtin_amdgcn_sched_barrier(0);        // (int8: the order pinned here would spill)
         });
@@ -870,27 +885,26 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                     if (!there || key + 4 * g + r > vis[b]) sc[b][kb][r] = -__builtin_inff();
         }
     };
-    // moves the running maximum where a score is past the limit (see STALE)
-    auto maximum = [&]() __attribute__((always_inline)) {
+    // Probabilities are relative to an offset m that is STALE above the largest
+    // score of the tile that set it, so that they stay below 2 until a score is
+    // past that by STALE + 1.  Whether one is, is seen in the probabilities
+    // themselves (the top bit of the exponent, which a NaN has too): the maximum
+    // of a tile's scores is needed only where the offset moves.  (int8: by the
+    // maximum of each tile's scores.)
+    auto move = [&](int b) __attribute__((always_inline)) {
+        float top = -__builtin_inff();
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            float top = -__builtin_inff();
+        for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32)) * SCALE_LOG2;
+        const float now = top > m[b] ? top + STALE : m[b];
+        const float by = m[b] == now ? 1.f : pow2(m[b] - now);
+        l[b] *= by;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
-            if (__builtin_amdgcn_ballot_w64(top * SCALE_LOG2 > m[b] + STALE) != 0) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(m[b], top * SCALE_LOG2);
-                // (all -inf so far: nothing to rescale)
-                const float by = m[b] == now ? 1.f : pow2(m[b] - now);
-                l[b] *= by;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[b][d] *= by;
-                m[b] = now;
-            }
-        }
+        for (int d = 0; d < DB; ++d) o[b][d] *= by;
+        m[b] = now;
     };
     auto masked = [&](int it) { return key_of(it) + BN - 1 > least || gaps; };
     // A tile that some row does not see whole is looked through for values that
@@ -911,6 +925,15 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     // (int8: the values' scales are multiplied in; where some row does not see a
     // key, its scale may be anything)
     auto scaled = [&](int it, bool some, Probs &pf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
+            if (__builtin_amdgcn_ballot_w64(top * SCALE_LOG2 > m[b]) != 0) move(b);
+        }
         seq<0, KB>([&](auto kc) __attribute__((always_inline)) {
             constexpr int kb = decltype(kc)::value;
             const f32x4 vs = *(const f32x4 *)&scales[sp][it & 1][1][16 * kb + 4 * g];
@@ -936,7 +959,22 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         });
     };
 #else
+    // probabilities of 16 keys; their bits
+    auto probs = [&](int b, int kb, Probs &pf) __attribute__((always_inline)) {
+        const float minus = -least_finite(m[b]);
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = pow2(__builtin_fmaf(sc[b][kb][r], SCALE_LOG2, minus));
+        u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
+        const u32 x = pack2(p[0], p[1]), y = pack2(p[2], p[3]);
+        w[2 * (kb % 2)] = x;
+        w[2 * (kb % 2) + 1] = y;
+        pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
+        return x | y;
+    };
+    auto past = [&](u32 bits) __attribute__((always_inline)) { return __builtin_amdgcn_ballot_w64((bits & 0x40004000u) != 0) != 0; };
     auto exps = [&](int it, auto act, Probs &pf) __attribute__((always_inline)) {
+        u32 bits[QB] = {};
         const From kn = rows_of(it + 2), vn = next;
         next = kn;
         const u32 lk = slot(0, it & 1), lv = slot(1, (it + 1) & 1);
@@ -948,16 +986,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                     load(a.K, k_src, kn, lk, d0, d1 < WL ? d1 : WL, IntC<0>{});
                 if constexpr (decltype(loads)::value && d1 > WL)
                     load(a.V, v_src, vn, lv, d0 > WL ? d0 - WL : 0, d1 - WL, IntC<0>{});
-                if constexpr (decltype(act)::value) {
-                    float p[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) p[r] = pow2(__builtin_fmaf(sc[b][kb][r], SCALE_LOG2, -least_finite(m[b])));
-                    l[b] += (p[0] + p[1]) + (p[2] + p[3]);
-                    u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
-                    w[2 * (kb % 2)] = pack2(p[0], p[1]);
-                    w[2 * (kb % 2) + 1] = pack2(p[2], p[3]);
-                    pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
-                }
+                if constexpr (decltype(act)::value) bits[b] |= probs(b, kb, pf);
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
@@ -967,6 +996,16 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             groups(IntC<0>{});
         } else {
             groups(IntC<1>{});
+        }
+        if constexpr (decltype(act)::value) {
+            seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
+                constexpr int b = decltype(bc)::value;
+                if (past(bits[b])) {
+                    move(b);
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) probs(b, kb, pf);
+                }
+            });
         }
     };
 #endif
@@ -1015,13 +1054,11 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (some) mask(it);
-            maximum();
             scaled(it, some, pf);
         }
 #else
         if (act) {
             if (some) mask(it);
-            maximum();
             exps(it, IntC<1>{}, pf);
         } else {
             exps(it, IntC<0>{}, pf);
@@ -1062,27 +1099,28 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
                 seq<0, AHEAD>([&](auto f) __attribute__((always_inline)) { fr[decltype(f)::value] = read_kf(f, k0); });
                 qk(k0, fr);
                 if (masked(it)) mask(it);
-                maximum();
+                Probs pf;
 #pragma unroll
-                for (int kb = 0; kb < KB; kb += 2)
+                for (int b = 0; b < QB; ++b) {
+                    u32 bits = 0;
 #pragma unroll
-                    for (int b = 0; b < QB; ++b) {
-                        const bf16x8 see = seen(sc[b][kb], sc[b][kb + 1]);
-                        u32x4 w;
+                    for (int kb = 0; kb < KB; ++kb) bits |= probs(b, kb, pf);
+                    if (past(bits)) {
+                        move(b);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float p[4];
+                        for (int kb = 0; kb < KB; ++kb) probs(b, kb, pf);
+                    }
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) l[b] += p[r] = pow2(__builtin_fmaf(sc[b][kb + c][r], SCALE_LOG2, -least_finite(m[b])));
-                            w[2 * c] = pack2(p[0], p[1]);
-                            w[2 * c + 1] = pack2(p[2], p[3]);
-                        }
+                    for (int j = 0; j < NPJ; ++j) {
+                        const bf16x8 see = seen(sc[b][2 * j], sc[b][2 * j + 1]);
+                        l[b] = mfma(ones_row, pf[j][b], l[b]);
 #pragma unroll
                         for (int d = 0; d < DB; ++d) {
-                            o[b][d] = add_far(__builtin_bit_cast(u32x4, read_v(v0, d, kb / 2)), __builtin_bit_cast(bf16x8, w), see, o[b][d]);
+                            o[b][d] = add_far(__builtin_bit_cast(u32x4, read_v(v0, d, j)), pf[j][b], see, o[b][d]);
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
+                }
             }
             __syncthreads();
         }
@@ -1090,16 +1128,18 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
 #endif
 
     // the two halves' states
+#if I8
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         l[b] += __shfl_xor(l[b], 16);
         l[b] += __shfl_xor(l[b], 32);
     }
+#endif
     float *const other = (float *)ring[0] + rg * (QB * (32 + DB * 256));
     if (sp == 1) {
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            if (g == 0) other[b * 32 + i] = m[b], other[b * 32 + 16 + i] = l[b];
+            if (g == 0) other[b * 32 + i] = m[b], other[b * 32 + 16 + i] = SUM(b);
 #pragma unroll
             for (int d = 0; d < DB; ++d) *(f32x4 *)(other + QB * 32 + ((b * DB + d) * 64 + lane) * 4) = o[b][d];
         }
@@ -1111,7 +1151,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     for (int b = 0; b < QB; ++b) {
         const float mo = other[b * 32 + i], lo = other[b * 32 + 16 + i], top = fmaxf(m[b], mo);
         const float by = m[b] == top ? 1.f : pow2(m[b] - top), byo = mo == top ? 1.f : pow2(mo - top);
-        const float sum = l[b] * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float sum = SUM(b) * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
         // (the row's token and head are formed anew: held, they take registers
         // that the turns need)
         int row = r0w + 16 * b + i;
