@@ -64,7 +64,7 @@ struct SeqsArgs {
     bf16_t *O;
     float *P;                      // states of pieces (SPLIT)
     int T, TK, B, G, HKV, shift, pages, width, causal, slots;
-    int share;                     // the join: four waves a row
+    int by;                        // the join: see there
 };
 
 __device__ __forceinline__ int limit(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -129,12 +129,13 @@ __device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amd
 // that pieces of blocks that are cut are at most 2 a.slots: each takes more than
 // half of it.  The pieces' states are in this order too: sequence by sequence,
 // its last block (the one that sees most keys) first, piece by piece, head by
-// head.  Item `index` of that order, or (JOIN) the first piece's of what row
-// `index` of Q is in.
-template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int index, Item &item) {
+// head.  Item `index` of that order (ITEMS), the first piece's of what row
+// `index` of Q is in (ROWS), or of the `index`-th block that is cut (BLOCKS).
+enum Find { ITEMS, ROWS, BLOCKS };
+template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int index, Item &item) {
     const int lane = threadIdx.x & 63;
-    item.h = JOIN ? 0 : index % a.HKV;
-    int j = JOIN ? index : index / a.HKV;
+    item.h = WHAT == ROWS ? 0 : index % a.HKV;
+    int j = WHAT == ROWS ? index : index / a.HKV;
     int most = 1 << 30;
     Seq first = {};                // of the first 64 sequences
     if (lane < a.B) first = sequence(a, lane);
@@ -154,8 +155,9 @@ template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int
         const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
         const int blocks = c + lane < a.B ? blocks_of(a, s) : 0, pieces = SPLIT ? max(1, (tiles_of(s) + most - 1) / most) : 1;
         const int cut = pieces > 1 ? blocks * pieces : 0;      // states that the sequence leaves
-        const int items = blocks * pieces, sum = JOIN ? 0 : scan(items), sums = SPLIT ? scan(cut) : 0;
-        const unsigned long long past = __builtin_amdgcn_ballot_w64(JOIN ? blocks > 0 && s.q0 <= j && j < s.q0 + s.n : sum > j);
+        const int items = WHAT == ITEMS ? blocks * pieces : pieces > 1 ? blocks : 0;
+        const int sum = WHAT == ROWS ? 0 : scan(items), sums = SPLIT ? scan(cut) : 0;
+        const unsigned long long past = __builtin_amdgcn_ballot_w64(WHAT == ROWS ? blocks > 0 && s.q0 <= j && j < s.q0 + s.n : sum > j);
         if (past) {
             const int at = __builtin_ctzll(past);
             item.s.q0 = from_lane(s.q0, at), item.s.n = from_lane(s.n, at), item.s.len = from_lane(s.len, at);
@@ -164,18 +166,18 @@ template <bool JOIN> __device__ __forceinline__ bool find(const SeqsArgs &a, int
             item.s.k0 = PAGED ? c + at : from_lane(s.k0, at);
             item.pieces = from_lane(pieces, at);
             slot += from_lane(sums - cut, at);
-            if (JOIN) {
+            if (WHAT == ROWS) {
                 item.slot = slot;
                 item.block = from_lane(blocks, at);            // how many there are
                 return true;
             }
-            const int i = j - from_lane(sum - items, at), order = i / item.pieces;
+            const int i = j - from_lane(sum - items, at), order = WHAT == ITEMS ? i / item.pieces : i;
             item.block = from_lane(blocks, at) - 1 - order;
-            item.piece = i % item.pieces;
-            item.slot = (slot + i) * a.HKV + item.h;
+            item.piece = WHAT == ITEMS ? i % item.pieces : 0;
+            item.slot = (slot + order * item.pieces + item.piece) * a.HKV + item.h;
             return true;
         }
-        if (!JOIN) j -= from_lane(sum, 63);
+        if (WHAT != ROWS) j -= from_lane(sum, 63);
         slot += from_lane(sums, 63);
     }
     return false;
@@ -258,7 +260,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane % 16, g = lane / 16;
     Item item;
-    if (!find<false>(a, blockIdx.x, item)) return;
+    if (!find<ITEMS>(a, blockIdx.x, item)) return;
     const Seq s = item.s;
     const int rows = s.n * a.G, r0 = item.block * BM;
 
@@ -564,6 +566,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 
 #if STAGES == 3
 #define ROWG 4                     // groups of rows
+#define HALVES (NW / ROWG)         // 2: of the waves, 1: all of them take every tile
 #define BNW (BN / ROWG)            // keys that a wave loads of a tile
 #define KB (BN / 16)
 #define DB (HD / 16)
@@ -592,20 +595,28 @@ template <int A, int B, class F> __device__ __forceinline__ void seq(F &&f) {
 // at most n loads of this wave are left in flight
 #define WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | ((((n) >> 4) & 3) << 14) | (7 << 4) | (15 << 8))
 
-extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void rc_attention_seqs(SeqsArgs a) {
+// the lane's number, formed where it is used: held, it takes a register that the
+// turns need
+__device__ __forceinline__ int lane_here() {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+}
+
+extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void rc_attention_seqs(SeqsArgs a) {
 #if I8
     // K of each half's tile, then V; the last for the halves' states
-    __shared__ __attribute__((aligned(16))) bf16_t ring[5][TILE];
-    __shared__ __attribute__((aligned(16))) float scales[2][2][2][BN];        // of each half: two tiles' Ks and Vs
+    __shared__ __attribute__((aligned(16))) bf16_t ring[HALVES == 2 ? 5 : 2][TILE];
+    __shared__ __attribute__((aligned(16))) float scales[HALVES][2][2][BN];   // of each half: two tiles' Ks and Vs
 #else
-    __shared__ __attribute__((aligned(16))) bf16_t ring[8][TILE];      // K of each half's two tiles, then V
+    __shared__ __attribute__((aligned(16))) bf16_t ring[4 * HALVES][TILE];    // K of each half's two tiles, then V
     __shared__ int again;
     if (threadIdx.x == 0) again = 0;
 #endif
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane % 16, g = lane / 16, rg = wave % ROWG, sp = wave / ROWG;
     Item item;
-    if (!find<false>(a, blockIdx.x, item)) return;
+    if (!find<ITEMS>(a, blockIdx.x, item)) return;
     const Seq s = item.s;
     const int rows = s.n * a.G, r0 = item.block * BM, r0w = r0 + 16 * QB * rg;
 
@@ -613,7 +624,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     const int last_vis = s.vis((min(rows, r0 + BM) - 1) / a.G, a.causal);
     const int all = (max(last_vis + 1, 0) + BN - 1) / BN, share = (all + item.pieces - 1) / item.pieces;
     const int kt0 = item.piece * share, n_kt = max(0, min(all, kt0 + share) - kt0);
-    const int n_it = (n_kt + 1) / 2, n_loc = (n_kt + 1 - sp) / 2;      // turns; tiles of this half
+    const int n_it = (n_kt + HALVES - 1) / HALVES, n_loc = (n_kt + HALVES - 1 - sp) / HALVES;        // turns; tiles of this half
 
     // loads: lane's byte offsets within the wave's rows of a tile
 #if I8
@@ -621,7 +632,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     const int row = lane / (HD / 16), chunk = lane % (HD / 16), rw = rg * BNW + row;
     // (elements of the first of them; 1024 / HD rows on the XOR-ed part changes
     // by a constant)
-    const int k_to = sp * TILE + rw * HD + 8 * ((2 * chunk) ^ KSWZ(rw)), v_to = (2 + sp) * TILE + rw * HD + 8 * ((2 * chunk) ^ VSWZ(rw));
+    const int k_to = sp * TILE + rw * HD + 8 * ((2 * chunk) ^ KSWZ(rw)), v_to = (HALVES + sp) * TILE + rw * HD + 8 * ((2 * chunk) ^ VSWZ(rw));
 #else
 #if PAGED
     constexpr u32 step = HD * 2;
@@ -638,7 +649,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     typedef __attribute__((address_space(3))) bf16_t *lds_p;
     const u32 lds0 = (u32)(size_t)(lds_p)ring[0] + rg * (WL * 1024u);
     // K or V (v) of this half's slot b
-    auto slot = [&](int v, int b) { return lds0 + (u32)(4 * v + 2 * sp + b) * (TILE * 2u); };
+    auto slot = [&](int v, int b) { return lds0 + (u32)(2 * HALVES * v + 2 * sp + b) * (TILE * 2u); };
     // (issued from inline assembly, which the compiler's own waits do not see:
     // it would drain them before every read of shared memory)
     auto dma = [&](const char *base, u32 off, u32 lds) {
@@ -654,7 +665,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     };
     const int last_key = s.keys - 1;
     int ids = 0;                           // pages of the wave's rows of 64 tiles
-    auto first_key = [&](int it) { return min((kt0 + 2 * it + sp) * BN + BNW * rg, last_key & ~(BNW - 1)); };
+    auto first_key = [&](int it) { return min((kt0 + HALVES * it + sp) * BN + BNW * rg, last_key & ~(BNW - 1)); };
     auto rows_of = [&](int it) {
         it = min(it, max(n_loc - 1, 0));
         const int key = first_key(it);
@@ -662,7 +673,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         f.end = last_key - key;
 #if PAGED
         if (it % 64 == 0) {
-            const int x = first_key(it + lane);
+            const int x = first_key(it + lane_here());
             ids = a.table[(size_t)s.k0 * a.width + (x >> a.shift)];
         }
         const int id = __builtin_amdgcn_readlane(ids, it % 64);
@@ -814,7 +825,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     // tile starts at a multiple of HD); of V likewise
     constexpr int SLOTS = I8 ? 1 : 2;      // of a half's operand
     const int k0 = SLOTS * sp * TILE + i * HD + 8 * (g ^ KSWZ(i));
-    const int vr = 4 * g + i / 4, v0 = SLOTS * (2 + sp) * TILE + vr * HD + 8 * ((lane & 3) / 2 ^ VSWZ(vr)) + (lane & 1) * 4;
+    const int vr = 4 * g + i / 4, v0 = SLOTS * (HALVES + sp) * TILE + vr * HD + 8 * ((lane & 3) / 2 ^ VSWZ(vr)) + (lane & 1) * 4;
     auto read_kf = [&](auto fc, int k) __attribute__((always_inline)) {
         constexpr int f = decltype(fc)::value;
         return *(const bf16x8 *)(ring[0] + (k ^ 32 * (f % NKS)) + (f / NKS) * 16 * HD);
@@ -871,7 +882,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
             if (!I8) __builtin_amdgcn_sched_barrier(0);        // (int8: the order pinned here would spill)
         });
     };
-    auto key_of = [&](int it) { return (kt0 + 2 * it + sp) * BN; };
+    auto key_of = [&](int it) { return (kt0 + HALVES * it + sp) * BN; };
     auto live = [&](int it) { return it < n_loc && key_of(it) <= most; };
     auto mask = [&](int it) __attribute__((always_inline)) {
 #pragma unroll
@@ -1079,7 +1090,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         turn_end();
     }
     WAIT_VM(0);
-    if (sp == 0) turn_end();
+    if (HALVES == 2 && sp == 0) turn_end();
 #if !I8
     if (far_seen) again = 1;
 #endif
@@ -1135,6 +1146,7 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
         l[b] += __shfl_xor(l[b], 32);
     }
 #endif
+#if HALVES == 2
     float *const other = (float *)ring[0] + rg * (QB * (32 + DB * 256));
     if (sp == 1) {
 #pragma unroll
@@ -1146,53 +1158,52 @@ extern "C" __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(
     }
     __syncthreads();
     if (sp == 1) return;
+#endif
     float *state = a.P + (SPLIT ? (size_t)item.slot * STATE : 0);
+    const int ie = lane_here() % 16, ge = lane_here() / 16;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-        const float mo = other[b * 32 + i], lo = other[b * 32 + 16 + i], top = fmaxf(m[b], mo);
+#if HALVES == 2
+        const float mo = other[b * 32 + ie], lo = other[b * 32 + 16 + ie], top = fmaxf(m[b], mo);
         const float by = m[b] == top ? 1.f : pow2(m[b] - top), byo = mo == top ? 1.f : pow2(mo - top);
         const float sum = SUM(b) * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
-        // (the row's token and head are formed anew: held, they take registers
-        // that the turns need)
-        int row = r0w + 16 * b + i;
-        asm volatile("" : "+v"(row));
-        const int r = row - r0;
+#else
+        const float top = m[b], sum = SUM(b), inv = sum == 0.f ? 0.f : 1.f / sum;
+#endif
+        const int row = r0w + 16 * b + ie, r = row - r0;
         if (row >= rows) continue;
-        if (SPLIT && item.pieces > 1 && g == 0) state[r] = top, state[BM + r] = sum;
+        if (SPLIT && item.pieces > 1 && ge == 0) state[r] = top, state[BM + r] = sum;
         bf16_t *p = a.O + ((size_t)(s.q0 + row / a.G) * a.HKV * a.G + item.h * a.G + row % a.G) * HD;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-            const f32x4 x = o[b][d] * by + *(const f32x4 *)(other + QB * 32 + ((b * DB + d) * 64 + lane) * 4) * byo;
-            if (SPLIT && item.pieces > 1) *(f32x4 *)(state + 2 * BM + r * HD + 16 * d + 4 * g) = x;
-            else *(u32x2 *)(p + 16 * d + 4 * g) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
+#if HALVES == 2
+            const f32x4 x = o[b][d] * by + *(const f32x4 *)(other + QB * 32 + ((b * DB + d) * 64 + 16 * ge + ie) * 4) * byo;
+#else
+            const f32x4 x = o[b][d];
+#endif
+            if (SPLIT && item.pieces > 1) *(f32x4 *)(state + 2 * BM + r * HD + 16 * d + 4 * ge) = x;
+            else *(u32x2 *)(p + 16 * d + 4 * ge) = u32x2{pack2(x[0] * inv, x[1] * inv), pack2(x[2] * inv, x[3] * inv)};
         }
     }
 }
 #endif
 
 // ---------------------------------------------------------------------------
-// Rows of sequences that were cut: a wave takes a row, or a workgroup (`share`)
+// The pieces of blocks that were cut
 // ---------------------------------------------------------------------------
 //
-// A lane takes 4 channels of every 256 / HD-th piece (of every 1024 / HD-th with
-// four waves a row), eight pieces at once: the time is that of the way to memory
-// and back.
+// A lane takes 4 channels.  By blocks: a workgroup takes the pieces of 2048 / HD
+// rows of a block, four at once.  By rows, where a block has few but may have
+// many pieces: a wave takes a row (`by` 0), or a workgroup (1), a lane every 256 /
+// HD-th piece (1024 / HD-th), eight at once.  The time is that of the way to
+// memory and back, and for large blocks of their states (26 MB of 200 blocks of
+// 128 rows in two pieces).
 #if SPLIT
 extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArgs a) {
     __shared__ f32x4 po[4][HD / 4];
     __shared__ float pm[4], pl[4];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.HKV * a.G;
-    const long long at = a.share ? blockIdx.x : (long long)blockIdx.x * 4 + w;
-    if (at >= (long long)a.T * H) return;
-    const int token = (int)(at / H), head = (int)(at % H);
-    Item item;
-    if (!find<true>(a, token, item) || item.pieces == 1) return;
-    const int row = (token - item.s.q0) * a.G + head % a.G, r = row % BM;
-    const float *state = a.P + ((size_t)(item.slot + (item.block - 1 - row / BM) * item.pieces) * a.HKV + head / a.G) * STATE;
-    const size_t next = (size_t)a.HKV * STATE;          // of the block's next piece
-    constexpr int LANES = HD / 4, PAR = 64 / LANES;
-    const int part = lane / LANES, d = lane % LANES * 4;
-    const int step = a.share ? 4 * PAR : PAR;
+    const size_t next = (size_t)a.HKV * STATE;          // of a block's next piece
     float m = -__builtin_inff(), l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float mp, float lp, const f32x4 &op) {
@@ -1201,7 +1212,50 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
         o = o * x + op * y;
         m = top;
     };
-    for (int p0 = a.share ? w * PAR + part : part; p0 - part < item.pieces; p0 += 8 * step) {
+    constexpr int LANES = HD / 4, PAR = 64 / LANES;
+#if STAGES == 3
+    {
+        constexpr int ROWS_OF = 8 * PAR, SHARES = BM / ROWS_OF;      // rows of a workgroup, workgroups of a block
+        Item item;
+        if (!find<BLOCKS>(a, blockIdx.x / SHARES, item)) return;
+        const int d = threadIdx.x % LANES * 4;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = blockIdx.x % SHARES * ROWS_OF + half * (ROWS_OF / 2) + threadIdx.x / LANES, row = item.block * BM + r;
+            if (row >= item.s.n * a.G) continue;
+            const float *state = a.P + (size_t)item.slot * STATE;
+            m = -__builtin_inff(), l = 0.f;
+            o = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < item.pieces; p += 4) {
+                float mp[4], lp[4];
+                f32x4 op[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float *x = state + (size_t)min(p + i, item.pieces - 1) * next;
+                    mp[i] = x[r], lp[i] = x[BM + r];
+                    op[i] = *(const f32x4 *)(x + 2 * BM + r * HD + d);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (p + i < item.pieces) add(mp[i], lp[i], op[i]);
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            bf16_t *to = a.O + ((size_t)(item.s.q0 + row / a.G) * H + item.h * a.G + row % a.G) * HD + d;
+            *(u32x2 *)to = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+        }
+        return;
+    }
+#endif
+    const long long at = a.by ? blockIdx.x : (long long)blockIdx.x * 4 + w;
+    if (at >= (long long)a.T * H) return;
+    const int token = (int)(at / H), head = (int)(at % H);
+    Item item;
+    if (!find<ROWS>(a, token, item) || item.pieces == 1) return;
+    const int row = (token - item.s.q0) * a.G + head % a.G, r = row % BM;
+    const float *state = a.P + ((size_t)(item.slot + (item.block - 1 - row / BM) * item.pieces) * a.HKV + head / a.G) * STATE;
+    const int part = lane / LANES, d = lane % LANES * 4;
+    const int step = a.by ? 4 * PAR : PAR;
+    for (int p0 = a.by ? w * PAR + part : part; p0 - part < item.pieces; p0 += 8 * step) {
         float mp[8], lp[8];
         f32x4 op[8];
 #pragma unroll
@@ -1219,7 +1273,7 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
         const f32x4 other = {__shfl_xor(o[0], x), __shfl_xor(o[1], x), __shfl_xor(o[2], x), __shfl_xor(o[3], x)};
         add(__shfl_xor(m, x), __shfl_xor(l, x), other);
     }
-    if (a.share) {
+    if (a.by) {
         if (part == 0) po[w][d / 4] = o;
         if (lane == 0) pm[w] = m, pl[w] = l;
         __syncthreads();

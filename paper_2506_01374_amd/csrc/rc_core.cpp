@@ -620,6 +620,10 @@ int64_t seqs_items(const rc_op_desc *d, int bm, int splits) {
     return q.Hkv * (q.T * (q.H / q.Hkv) / bm + std::min(q.B, q.T)) + 256 * splits;
 }
 
+int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits) {
+    return std::min<int64_t>(256 * splits, seqs_items(d, bm, 0));
+}
+
 static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
@@ -628,8 +632,8 @@ static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *
     if (sp && q.T * q.H * 64 + 192 > MAX_GRID_THREADS) return "splits: the rows exceed the joining launch's grid";
     if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     if (kv(d, s, "stages") == 3) {
-        if (w != 8 || kv(d, s, "occ") != 2) return "the ring in turns (stages 3) takes 8 waves, two a SIMD (occ 2)";
-        if (bm != 64 && !(bm == 128 && q.D < 256)) return fmt("the ring in turns (stages 3) takes blocks of 64 rows, or 128 with D < 256 (%d, %lld)", bm, (long long)q.D);
+        if ((w != 4 && w != 8) || kv(d, s, "occ") != 2) return "the ring (stages 3) takes 4 waves, or 8 in turns, two a SIMD (occ 2)";
+        if (bm != 64 && !(bm == 128 && q.D < 256)) return fmt("the ring (stages 3) takes blocks of 64 rows, or 128 with D < 256 (%d, %lld)", bm, (long long)q.D);
         return "";
     }
     const int64_t lds = (int64_t)w * bm * (q.D + 6) * 4;
@@ -1069,8 +1073,10 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
         return check_schedule(d, s).empty();
     };
     if (rows > 32 * q.B && rows > 256) {
-        const int bm = q.D == 256 ? 64 : 128, splits = seqs_items(d, bm, 0) < 512 ? 1 : 0;
-        if (set(bm, 8, 3, 2, splits)) return;
+        const int64_t items = q.Hkv * rows / 128;
+        const int bm = q.D < 256 && items >= 384 ? 128 : 64;
+        const int waves = items >= 1024 || (bm == 64 && items >= 192) ? 4 : 8;
+        if (set(bm, waves, 3, 2, items < 64 ? 1 : 0)) return;
     }
     for (int sp : {2, 0})
         for (int occ : {2, 1})
@@ -1164,7 +1170,7 @@ static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
     const bool cache = kind->kind == RC_OP_KV_WRITE || kind->kind == RC_OP_KV_READ;
     for (int64_t D : {64, 128, 256}) {         // (a definition of the kernels)
         Suggestions once;
-        for (int64_t T : {1, 2, 3, 5, 300, 1 << 20}) {
+        for (int64_t T : {1, 2, 3, 5, 300, 8192, 24576, 49152, 1 << 20}) {
             rc_op_desc d = *kind;
             const int64_t dims[8] = {T, 1, 1, cache ? D : 1, cache ? 16 : d.kind == RC_OP_ATTENTION_PAGED ? D : 1,
                                      cache || d.kind == RC_OP_ATTENTION_PAGED ? 16 : D, 1 << 16, 1 << 16};

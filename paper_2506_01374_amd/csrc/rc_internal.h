@@ -47,8 +47,11 @@ struct SeqDims {
 };
 SeqDims seq_dims(const rc_op_desc *d);
 int expected_dims(int32_t kind);
-// Work items that an attention over sequences has at most.
+// Work items that an attention over sequences has at most, and blocks of rows
+// that it cuts: of two pieces at least, which are fewer than two a workgroup that
+// the keys are cut for.
 int64_t seqs_items(const rc_op_desc *d, int bm, int splits);
+int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits);
 
 // Legality with a reason; "" when legal.
 std::string check_schedule(const rc_op_desc *d, const rc_schedule *s);

@@ -87,7 +87,7 @@ struct CacheArgs {
 struct SeqsArgs {
     const void *Q, *K, *V, *Ks, *Vs, *offsets, *lens, *table;
     void *O, *P;
-    int T, TK, B, G, HKV, shift, pages, width, causal, slots, share;
+    int T, TK, B, G, HKV, shift, pages, width, causal, slots, by;
 };
 struct PadI8Args {
     const void *A, *B0, *B1;
@@ -974,8 +974,10 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             // states of the pieces of cut blocks: fewer than two a workgroup that
             // the keys are cut for
             const size_t offP = sp ? ws.add((size_t)512 * sp * bm * (q.D + 2) * 4, "partials") : 0;
-            // few rows have many pieces: four waves a row then
-            const int share = q.T * q.H <= 4096;
+            // the join: by blocks; by rows where a block has few, four waves a row
+            // where there are few rows, which have many pieces
+            const bool ring = kv(d, s, "stages") == 3;
+            const int by = q.T * q.H <= 4096;
             char scale[64];
             snprintf(scale, sizeof scale, "#define SCALE_LOG2 %.17gf\n", 1.4426950408889634 / std::sqrt((double)q.D));
             Kern k;
@@ -990,14 +992,14 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
                 put(b, SeqsArgs{a->in[0], a->in[1], a->in[2], i8 ? a->in[3] : nullptr, i8 ? a->in[4] : nullptr, a->in[at],
                                 a->in[at + 1], paged ? a->in[at + 2] : nullptr, a->out[0], sp ? wsp + offP : nullptr,
                                 (int)q.T, (int)q.TK, (int)q.B, (int)(q.H / q.Hkv), (int)q.Hkv,
-                                paged ? __builtin_ctzll(q.page) : 0, (int)q.pages, (int)q.width, causal, 256 * sp, share});
+                                paged ? __builtin_ctzll(q.page) : 0, (int)q.pages, (int)q.width, causal, 256 * sp, by});
             };
             p.kerns.push_back(k);
             if (sp) {
                 Kern kj = k;
                 kj.flops = 0;
                 kj.src.entry = "rc_attention_seqs_join";
-                kj.grid = dim3((unsigned)(share ? q.T * q.H : (q.T * q.H + 3) / 4), 1, 1);
+                kj.grid = dim3((unsigned)(ring ? seqs_cut_blocks(d, bm, sp) * (bm * q.D / 2048) : by ? q.T * q.H : (q.T * q.H + 3) / 4), 1, 1);
                 kj.block = dim3(256, 1, 1);
                 p.kerns.push_back(kj);
             }
