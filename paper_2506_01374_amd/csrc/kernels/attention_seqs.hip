@@ -149,6 +149,23 @@ template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int
     }
     work = (work * a.HKV + a.slots - 1) / a.slots;
     most = work < LEAST ? LEAST : work > (1 << 30) ? 1 << 30 : (int)work;
+#if STAGES == 3
+    // (a last piece more of many blocks can be a second round of workgroups: 25
+    // blocks of 8 heads in 3 pieces for 2, with 15 single rows, 157 us for 148)
+    for (int tries = 0; tries < 4; ++tries) {
+        long long items = 0;
+        bool cut = false;
+        for (int c = 0; c < a.B; c += 64) {
+            const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
+            const int pieces = c + lane < a.B ? max(1, (tiles_of(s) + most - 1) / most) : 1;
+            items += from_lane(scan(c + lane < a.B ? (int)min((long long)blocks_of(a, s) * pieces, 1ll << 24) : 0), 63);
+            cut |= __builtin_amdgcn_ballot_w64(pieces > 1) != 0;
+        }
+        items *= a.HKV;
+        if (!cut || items * 16 <= a.slots * 17ll) break;
+        most = (int)min((long long)(1 << 30), most * items / a.slots + 1);
+    }
+#endif
 #endif
     int slot = 0;
     for (int c = 0; c < a.B; c += 64) {
@@ -607,7 +624,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 #if I8
     // K of each half's tile, then V; the last for the halves' states
     __shared__ __attribute__((aligned(16))) bf16_t ring[HALVES == 2 ? 5 : 2][TILE];
-    __shared__ __attribute__((aligned(16))) float scales[HALVES][2][2][BN];   // of each half: two tiles' Ks and Vs
+    __shared__ __attribute__((aligned(16))) float scales[HALVES][2][2][BN];   // of each half: two tiles' Ks (times SCALE_LOG2) and Vs
+    __shared__ __attribute__((aligned(16))) float ones[BN];
+    if (threadIdx.x < BN) ones[threadIdx.x] = 1.f;
 #else
     __shared__ __attribute__((aligned(16))) bf16_t ring[4 * HALVES][TILE];    // K of each half's two tiles, then V
     __shared__ int again;
@@ -715,7 +734,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
             }
     };
     auto put_scales = [&](int b) __attribute__((always_inline)) {
-        if (lane < 2 * BNW) scales[sp][b][lane / BNW][rg * BNW + lane % BNW] = lane < BNW ? sx : sy;
+        if (lane < 2 * BNW) scales[sp][b][lane / BNW][rg * BNW + lane % BNW] = lane < BNW ? sx * SCALE_LOG2 : sy;
     };
     From next = {0, BNW};
     if (n_kt > 0) {
@@ -900,16 +919,15 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     // score of the tile that set it, so that they stay below 2 until a score is
     // past that by STALE + 1.  Whether one is, is seen in the probabilities
     // themselves (the top bit of the exponent, which a NaN has too): the maximum
-    // of a tile's scores is needed only where the offset moves.  (int8: by the
-    // maximum of each tile's scores.)
-    auto move = [&](int b) __attribute__((always_inline)) {
+    // of a tile's scores is needed only where the offset moves.
+    auto move = [&](int b, const float *scale) __attribute__((always_inline)) {
         float top = -__builtin_inff();
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r] * (I8 ? scale[16 * kb + r] : SCALE_LOG2));
         top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32)) * SCALE_LOG2;
+        top = fmaxf(top, __shfl_xor(top, 32));
         const float now = top > m[b] ? top + STALE : m[b];
         const float by = m[b] == now ? 1.f : pow2(m[b] - now);
         l[b] *= by;
@@ -936,37 +954,48 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     // (int8: the values' scales are multiplied in; where some row does not see a
     // key, its scale may be anything)
     auto scaled = [&](int it, bool some, Probs &pf) __attribute__((always_inline)) {
+        // (the scores of a tile that some row does not see whole have their
+        // scales, and the mask, already)
+        const float *const scale = (some ? ones : scales[sp][it & 1][0]) + 4 * g;
+        u32 bits[QB] = {};
+        float sum[QB] = {};
+        auto all = [&](int first, int last) __attribute__((always_inline)) {
+            seq<0, KB>([&](auto kc) __attribute__((always_inline)) {
+                constexpr int kb = decltype(kc)::value;
+                const f32x4 ks = *(const f32x4 *)(scale + 16 * kb), vs = *(const f32x4 *)&scales[sp][it & 1][1][16 * kb + 4 * g];
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            float top = -__builtin_inff();
+                for (int b = first; b < last; ++b) {
+                    const float minus = -least_finite(m[b]);
+                    float p[4];
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
+                    for (int r = 0; r < 4; ++r) {
+                        p[r] = pow2(__builtin_fmaf(sc[b][kb][r], ks[r], minus));
+                        bits[b] |= __builtin_bit_cast(u32, p[r]);
+                    }
+                    sum[b] += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[b][kb][r]);
-            if (__builtin_amdgcn_ballot_w64(top * SCALE_LOG2 > m[b]) != 0) move(b);
-        }
-        seq<0, KB>([&](auto kc) __attribute__((always_inline)) {
-            constexpr int kb = decltype(kc)::value;
-            const f32x4 vs = *(const f32x4 *)&scales[sp][it & 1][1][16 * kb + 4 * g];
-            seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
-                constexpr int b = decltype(bc)::value;
-                const float minus = -least_finite(m[b]);
-                float p[4];
+                    for (int r = 0; r < 4; ++r) p[r] *= vs[r];
+                    if (some) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = pow2(__builtin_fmaf(sc[b][kb][r], SCALE_LOG2, minus));
-                l[b] += (p[0] + p[1]) + (p[2] + p[3]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] *= vs[r];
-                if (some) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) p[r] = sc[b][kb][r] == -__builtin_inff() ? 0.f : p[r];
+                        for (int r = 0; r < 4; ++r) p[r] = sc[b][kb][r] == -__builtin_inff() ? 0.f : p[r];
+                    }
+                    u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
+                    w[2 * (kb % 2)] = pack2(p[0], p[1]);
+                    w[2 * (kb % 2) + 1] = pack2(p[2], p[3]);
+                    pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
                 }
-                u32x4 w = __builtin_bit_cast(u32x4, pf[kb / 2][b]);
-                w[2 * (kb % 2)] = pack2(p[0], p[1]);
-                w[2 * (kb % 2) + 1] = pack2(p[2], p[3]);
-                pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
+                __builtin_amdgcn_sched_barrier(0);
             });
-            __builtin_amdgcn_sched_barrier(0);
+        };
+        all(0, QB);
+        seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
+            constexpr int b = decltype(bc)::value;
+            if (__builtin_amdgcn_ballot_w64(bits[b] >> 30 & 1) != 0) {
+                move(b, scale);
+                sum[b] = 0.f;
+                all(b, b + 1);
+            }
+            l[b] += sum[b];
         });
     };
 #else
@@ -1012,7 +1041,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
             seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
                 constexpr int b = decltype(bc)::value;
                 if (past(bits[b])) {
-                    move(b);
+                    move(b, nullptr);
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) probs(b, kb, pf);
                 }
@@ -1057,14 +1086,15 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         next = kn;
         __builtin_amdgcn_sched_barrier(0);
         if (act) {
+            if (some) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const f32x4 ks = *(const f32x4 *)&scales[sp][it & 1][0][16 * kb + 4 * g];
+                for (int kb = 0; kb < KB; ++kb) {
+                    const f32x4 ks = *(const f32x4 *)&scales[sp][it & 1][0][16 * kb + 4 * g];
 #pragma unroll
-                for (int b = 0; b < QB; ++b) sc[b][kb] *= ks;
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int b = 0; b < QB; ++b) sc[b][kb] *= ks;
+                }
+                mask(it);
             }
-            if (some) mask(it);
             scaled(it, some, pf);
         }
 #else
@@ -1117,7 +1147,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 #pragma unroll
                     for (int kb = 0; kb < KB; ++kb) bits |= probs(b, kb, pf);
                     if (past(bits)) {
-                        move(b);
+                        move(b, nullptr);
 #pragma unroll
                         for (int kb = 0; kb < KB; ++kb) probs(b, kb, pf);
                     }
@@ -1192,10 +1222,10 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // The pieces of blocks that were cut
 // ---------------------------------------------------------------------------
 //
-// A lane takes 4 channels.  By blocks: a workgroup takes the pieces of 2048 / HD
-// rows of a block, four at once.  By rows, where a block has few but may have
-// many pieces: a wave takes a row (`by` 0), or a workgroup (1), a lane every 256 /
-// HD-th piece (1024 / HD-th), eight at once.  The time is that of the way to
+// A lane takes 4 channels.  By blocks (`by` 2): a workgroup takes the pieces of 2048
+// / HD rows of a block, four or eight at once.  By rows, where there are few, which
+// may have many pieces: a workgroup takes a row (1), a lane every 1024 / HD-th
+// piece, eight at once.  The time is that of the way to
 // memory and back, and for large blocks of their states (26 MB of 200 blocks of
 // 128 rows in two pieces).
 #if SPLIT
@@ -1213,30 +1243,30 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
         m = top;
     };
     constexpr int LANES = HD / 4, PAR = 64 / LANES;
-#if STAGES == 3
-    {
-        constexpr int ROWS_OF = 8 * PAR, SHARES = BM / ROWS_OF;      // rows of a workgroup, workgroups of a block
+    if (a.by == 2) {
+        constexpr int ROWS_OF = 8 * PAR, SHARES = BM > ROWS_OF ? BM / ROWS_OF : 1;       // rows of a workgroup, workgroups of a block
+        constexpr int ONCE = STAGES == 3 ? 4 : 8;
         Item item;
         if (!find<BLOCKS>(a, blockIdx.x / SHARES, item)) return;
         const int d = threadIdx.x % LANES * 4;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int r = blockIdx.x % SHARES * ROWS_OF + half * (ROWS_OF / 2) + threadIdx.x / LANES, row = item.block * BM + r;
-            if (row >= item.s.n * a.G) continue;
+            if (r >= BM || row >= item.s.n * a.G) continue;
             const float *state = a.P + (size_t)item.slot * STATE;
             m = -__builtin_inff(), l = 0.f;
             o = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int p = 0; p < item.pieces; p += 4) {
-                float mp[4], lp[4];
-                f32x4 op[4];
+            for (int p = 0; p < item.pieces; p += ONCE) {
+                float mp[ONCE], lp[ONCE];
+                f32x4 op[ONCE];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < ONCE; ++i) {
                     const float *x = state + (size_t)min(p + i, item.pieces - 1) * next;
                     mp[i] = x[r], lp[i] = x[BM + r];
                     op[i] = *(const f32x4 *)(x + 2 * BM + r * HD + d);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < ONCE; ++i)
                     if (p + i < item.pieces) add(mp[i], lp[i], op[i]);
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -1245,17 +1275,15 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
         }
         return;
     }
-#endif
-    const long long at = a.by ? blockIdx.x : (long long)blockIdx.x * 4 + w;
-    if (at >= (long long)a.T * H) return;
+    const long long at = blockIdx.x;
     const int token = (int)(at / H), head = (int)(at % H);
     Item item;
     if (!find<ROWS>(a, token, item) || item.pieces == 1) return;
     const int row = (token - item.s.q0) * a.G + head % a.G, r = row % BM;
     const float *state = a.P + ((size_t)(item.slot + (item.block - 1 - row / BM) * item.pieces) * a.HKV + head / a.G) * STATE;
     const int part = lane / LANES, d = lane % LANES * 4;
-    const int step = a.by ? 4 * PAR : PAR;
-    for (int p0 = a.by ? w * PAR + part : part; p0 - part < item.pieces; p0 += 8 * step) {
+    constexpr int step = 4 * PAR;
+    for (int p0 = w * PAR + part; p0 - part < item.pieces; p0 += 8 * step) {
         float mp[8], lp[8];
         f32x4 op[8];
 #pragma unroll
@@ -1273,14 +1301,12 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
         const f32x4 other = {__shfl_xor(o[0], x), __shfl_xor(o[1], x), __shfl_xor(o[2], x), __shfl_xor(o[3], x)};
         add(__shfl_xor(m, x), __shfl_xor(l, x), other);
     }
-    if (a.by) {
-        if (part == 0) po[w][d / 4] = o;
-        if (lane == 0) pm[w] = m, pl[w] = l;
-        __syncthreads();
-        if (w) return;
+    if (part == 0) po[w][d / 4] = o;
+    if (lane == 0) pm[w] = m, pl[w] = l;
+    __syncthreads();
+    if (w) return;
 #pragma unroll
-        for (int x = 1; x < 4; ++x) add(pm[x], pl[x], po[x][d / 4]);
-    }
+    for (int x = 1; x < 4; ++x) add(pm[x], pl[x], po[x][d / 4]);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (part == 0) *(u32x2 *)(a.O + (size_t)at * HD + d) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
 }

@@ -1064,23 +1064,38 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
     set_knob(d, s, "waves", q.T > 4 ? 4 : q.T > 1 ? 2 : 1);
 }
 
+// Attention over sequences, whose lengths are on the device: by the rows that a
+// sequence has on average, and by the keys that it may have.  Fewer than 32 rows for
+// a K/V head (and with few rows in all) keys go straight to registers, a block of
+// 16 or 32 rows; where there may be more than 1024 keys, cut into pieces.  More
+// rows go through the ring: us, blocks of 128 rows with four waves (two
+// workgroups a CU), with eight, and of 64 rows with four and with eight (32 query
+// heads, 8 K/V heads of 128): prompts of 8192 tokens in all 150, 188, 192 and 238;
+// one of 2048 51, 47, 48 and 61, of 1000 28, 23, 22 and 24, of 512 17, 16, 13 and
+// 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22 and 19.  Few blocks with
+// many keys are cut: 512 rows over 8192 keys 74 (128 rows, four waves), 82 (64
+// rows, eight) where not.
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
+    const int64_t keys = q.page ? q.width * q.page : q.TK;
     auto set = [&](int bm, int waves, int stages, int occ, int splits) {
         set_knob(d, s, "block_m", bm), set_knob(d, s, "waves", waves), set_knob(d, s, "stages", stages);
         set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
         return check_schedule(d, s).empty();
     };
-    if (rows > 32 * q.B && rows > 256) {
+    if (rows >= 32 * q.B && rows >= 1024) {
         const int64_t items = q.Hkv * rows / 128;
-        const int bm = q.D < 256 && items >= 384 ? 128 : 64;
-        const int waves = items >= 1024 || (bm == 64 && items >= 192) ? 4 : 8;
-        if (set(bm, waves, 3, 2, items < 64 ? 1 : 0)) return;
+        const int most = q.D < 256 ? 128 : 64;
+        const bool cut = items < 512 && keys >= 4096;
+        if (cut && set(most, 4, 3, 2, 2)) return;
+        const int bm = items >= 384 ? most : 64;
+        if (set(bm, items >= 1024 || (bm == 64 && items >= 192) ? 4 : 8, 3, 2, 0)) return;
     }
-    for (int sp : {2, 0})
+    for (bool cut : {keys > 1024, false})
         for (int occ : {2, 1})
-            if (set(16, 4, 1, occ, sp)) return;
+            for (int bm : {rows > 16 * q.B ? 32 : 16, 16})
+                if (set(bm, 4, 1, occ, cut ? occ : 0)) return;
     set(16, 1, 1, 1, 0);
 }
 
@@ -1167,17 +1182,19 @@ static void all_rows_i8(const rc_op_desc *kind, Suggestions *out) {
 
 // The same of the kinds of attention in serving.
 static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
-    const bool cache = kind->kind == RC_OP_KV_WRITE || kind->kind == RC_OP_KV_READ;
     for (int64_t D : {64, 128, 256}) {         // (a definition of the kernels)
         Suggestions once;
-        for (int64_t T : {1, 2, 3, 5, 300, 8192, 24576, 49152, 1 << 20}) {
-            rc_op_desc d = *kind;
-            const int64_t dims[8] = {T, 1, 1, cache ? D : 1, cache ? 16 : d.kind == RC_OP_ATTENTION_PAGED ? D : 1,
-                                     cache || d.kind == RC_OP_ATTENTION_PAGED ? 16 : D, 1 << 16, 1 << 16};
-            for (int i = 0; i < expected_dims(d.kind); ++i) d.dim[i] = dims[i];
-            rc_schedule s;
-            if (rc_suggest_schedule(&d, &s) == RC_OK) list_once(&once, d, s);
-        }
+        // rows of one K/V head on either side of where the rules change, and keys
+        for (int64_t T : {1, 2, 3, 5, 17, 1024, 24576, 49152, 65536, 131072, 1 << 20})
+            for (int64_t keys : {16, 1 << 20}) {
+                const int64_t cache[] = {T, 1, 1, D, 16, 1, keys / 16}, paged[] = {T, 1, 1, 1, D, 16, 1, keys / 16};
+                const int64_t packed[] = {T, keys, 1, 1, 1, D};
+                rc_op_desc d = *kind;
+                const int64_t *dims = d.kind == RC_OP_ATTENTION_PAGED ? paged : d.kind == RC_OP_ATTENTION_PACKED ? packed : cache;
+                std::copy(dims, dims + expected_dims(d.kind), d.dim);
+                rc_schedule s;
+                if (rc_suggest_schedule(&d, &s) == RC_OK) list_once(&once, d, s);
+            }
         out->insert(out->end(), once.begin(), once.end());
     }
 }

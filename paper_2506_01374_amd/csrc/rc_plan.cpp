@@ -974,10 +974,9 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             // states of the pieces of cut blocks: fewer than two a workgroup that
             // the keys are cut for
             const size_t offP = sp ? ws.add((size_t)512 * sp * bm * (q.D + 2) * 4, "partials") : 0;
-            // the join: by blocks; by rows where a block has few, four waves a row
-            // where there are few rows, which have many pieces
-            const bool ring = kv(d, s, "stages") == 3;
-            const int by = q.T * q.H <= 4096;
+            // the join: by blocks, or by rows where there are few, which may have
+            // many pieces
+            const int by = kv(d, s, "stages") == 3 || q.T * q.H > 1536 ? 2 : 1;
             char scale[64];
             snprintf(scale, sizeof scale, "#define SCALE_LOG2 %.17gf\n", 1.4426950408889634 / std::sqrt((double)q.D));
             Kern k;
@@ -999,7 +998,7 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
                 Kern kj = k;
                 kj.flops = 0;
                 kj.src.entry = "rc_attention_seqs_join";
-                kj.grid = dim3((unsigned)(ring ? seqs_cut_blocks(d, bm, sp) * (bm * q.D / 2048) : by ? q.T * q.H : (q.T * q.H + 3) / 4), 1, 1);
+                kj.grid = dim3((unsigned)(by == 2 ? seqs_cut_blocks(d, bm, sp) * std::max<int64_t>(1, bm * q.D / 2048) : q.T * q.H), 1, 1);
                 kj.block = dim3(256, 1, 1);
                 p.kerns.push_back(kj);
             }
