@@ -210,3 +210,31 @@ def gemm_i8_inputs(M, N, K, bias=False, gated=False, seed=0):
         out["Bu"] = int_i8(seed, 66, (N, K))
         out["su"] = uniform_f32(seed, 67, (N,), 0.5 * scale, 1.5 * scale)
     return out
+
+
+def seqs_inputs(op, seed=0):
+    """Attention in serving, in the order of a launch: B sequences that share the
+    rows evenly and fill their part of the table (or of K's rows), with pages one
+    after the other; a sequence that would need more than there are has none."""
+    from . import rc
+    d, i8 = op.dims, op.flags & rc.RC_FLAG_I8_CACHE
+    if op.kind == rc.RC_OP_ATTENTION_PACKED:
+        T, TK, B, H, Hkv, D = d
+        share = lambda n: np.array([n * b // B for b in range(B + 1)], np.int32)
+        return {"Q": normal_bf16(seed, 71, (T, H, D)), "K": normal_bf16(seed, 72, (TK, Hkv, D)),
+                "V": normal_bf16(seed, 73, (TK, Hkv, D)), "offsets": share(T), "koffsets": share(TK)}
+    T, B = d[:2]
+    Hkv, D, page, pages, width = d[-5:]
+    table = np.arange(B * width, dtype=np.int32).reshape(B, width)
+    where = {"offsets": np.array([T * b // B for b in range(B + 1)], np.int32),
+             "lens": np.full(B, page * width, np.int32), "table": np.where(table < pages, table, -1).astype(np.int32)}
+    if op.kind == rc.RC_OP_KV_WRITE:
+        return {"k": normal_bf16(seed, 74, (T, Hkv, D)), "v": normal_bf16(seed, 75, (T, Hkv, D)), **where}
+    rows = {"Q": normal_bf16(seed, 71, (T, d[2], D))} if op.kind == rc.RC_OP_ATTENTION_PAGED else {}
+    shape = (pages, Hkv, page, D)
+    if i8:
+        cache = {"K": int_i8(seed, 76, shape), "V": int_i8(seed, 77, shape),
+                 "Ks": uniform_f32(seed, 78, shape[:3], 0.5 / 32, 1.5 / 32), "Vs": uniform_f32(seed, 79, shape[:3], 0.5 / 32, 1.5 / 32)}
+    else:
+        cache = {"K": normal_bf16(seed, 72, shape), "V": normal_bf16(seed, 73, shape)}
+    return {**rows, **cache, **where}

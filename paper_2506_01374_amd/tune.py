@@ -50,8 +50,9 @@ def reward_of(op: rc.Op, ms: float) -> float:
 
 
 def reference_schedule(name: str) -> str:
-    """A workload's tuned schedule, or an 8-bit one's suggested one."""
-    if name in W.I8_WORKLOADS:
+    """A workload's tuned schedule, or the suggested one of an 8-bit workload or
+    one of attention in serving."""
+    if name in W.I8_WORKLOADS or name in W.SEQS_WORKLOADS:
         return str(W.workload_op(name).suggest())
     with open(os.path.join(HERE, "tuned.json")) as f:
         return json.load(f)[name]
@@ -786,6 +787,19 @@ def schedule_features(op: rc.Op, sched: rc.Schedule) -> List[float]:
         T, C = D
         step = 64 * d["waves"] * d["vec"]
         f += [step, -(-C // step), -(-C // step) * step / C, -(-T // d["rows"]) / CUS, d["held"] * d["vec"]]
+    elif op.kind in (rc.RC_OP_KV_WRITE, rc.RC_OP_KV_READ):
+        # workgroups a compute unit, loads of a lane
+        f += [-(-D[0] // d["waves"]) / CUS, -(-2 * D[2] * D[3] // (64 * d["vec"]))]
+    elif op.kind in (rc.RC_OP_ATTENTION_PAGED, rc.RC_OP_ATTENTION_PACKED):
+        paged = op.kind == rc.RC_OP_ATTENTION_PAGED
+        T, B, H, Hkv, Dh = D[:5] if paged else D[:1] + D[2:]
+        keys = D[5] * D[7] if paged else D[1] / B
+        blocks = Hkv * B * -(-T * H // (Hkv * B * d["block_m"]))
+        groups = CUS * d["splits"]               # that the keys are cut for
+        bn = 32 if d["stages"] < 3 or Dh == 256 else 64
+        chain = min(keys, keys * blocks / groups) / bn if groups else keys / bn
+        f += [blocks / CUS, chain, chain / (d["waves"] if d["stages"] < 3 else d["waves"] / 4),
+              T * H / (Hkv * B * d["block_m"]), d["block_m"] * Dh / 64.0]
     return f
 
 
@@ -953,7 +967,7 @@ def _parse_seeds(text: str) -> List[int]:
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("--workload", required=True, choices=list(W.WORKLOADS) + list(W.I8_WORKLOADS))
+    ap.add_argument("--workload", required=True, choices=list(W.WORKLOADS) + list(W.I8_WORKLOADS) + list(W.SEQS_WORKLOADS))
     ap.add_argument("--policy", default="uct", choices=list(POLICIES) + ["list"])
     ap.add_argument("--budget", type=int, default=64)
     ap.add_argument("--seeds", default="0")

@@ -44,13 +44,25 @@ I8_WORKLOADS: Dict[str, Tuple[int, Tuple[int, ...], int]] = {
     "gated_i8_m2048_n14336_k4096": (rc.RC_OP_GEMM_I8, (2048, 14336, 4096), rc.RC_FLAG_GATED),
 }
 
+# Attention in serving (Llama-3-8B-style heads): tokens into a cache and back, a
+# step of 64 sequences over one, and four packed prompts.
+SEQS_WORKLOADS: Dict[str, Tuple[int, Tuple[int, ...], int]] = {
+    "kv_write_i8_t4096_h8_d128": (rc.RC_OP_KV_WRITE, (4096, 4, 8, 128, 64, 128, 32), rc.RC_FLAG_I8_CACHE),
+    "kv_read_i8_t4096_h8_d128": (rc.RC_OP_KV_READ, (4096, 4, 8, 128, 64, 128, 32), rc.RC_FLAG_I8_CACHE),
+    "attention_paged_b64_h32_kv8_d128_l2048": (rc.RC_OP_ATTENTION_PAGED, (64, 64, 32, 8, 128, 64, 2048, 32), rc.RC_FLAG_CAUSAL),
+    "attention_packed_b4_t8192_h32_kv8_d128": (rc.RC_OP_ATTENTION_PACKED, (8192, 8192, 4, 32, 8, 128), rc.RC_FLAG_CAUSAL),
+}
+
+
+SEQS_KINDS = (rc.RC_OP_KV_WRITE, rc.RC_OP_KV_READ, rc.RC_OP_ATTENTION_PAGED, rc.RC_OP_ATTENTION_PACKED)
+
 
 def op_for(kind: int, dims, flags: int = 0) -> rc.Op:
     return rc.Op(kind, dims, flags)
 
 
 def workload_op(name: str) -> rc.Op:
-    kind, dims, flags = WORKLOADS[name] if name in WORKLOADS else I8_WORKLOADS[name]
+    kind, dims, flags = {**WORKLOADS, **I8_WORKLOADS, **SEQS_WORKLOADS}[name]
     return rc.Op(kind, dims, flags)
 
 
@@ -74,6 +86,8 @@ def host_inputs(op: rc.Op, seed: int = 0) -> Dict[str, np.ndarray]:
     if op.kind == rc.RC_OP_GEMM_I8:
         return gen.gemm_i8_inputs(*d, bias=bool(op.flags & rc.RC_FLAG_BIAS), gated=bool(op.flags & rc.RC_FLAG_GATED),
                                   seed=seed)
+    if op.kind in SEQS_KINDS:
+        return gen.seqs_inputs(op, seed)
     raise ValueError(op.kind)
 
 
@@ -83,6 +97,12 @@ def output_shapes(op: rc.Op) -> List[Tuple[Tuple[int, ...], str]]:
     if op.kind in (rc.RC_OP_RMSNORM_I8, rc.RC_OP_QUANT_I8):
         outs = [(tuple(d), "int8"), ((d[0],), "float32")]
         return outs + [(tuple(d), "bfloat16")] if op.flags & rc.RC_FLAG_RESIDUAL else outs
+    if op.kind == rc.RC_OP_KV_WRITE:
+        T, B, Hkv, D, page, pages, width = d
+        i8 = op.flags & rc.RC_FLAG_I8_CACHE
+        return [((pages, Hkv, page, D), "int8" if i8 else "bfloat16")] * 2 + [((pages, Hkv, page), "float32")] * (2 if i8 else 0)
+    if op.kind == rc.RC_OP_KV_READ:
+        return [((d[0], d[2], d[3]), "bfloat16")] * 2
     return [output_shape(op)]
 
 
@@ -98,6 +118,10 @@ def output_shape(op: rc.Op) -> Tuple[Tuple[int, ...], str]:
         return (d[0], d[1]), "bfloat16"
     if op.kind == rc.RC_OP_GEMM_I8:
         return (d[0], d[1]), "float32" if op.flags & rc.RC_FLAG_OUT_F32 else "bfloat16"
+    if op.kind == rc.RC_OP_ATTENTION_PAGED:
+        return (d[0], d[2], d[4]), "bfloat16"
+    if op.kind == rc.RC_OP_ATTENTION_PACKED:
+        return (d[0], d[3], d[5]), "bfloat16"
     if op.kind != rc.RC_OP_CONV2D:
         raise ValueError("an operator of several outputs: see output_shapes")
     N, H, W, C, K, R, S, pad = d
@@ -131,6 +155,8 @@ def stored_inputs(op: rc.Op, sched: rc.Schedule, host: Dict[str, np.ndarray]) ->
         return [host[n] for n in ("x", "w", "r") if n in host]
     if op.kind == rc.RC_OP_GEMM_I8:
         return [host[n] for n in ("A", "sa", "B", "sb", "bias", "Bu", "su") if n in host]
+    if op.kind in SEQS_KINDS:
+        return list(host.values())
     raise ValueError(op.kind)
 
 
