@@ -5,12 +5,12 @@
 //
 // Compile-time schedule (generated prologue):
 //   BM      rows of a work item (TileSize), see below
-//   NW      waves that share an item's keys (Parallel)
-//   STAGES  1: a tile is loaded, then computed; 2: the next tile's loads are
-//           under way meanwhile; 3: tiles go through a ring in shared memory,
-//           and two halves of the waves take turns on the matrix cores
-//           (ComputeLocation)
-//   OCC     waves per SIMD the register allocation must leave room for
+//   NW      waves of a workgroup (Parallel)
+//   STAGES  keys and values go straight to registers, and 1: a tile is loaded,
+//           then computed, 2: the next tile's loads are under way meanwhile; 3:
+//           they go through a ring in shared memory (ComputeLocation)
+//   OCC     waves per SIMD the register allocation must leave room for (with
+//           the ring two)
 //   SPLIT   1: the keys of a sequence are cut into pieces for several
 //           workgroups, whose states rc_attention_seqs_join puts together
 //   HD      head dimension: 64, 128 or 256
@@ -225,6 +225,11 @@ __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f3
 // up with a byte permute, and the e-th of DE instructions takes the channels
 // DE i + e as its 16 rows.  The keys of a lane are those of its scores (4 (lane
 // / 16) + r of each 16), so that P^T stays where it is.
+//
+// Bound by the cache's bytes where there are many, by the way to memory (lengths,
+// table, tile) else: 64 rows over bf16 caches of 64 to 8192 tokens, 8 K/V heads of
+// 128, 87 us (4.7 TB/s), over int8 ones 48 (4.4; a byte takes 1.5 vector
+// instructions of a lane to widen); one row over 32768 tokens 25 (5.4).
 
 // Values that are not finite, in a tile that some row does not see whole: 0 times
 // one is a NaN.  O += V^T P^T takes them as 0, and +-1 in their place (a NaN both)
@@ -564,11 +569,16 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // Keys and values through shared memory, in turns (STAGES 3)
 // ---------------------------------------------------------------------------
 //
-// Eight waves: four of 16 QB rows each for the even key tiles of the piece, and
-// four for the odd ones, with their own softmax states, put together at the
-// end.  Waves w and w + 4 share a SIMD and take turns on its matrix cores: while
-// one multiplies (O^T += V^T P^T of its tile, then S^T = K Q^T of its next),
-// the other does its softmax (vector work); a barrier ends each turn.  K and V
+// Four waves of 16 QB rows each, or eight: four for the even key tiles of the
+// piece, and four for the odd ones, with their own softmax states, put together
+// at the end.  Waves w and w + 4 share a SIMD and take turns on its matrix cores:
+// while one multiplies (O^T += V^T P^T of its tile, then S^T = K Q^T of its next),
+// the other does its softmax (vector work); a barrier ends each turn.  Four waves
+// alternate the same turns, two workgroups a CU, which fall out of step by
+// themselves and fill each other's starts and ends, 17000 cycles a block (8
+// prompts of 8192 tokens in all, 32 heads of 128: 150 us, with eight waves 188);
+// eight are for few blocks, each of them done sooner (64 rows, 8 sequences: 19 and
+// 22).  K and V
 // go straight from memory to shared memory, into a ring of two tiles for each
 // operand and half of the waves; the softmax turn issues the loads between its
 // exponentials, K of the tile after the next and V of the next, into the places
@@ -580,6 +590,13 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // has loaded to bf16 (exactly) and writes it, K of the next tile and V of this
 // one, so that one place for each is enough.  K's scale is multiplied into the
 // scores, V's into the probabilities.
+//
+// Bound by the issue of vector and matrix instructions together, at a clock that
+// the power limits: a prompt of 16384 tokens, 32 heads of 128, 1.83 ms (1.20
+// PFLOP/s), matrix cores busy 51 % of the time at 1.87 GHz.  Over an int8 cache by
+// vector instructions, a third of which widen (512 rows over 8192 tokens 109 us, over
+// bf16 75).  Slower were: loads issued by the matrix turn (1972 -> 2147 us), V read
+// by 16 bytes and paired by permutes (7 % more), the matrix turn without priority.
 
 #if STAGES == 3
 #define ROWG 4                     // groups of rows
@@ -947,12 +964,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         const float y = (x[0] + x[1]) + (x[2] + x[3]);
         return __builtin_amdgcn_ballot_w64(y != y) != 0;
     };
-    // The softmax turn of tile `it` after its row maximum, in KB x QB groups of
-    // exponentials with a share of the loads in each; a turn that loads the
-    // sequence's last, partial tile issues its loads first
 #if I8
-    // (int8: the values' scales are multiplied in; where some row does not see a
-    // key, its scale may be anything)
+    // The softmax of tile `it`.  The values' scales are multiplied in; where some
+    // row does not see a key, its scale may be anything.
     auto scaled = [&](int it, bool some, Probs &pf) __attribute__((always_inline)) {
         // (the scores of a tile that some row does not see whole have their
         // scales, and the mask, already)
@@ -1012,7 +1026,11 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         pf[kb / 2][b] = __builtin_bit_cast(bf16x8, w);
         return x | y;
     };
+    // does one of two probabilities in `bits` have the exponent's top bit?
     auto past = [&](u32 bits) __attribute__((always_inline)) { return __builtin_amdgcn_ballot_w64((bits & 0x40004000u) != 0) != 0; };
+    // The softmax turn of tile `it`, in KB x QB groups of exponentials with a share
+    // of the loads in each; a turn that loads the sequence's last, partial tile
+    // issues its loads first
     auto exps = [&](int it, auto act, Probs &pf) __attribute__((always_inline)) {
         u32 bits[QB] = {};
         const From kn = rows_of(it + 2), vn = next;
@@ -1224,10 +1242,10 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 //
 // A lane takes 4 channels.  By blocks (`by` 2): a workgroup takes the pieces of 2048
 // / HD rows of a block, four or eight at once.  By rows, where there are few, which
-// may have many pieces: a workgroup takes a row (1), a lane every 1024 / HD-th
-// piece, eight at once.  The time is that of the way to
-// memory and back, and for large blocks of their states (26 MB of 200 blocks of
-// 128 rows in two pieces).
+// may have many pieces (`by` 1): a workgroup takes a row, a lane every 1024 / HD-th
+// piece, eight at once.  The time is that of the way to memory and back, 6 us, and
+// for large blocks of their states (26 MB of 200 blocks of 128 rows in two pieces,
+// 10 us).
 #if SPLIT
 extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArgs a) {
     __shared__ f32x4 po[4][HD / 4];

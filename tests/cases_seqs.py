@@ -30,7 +30,8 @@ PACKED_CASES = [
 CACHE_TEXTS = ["", "vec=8", "waves=4,vec=8"]
 ATTENTION_TEXTS = ["", "block_m=32", "waves=4", "block_m=32,waves=2,splits=1", "waves=4,splits=2",
                    "block_m=64,waves=8,stages=3,occ=2", "block_m=128,waves=8,stages=3,occ=2,splits=1", "block_m=64,waves=8,stages=3,occ=2,splits=4",
-                   "stages=2,waves=2,occ=1,splits=1", "stages=1,waves=4,occ=2,splits=2"]
+                   "stages=2,waves=2,occ=1,splits=1", "stages=1,waves=4,occ=2,splits=2",
+                   "block_m=64,waves=4,stages=3,occ=2", "block_m=128,waves=4,stages=3,occ=2,splits=2"]
 
 
 def cache_op(kind, case, flags, pages=None):

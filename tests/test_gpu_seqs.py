@@ -480,6 +480,120 @@ def test_offsets_and_lengths_that_make_no_sense_stay_in_bounds():
             run_write(wr, str(wr.suggest()), [kv, kv], [ints(offsets), ints(lens), ints(table)], cache)
 
 
+@pytest.mark.parametrize("flags", [C, I8 | C])
+@pytest.mark.parametrize("case", [([1], [9000], 1, 4, 64, 16), ([1] * 40, [700 + 61 * i for i in range(40)], 2, 16, 64, 16),
+                                  ([90, 1, 0, 1], [2500, 4000, 5, 31], 2, 8, 64, 64)])
+def test_many_pieces(case, flags):
+    # one row, joined by rows; 1280 and 2944 rows' pieces: by rows and by blocks
+    q, lens, hkv, g, d, page = case
+    op = S.paged_op(case, flags)
+    rows, cache, table = paged_inputs(case, flags & I8, 21)
+    keys, _ = keys_of(cache, table, lens, page, flags & I8)
+    want, tol = reference(q, lens, f64(rows), keys, True, d ** -0.5)
+    for text in S.legal(op, ["waves=4,splits=2", "waves=1,splits=4", "block_m=64,waves=8,stages=3,occ=2,splits=4",
+                             "block_m=128,waves=4,stages=3,occ=2,splits=2"]):
+        check(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]), want, tol)
+
+
+def test_thousands_of_sequences():
+    r = np.random.default_rng(30)
+    q = r.integers(0, 3, 5000).tolist()
+    lens = [n + int(m) for n, m in zip(q, r.integers(0, 20, 5000))]
+    q[4321], lens[4321], q[70], lens[70] = 100, 400, 40, 40
+    case = (q, lens, 1, 2, 64, 16)
+    op = S.paged_op(case, C)
+    rows, cache, table = paged_inputs(case, 0, 31)
+    keys, _ = keys_of(cache, table, lens, 16, 0)
+    want, tol = reference(q, lens, f64(rows), keys, True, 64 ** -0.5)
+    for text in S.legal(op, ["", "waves=4,splits=2", "block_m=128,waves=4,stages=3,occ=2,splits=2"]):
+        check(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]), want, tol)
+
+
+def test_sequences_that_share_pages():
+    # the same first pages in two tables, and one page twice in a table
+    case = ([3, 40], [40, 75], 2, 4, 128, 16)
+    q, lens, hkv, g, d, page = case
+    op = S.paged_op(case, C)
+    rows, cache, table = paged_inputs(case, 0, 33)
+    table[1, :2], table[1, 3] = table[0, :2], table[1, 2]
+    keys, _ = keys_of(cache, table, lens, page, 0)
+    want, tol = reference(q, lens, f64(rows), keys, True, d ** -0.5)
+    for text in S.legal(op, S.ATTENTION_TEXTS):
+        check(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]), want, tol)
+
+
+@pytest.mark.parametrize("i8", [0, I8])
+def test_a_cache_past_32_bits(i8):
+    # pages on both sides of 2^32 elements of K and of V; what is in no page that
+    # the table names is not initialised
+    hkv, g, d, page, pages, q, lens = 8, 2, 128, 64, 66000, [300, 1], [330, 1000]
+    assert pages * hkv * page * d > 2 ** 32
+    ids = [pages - 1 - i for i in range(12)] + list(range(10))
+    table = np.full((2, 16), -1, np.int64)
+    table[0, :6], table[1, :16] = ids[:6], ids[6:]
+    dims = (301, 2, hkv, d, page, pages, 16)
+    r = np.random.default_rng(40)
+    cache = [torch.empty(pages, hkv, page, d, dtype=torch.int8 if i8 else torch.bfloat16, device="cuda") for _ in range(2)]
+    if i8:
+        cache += [torch.empty(pages, hkv, page, device="cuda") for _ in range(2)]
+    where = [ints(starts(lens)).cuda(), ints(lens).cuda(), ints(table).cuda()]
+    kv = [bf16(r.standard_normal((sum(lens), hkv, d))).cuda() for _ in range(2)]
+    for kind, ins, out in ((rc.RC_OP_KV_WRITE, kv, cache), (rc.RC_OP_KV_READ, cache, [torch.zeros_like(x) for x in kv])):
+        op = rc.Op(kind, (sum(lens),) + dims[1:], i8)
+        print(f"[gpu] kind={kind} dims={op.dims} flags={i8}", flush=True)
+        rc.Plan(op, op.suggest()).launch(ins + where, tuple(out))
+        torch.cuda.synchronize()
+    want = [f64(x) for x in kv]
+    if i8:
+        want = [y * s.astype(np.float64)[..., None] for y, s in map(quantised, want)]
+    for x, y in zip(out, want):
+        assert same(x, f64(bf16(y)))
+    at = starts(lens)
+    keys = [[x[at[b]:at[b + 1]] for x in want] for b in range(2)]
+    rows = bf16(r.standard_normal((301, hkv * g, d)))
+    op = rc.Op(rc.RC_OP_ATTENTION_PAGED, (301, 2, hkv * g, hkv, d, page, pages, 16), i8 | C)
+    want, tol = reference(q, lens, f64(rows), keys, True, d ** -0.5)
+    for text in S.legal(op, ["waves=4,splits=2", "block_m=64,waves=8,stages=3,occ=2,splits=4",
+                             "block_m=128,waves=4,stages=3,occ=2,splits=2"]):
+        print(f"[gpu] paged dims={op.dims} flags={op.flags} sched={text}", flush=True)
+        plan, got = rc.Plan(op, op.from_string(text)), torch.empty(301, hkv * g, d, dtype=torch.bfloat16, device="cuda")
+        plan.launch([rows.cuda()] + cache + [ints(starts(q)).cuda()] + where[1:], got, plan.workspace())
+        torch.cuda.synchronize()
+        check(got, want, tol)
+
+
+def test_one_plan_on_two_streams():
+    case = ([1] * 6, [3000, 1, 500, 64, 2000, 77], 2, 4, 64, 16)
+    q, lens, hkv, g, d, page = case
+    op = S.paged_op(case, C)
+    plan = rc.Plan(op, op.suggest())
+    assert plan.workspace_bytes > 0
+    sets, streams = [paged_inputs(case, 0, 50 + i) for i in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    dev = [[x.cuda() for x in [rows] + cache + [ints(starts(q)), ints(lens), ints(table)]] for rows, cache, table in sets]
+    outs, ws = [torch.empty_like(x[0]) for x in dev], [plan.workspace() for _ in dev]
+    torch.cuda.synchronize()
+    for i in (0, 1) * 3:
+        plan.launch(dev[i], outs[i], ws[i], streams[i])
+    torch.cuda.synchronize()
+    for (rows, cache, table), out in zip(sets, outs):
+        keys, _ = keys_of(cache, table, lens, page, 0)
+        check(out, *reference(q, lens, f64(rows), keys, True, d ** -0.5))
+
+
+def test_launch_without_allocation():
+    case = ([5, 1, 20], [40, 33, 20], 2, 4, 64, 16)
+    q, lens, hkv, g, d, page = case
+    op = S.paged_op(case, C)
+    rows, cache, table = paged_inputs(case, 0, 60)
+    ins = [x.cuda() for x in [rows] + cache + [ints(starts(q)), ints(lens), ints(table)]]
+    plan = rc.Plan(op, op.from_string("waves=4"))
+    outs = [torch.empty_like(ins[0]) for _ in range(2)]
+    plan.launch(ins, outs[0], plan.workspace())
+    plan.launch_static(ins, outs[1])
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+
+
 # ---------------------------------------------------------------------------
 # The operators together
 # ---------------------------------------------------------------------------
