@@ -1075,7 +1075,15 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 // one of 2048 51, 47, 48 and 61, of 1000 28, 23, 22 and 24, of 512 17, 16, 13 and
 // 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22 and 19.  Few blocks with
 // many keys are cut: 512 rows over 8192 keys 74 (128 rows, four waves), 82 (64
-// rows, eight) where not.
+// rows, eight) where not.  Sequences of 17 to 64 rows whose bf16 keys are cut, and
+// whose blocks of 32 rows leave no registers for two waves a SIMD, go through the
+// ring in blocks of 64 too: 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4
+// in blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 48 of D = 256 and 3000 keys
+// 29 and 32 (one of 400 rows with 15 of 4 rows 36 and 34); 32 of 32 rows and up to
+// 8192 keys 24 (27 in blocks of 128).  With D = 64, or of int8, blocks of 32 take
+// less: 16.2 and 19.3, 27.5 and 38.  Up to 64 rows of a sequence over int8 keys that
+// are cut go through the ring with four waves: 16 sequences of 64 rows and 5000 keys
+// 71 (78 with eight, 76 in blocks of 128).
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
@@ -1085,14 +1093,17 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
         set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
         return check_schedule(d, s).empty();
     };
-    if (rows >= 32 * q.B && rows >= 1024) {
+    const bool i8 = d->flags & RC_FLAG_I8_CACHE;
+    if (rows > (i8 ? 32 : 31) * q.B && rows >= 1024) {
         const int64_t items = q.Hkv * rows / 128;
         const int most = q.D < 256 ? 128 : 64;
         const bool cut = items < 512 && keys >= 4096;
+        if (cut && rows <= 64 * q.B && (i8 ? set(64, 4, 3, 2, 2) : set(64, 8, 3, 2, 1))) return;
         if (cut && set(most, 4, 3, 2, 2)) return;
         const int bm = items >= 384 ? most : 64;
         if (set(bm, items >= 1024 || (bm == 64 && items >= 192) ? 4 : 8, 3, 2, 0)) return;
     }
+    if (keys > 1024 && rows > 16 * q.B && q.D > 64 && !i8 && set(64, 8, 3, 2, 1)) return;
     for (bool cut : {keys > 1024, false})
         for (int occ : {2, 1})
             for (int bm : {rows > 16 * q.B ? 32 : 16, 16})
@@ -1185,11 +1196,13 @@ static void all_rows_i8(const rc_op_desc *kind, Suggestions *out) {
 static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
     for (int64_t D : {64, 128, 256}) {         // (a definition of the kernels)
         Suggestions once;
-        // rows of one K/V head on either side of where the rules change, and keys
-        for (int64_t T : {1, 2, 3, 5, 17, 1024, 24576, 49152, 65536, 131072, 1 << 20})
-            for (int64_t keys : {16, 1 << 20}) {
-                const int64_t cache[] = {T, 1, 1, D, 16, 1, keys / 16}, paged[] = {T, 1, 1, 1, D, 16, 1, keys / 16};
-                const int64_t packed[] = {T, keys, 1, 1, 1, D};
+        // rows of one K/V head on either side of where the rules change, of one and
+        // of many sequences, and keys
+        for (int64_t T : {1, 2, 3, 5, 17, 40, 1024, 24576, 49152, 65536, 131072, 1 << 20})
+            for (int64_t i : {0, 1, 2, 3}) {
+                const int64_t keys = i & 1 ? 1 << 20 : 16, B = i & 2 ? (T + 39) / 40 : 1;
+                const int64_t cache[] = {T, B, 1, D, 16, 1, keys / 16}, paged[] = {T, B, 1, 1, D, 16, 1, keys / 16};
+                const int64_t packed[] = {T, keys, B, 1, 1, D};
                 rc_op_desc d = *kind;
                 const int64_t *dims = d.kind == RC_OP_ATTENTION_PAGED ? paged : d.kind == RC_OP_ATTENTION_PACKED ? packed : cache;
                 std::copy(dims, dims + expected_dims(d.kind), d.dim);
