@@ -1066,24 +1066,32 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 }
 
 // Attention over sequences, whose lengths are on the device: by the rows that a
-// sequence has on average, and by the keys that it may have.  Fewer than 32 rows for
-// a K/V head (and with few rows in all) keys go straight to registers, a block of
-// 16 or 32 rows; where there may be more than 1024 keys, cut into pieces.  More
-// rows go through the ring: us, blocks of 128 rows with four waves (two
-// workgroups a CU), with eight, and of 64 rows with four and with eight (32 query
-// heads, 8 K/V heads of 128): prompts of 8192 tokens in all 150, 188, 192 and 238;
-// one of 2048 51, 47, 48 and 61, of 1000 28, 23, 22 and 24, of 512 17, 16, 13 and
-// 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22 and 19.  Few blocks with
-// many keys are cut: 512 rows over 8192 keys 74 (128 rows, four waves), 82 (64
-// rows, eight) where not.  Sequences of 17 to 64 rows whose bf16 keys are cut, and
-// whose blocks of 32 rows leave no registers for two waves a SIMD, go through the
-// ring in blocks of 64 too: 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4
-// in blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 48 of D = 256 and 3000 keys
-// 29 and 32 (one of 400 rows with 15 of 4 rows 36 and 34); 32 of 32 rows and up to
-// 8192 keys 24 (27 in blocks of 128).  With D = 64, or of int8, blocks of 32 take
-// less: 16.2 and 19.3, 27.5 and 38.  Up to 64 rows of a sequence over int8 keys that
-// are cut go through the ring with four waves: 16 sequences of 64 rows and 5000 keys
-// 71 (78 with eight, 76 in blocks of 128).
+// sequence has on average, and by the keys that it may have.
+// Few rows: keys go straight to registers, blocks of 16 or 32 rows; where there may
+// be more than 1024 keys, cut into pieces.  Sequences of 17 rows or more whose bf16
+// keys are cut, and whose blocks of 32 rows leave no registers for two waves a SIMD,
+// go through the ring in blocks of 64 (us): 16 sequences of 20 rows and up to 8192
+// keys 25.7, 32.4 in blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 48 of D = 256
+// and 3000 keys 29 and 32 (one of 400 rows with 15 of 4 rows 36 and 34); with D = 64,
+// or of int8, blocks of 32 take less: 16.2 and 19.3, 27.5 and 38.
+// More rows: the ring.  `items` is the number of blocks of 128 rows.  Few of them with
+// keys enough are cut for two workgroups of four waves a CU: 64 and 8192 keys 77
+// (uncut, 8 waves, 82), 75 and 5000 of D = 64 37 (41); int8 keys, and D = 256, take
+// about twice as long, so that shorter ones are: 75 and 2048 of int8 44 (52), 150 and
+// 2300 56 (94), 225 and 3000 83 (90), but 300 and 2300 105 (97); 54 and 2038 of D =
+// 256 34 (48), 75 and 2300 48 (53), 112 58 (55), 112 and 5000 102 (115), 200 173
+// (166).  D = 128 without int8, 225 and 5000 take 87 (77), 450 139 (126).  Sequences
+// of up to 64 rows are cut in blocks of 64: 32 of 32 rows and up to 8192 keys 24 with
+// eight waves (27 in blocks of 128), over int8 keys with four, 16 of 64 rows and 5000
+// keys 67 (78 with eight, 76 in blocks of 128).
+// Uncut blocks of 128 rows with four waves (two workgroups a CU), with eight, and of
+// 64 rows with four and with eight: 2048 items of prompts of 8192 tokens 150, 188,
+// 192 and 238; a prompt with 512 items 51, 47, 48 and 61, with 250 28, 23, 22 and 24,
+// with 128 17, 16, 13 and 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22
+// and 19; 225 items and 5000 keys 107, 77, 91 and 104; of int8, 300 and 2300 95, 97,
+// 98 and 125, 450 and 6000 238, 284, 342 and 446, 375 and 1500 65, 54, 53 and 78.  D =
+// 256 has blocks of 64 alone, four waves and eight: 112 items 80 and 57, 256 71 and
+// 59, 512 164 and 195, of int8 200 271 and 316.
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
@@ -1093,15 +1101,17 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
         set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
         return check_schedule(d, s).empty();
     };
-    const bool i8 = d->flags & RC_FLAG_I8_CACHE;
+    const bool i8 = d->flags & RC_FLAG_I8_CACHE, wide = q.D == 256;
     if (rows > (i8 ? 32 : 31) * q.B && rows >= 1024) {
         const int64_t items = q.Hkv * rows / 128;
-        const int most = q.D < 256 ? 128 : 64;
-        const bool cut = items < 512 && keys >= 4096;
-        if (cut && rows <= 64 * q.B && (i8 ? set(64, 4, 3, 2, 2) : set(64, 8, 3, 2, 1))) return;
-        if (cut && set(most, 4, 3, 2, 2)) return;
-        const int bm = items >= 384 ? most : 64;
-        if (set(bm, items >= 1024 || (bm == 64 && items >= 192) ? 4 : 8, 3, 2, 0)) return;
+        const int64_t few = wide ? (keys >= 4096 ? 160 : 96) : i8 ? 256 : 192;
+        if (items < few && keys * (wide ? 2 : 1) * (i8 ? 2 : 1) >= 4096) {
+            if (rows <= 64 * q.B && (i8 ? set(64, 4, 3, 2, 2) : set(64, 8, 3, 2, 1))) return;
+            if (set(wide ? 64 : 128, 4, 3, 2, 2)) return;
+        }
+        const int bm = !wide && items >= (keys >= 2048 ? 192 : 384) ? 128 : 64;
+        const int four = wide ? (i8 ? 192 : 384) : bm == 64 ? 192 : i8 && keys >= 2048 ? 256 : 1024;      // items with four waves
+        if (set(bm, items >= four ? 4 : 8, 3, 2, 0)) return;
     }
     if (keys > 1024 && rows > 16 * q.B && q.D > 64 && !i8 && set(64, 8, 3, 2, 1)) return;
     for (bool cut : {keys > 1024, false})
@@ -1198,7 +1208,7 @@ static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
         Suggestions once;
         // rows of one K/V head on either side of where the rules change, of one and
         // of many sequences, and keys
-        for (int64_t T : {1, 2, 3, 5, 17, 40, 1024, 24576, 49152, 65536, 131072, 1 << 20})
+        for (int64_t T : {1, 2, 3, 5, 17, 40, 1024, 24576, 32768, 49152, 65536, 131072, 1 << 20})
             for (int64_t i : {0, 1, 2, 3}) {
                 const int64_t keys = i & 1 ? 1 << 20 : 16, B = i & 2 ? (T + 39) / 40 : 1;
                 const int64_t cache[] = {T, B, 1, D, 16, 1, keys / 16}, paged[] = {T, B, 1, 1, D, 16, 1, keys / 16};
