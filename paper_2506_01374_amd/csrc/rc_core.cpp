@@ -1068,12 +1068,19 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 // Attention over sequences, whose lengths are on the device: by the rows that a
 // sequence has on average, and by the keys that it may have.
 // Few rows: keys go straight to registers, blocks of 16 or 32 rows; where there may
-// be more than 1024 keys, cut into pieces.  Sequences of 17 rows or more whose bf16
-// keys are cut, and whose blocks of 32 rows leave no registers for two waves a SIMD,
-// go through the ring in blocks of 64 (us): 16 sequences of 20 rows and up to 8192
-// keys 25.7, 32.4 in blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 48 of D = 256
-// and 3000 keys 29 and 32 (one of 400 rows with 15 of 4 rows 36 and 34); with D = 64,
-// or of int8, blocks of 32 take less: 16.2 and 19.3, 27.5 and 38.
+// be more than 1024 keys (512 of D = 256: 16 sequences of 900 19 us, 24 uncut), cut
+// into pieces.  Four waves share a piece, eight with int8 and D = 256, whose registers
+// leave room for one workgroup of four a CU (64 sequences of up to 4096 keys 76 and
+// 90 us, 8 of 8000 34 and 35).  Sequences of 17 rows or more whose keys are cut, and
+// whose blocks of 32 rows leave no registers for two waves a SIMD, go through the ring
+// in blocks of 64 (us): 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4 in
+// blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 8 of D = 256, 24 rows and 3000
+// keys 29 and 32, of 40 rows and 6000 int8 keys 38 and 51 (one of 400 rows with 15 of
+// 4 rows 36 and 34; 10 of 31 rows and 31 to 3200 keys of 2 heads 20 and 13); with D =
+// 64, or of int8 otherwise, blocks of 32 take less: 16.2 and 19.3, 27.5 and 38.  Up to
+// 512 blocks of 16 rows with few keys stay as they are: 64 items of a prompt of 256
+// 8.8 (ring 9.8), 7 prompts of 100 6.6 (9.1), 600 tokens of one head 9.9 (12.3), but
+// 1000 with three shorter prompts 18 (16).
 // More rows: the ring.  `items` is the number of blocks of 128 rows.  Few of them with
 // keys enough are cut for two workgroups of four waves a CU: 64 and 8192 keys 77
 // (uncut, 8 waves, 82), 75 and 5000 of D = 64 37 (41); int8 keys, and D = 256, take
@@ -1088,21 +1095,24 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 // 64 rows with four and with eight: 2048 items of prompts of 8192 tokens 150, 188,
 // 192 and 238; a prompt with 512 items 51, 47, 48 and 61, with 250 28, 23, 22 and 24,
 // with 128 17, 16, 13 and 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22
-// and 19; 225 items and 5000 keys 107, 77, 91 and 104; of int8, 300 and 2300 95, 97,
-// 98 and 125, 450 and 6000 238, 284, 342 and 446, 375 and 1500 65, 54, 53 and 78.  D =
-// 256 has blocks of 64 alone, four waves and eight: 112 items 80 and 57, 256 71 and
-// 59, 512 164 and 195, of int8 200 271 and 316.
+// and 19; 4 prompts of 512 25, 32, 27 and 37, 64 of 128 60, 102, 73 and 129; 225 items
+// and 5000 keys 107, 77, 91 and 104; of int8, 300 and 2300 95, 97, 98 and 125, 450 and
+// 6000 238, 284, 342 and 446, 375 and 1500 65, 54, 53 and 78.  D = 256 has blocks of
+// 64 alone, four waves and eight: 112 items 80 and 57, 256 71 and 59, 512 164 and 195,
+// of int8 200 271 and 316.
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
-    const int64_t keys = q.page ? q.width * q.page : q.TK;
+    const int64_t keys = q.page ? q.width * q.page : q.TK / q.B;
     auto set = [&](int bm, int waves, int stages, int occ, int splits) {
         set_knob(d, s, "block_m", bm), set_knob(d, s, "waves", waves), set_knob(d, s, "stages", stages);
         set_knob(d, s, "occ", occ), set_knob(d, s, "splits", splits);
         return check_schedule(d, s).empty();
     };
     const bool i8 = d->flags & RC_FLAG_I8_CACHE, wide = q.D == 256;
-    if (rows > (i8 ? 32 : 31) * q.B && rows >= 1024) {
+    const int64_t short_blocks = q.Hkv * rows / 16;
+    const bool brief = !wide && short_blocks <= 512 && short_blocks * keys <= 1 << 17;
+    if (rows > (i8 ? 32 : 31) * q.B && rows >= 1024 && !brief) {
         const int64_t items = q.Hkv * rows / 128;
         const int64_t few = wide ? (keys >= 4096 ? 160 : 96) : i8 ? 256 : 192;
         if (items < few && keys * (wide ? 2 : 1) * (i8 ? 2 : 1) >= 4096) {
@@ -1110,14 +1120,15 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
             if (set(wide ? 64 : 128, 4, 3, 2, 2)) return;
         }
         const int bm = !wide && items >= (keys >= 2048 ? 192 : 384) ? 128 : 64;
-        const int four = wide ? (i8 ? 192 : 384) : bm == 64 ? 192 : i8 && keys >= 2048 ? 256 : 1024;      // items with four waves
+        const int four = wide ? (i8 ? 192 : 384) : bm == 64 ? 192 : keys < 2048 ? 384 : i8 ? 256 : 1024;      // items with four waves
         if (set(bm, items >= four ? 4 : 8, 3, 2, 0)) return;
     }
-    if (keys > 1024 && rows > 16 * q.B && q.D > 64 && !i8 && set(64, 8, 3, 2, 1)) return;
-    for (bool cut : {keys > 1024, false})
+    if (keys > 1024 && rows > 16 * q.B && (wide || (q.D > 64 && !i8)) && q.Hkv * q.B * keys >= (wide ? 1 << 16 : 1 << 18))
+        if (set(64, 8, 3, 2, 1)) return;
+    for (bool cut : {keys * (wide ? 2 : 1) > 1024, false})
         for (int occ : {2, 1})
             for (int bm : {rows > 16 * q.B ? 32 : 16, 16})
-                if (set(bm, 4, 1, occ, cut ? occ : 0)) return;
+                if (set(bm, wide && i8 ? 8 : 4, 1, occ, cut ? occ : 0)) return;
     set(16, 1, 1, 1, 0);
 }
 
@@ -1208,7 +1219,7 @@ static void all_seqs(const rc_op_desc *kind, Suggestions *out) {
         Suggestions once;
         // rows of one K/V head on either side of where the rules change, of one and
         // of many sequences, and keys
-        for (int64_t T : {1, 2, 3, 5, 17, 40, 1024, 24576, 32768, 49152, 65536, 131072, 1 << 20})
+        for (int64_t T : {1, 2, 3, 5, 17, 40, 1024, 12288, 24576, 32768, 49152, 65536, 131072, 1 << 20})
             for (int64_t i : {0, 1, 2, 3}) {
                 const int64_t keys = i & 1 ? 1 << 20 : 16, B = i & 2 ? (T + 39) / 40 : 1;
                 const int64_t cache[] = {T, B, 1, D, 16, 1, keys / 16}, paged[] = {T, B, 1, 1, D, 16, 1, keys / 16};
