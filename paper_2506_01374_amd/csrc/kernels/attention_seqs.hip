@@ -576,27 +576,30 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // the other does its softmax (vector work); a barrier ends each turn.  Four waves
 // alternate the same turns, two workgroups a CU, which fall out of step by
 // themselves and fill each other's starts and ends, 17000 cycles a block (8
-// prompts of 8192 tokens in all, 32 heads of 128: 150 us, with eight waves 188);
+// prompts of 8192 tokens in all, 32 heads of 128: 152 us, with eight waves 188);
 // eight are for few blocks, each of them done sooner (64 rows, 8 sequences: 19 and
-// 22).  K and V
-// go straight from memory to shared memory, into a ring of two tiles for each
-// operand and half of the waves; the softmax turn issues the loads between its
+// 22).
+// K and V go straight from memory to shared memory, into a ring of two tiles for
+// each operand and half of the waves; the softmax turn issues the loads between its
 // exponentials, K of the tile after the next and V of the next, into the places
-// that the matrix turn before it has read, and waits for those of the softmax
-// turn before.  16-byte chunks of a row are XOR-ed with the row's number (KSWZ,
-// VSWZ), by the choice of what a lane fetches, so that fragment reads have no
-// bank conflicts; V's are transposed by the reading instruction.
+// that the matrix turn before it has read, and waits for those of the softmax turn
+// before.  16-byte chunks of a row are XOR-ed with the row's number (KSWZ, VSWZ),
+// by the choice of what a lane fetches, so that fragment reads have no bank
+// conflicts; V's are transposed by the reading instruction.
 // An int8 tile goes through registers: a softmax turn widens what the one before
 // has loaded to bf16 (exactly) and writes it, K of the next tile and V of this
 // one, so that one place for each is enough.  K's scale is multiplied into the
 // scores, V's into the probabilities.
 //
 // Bound by the issue of vector and matrix instructions together, at a clock that
-// the power limits: a prompt of 16384 tokens, 32 heads of 128, 1.83 ms (1.20
-// PFLOP/s), matrix cores busy 51 % of the time at 1.87 GHz.  Over an int8 cache by
-// vector instructions, a third of which widen (512 rows over 8192 tokens 109 us, over
-// bf16 75).  Slower were: loads issued by the matrix turn (1972 -> 2147 us), V read
-// by 16 bytes and paired by permutes (7 % more), the matrix turn without priority.
+// the power limits: a prompt of 16384 tokens, 32 heads of 128, 1.84 ms (1.19
+// PFLOP/s), matrix cores busy 62 % of the time at 1.9 GHz.  Over an int8 cache by
+// vector instructions, more than a quarter of which widen (512 rows over 8192 tokens
+// 110 us, over bf16 74).  Slower were: loads issued by the matrix turn (1972 -> 2147
+// us), V read by 16 bytes and paired by permutes (7 % more), the matrix turn without
+// priority; no gain: none of the loads past a half's last tile, V and the second K
+// tile loaded behind the first's wait, priority for a block's start and end, V's rows
+// swizzled by their parity too.
 
 #if STAGES == 3
 #define ROWG 4                     // groups of rows
