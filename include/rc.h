@@ -174,7 +174,8 @@ typedef enum rc_op_kind {
      * held).  Rows of out[] that are no sequence's are left as they were.
      * D is 64, 128 or 256; page 16, 32, 64, 128 or 256; width * page at most
      * 2^30, pages * Hkv * page at most 2^40, T * H and T * Hkv at most 2^30,
-     * Hkv * D at most 2^20, and B at most 2^24.
+     * Hkv * D at most 2^20, B at most 2^24, and for attention B * Hkv at most
+     * 2^25.
      *
      * New tokens' K and V into the cache:
      *   bf16: as they are;

@@ -131,6 +131,12 @@ __device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amd
 // its last block (the one that sees most keys) first, piece by piece, head by
 // head.  Item `index` of that order (ITEMS), the first piece's of what row
 // `index` of Q is in (ROWS), or of the `index`-th block that is cut (BLOCKS).
+// Where there are more than SCANNED sequences, which are not cut then, they are not
+// gone through: sequence b has the indexes of blocks from first_index(b) on, which
+// are at least as many as its blocks, and is found by 64 of them at a time (8192
+// sequences of 64 tokens, 8 heads: 802 us, 3860 where all lengths are read).
+#define SCANNED 256
+__device__ __forceinline__ int first_index(const SeqsArgs &a, int b) { return (int)((u32)limit(a.offsets[b], 0, a.T) * a.G / BM) + b; }
 enum Find { ITEMS, ROWS, BLOCKS };
 template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int index, Item &item) {
     const int lane = threadIdx.x & 63;
@@ -167,10 +173,24 @@ template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int
     }
 #endif
 #endif
-    int slot = 0;
-    for (int c = 0; c < a.B; c += 64) {
-        const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
-        const int blocks = c + lane < a.B ? blocks_of(a, s) : 0, pieces = SPLIT ? max(1, (tiles_of(s) + most - 1) / most) : 1;
+    int slot = 0, c = 0, end = a.B;
+#if !SPLIT
+    if (a.B > SCANNED) {
+        // only the last sequence whose first index is not past j
+        for (int n = a.B, step; n > 1; n = end - c) {
+            step = (n + 63) / 64;
+            const unsigned long long before = __builtin_amdgcn_ballot_w64(lane * step < n && first_index(a, min(c + lane * step, a.B)) <= j);
+            if (!before) return false;
+            c += (63 - __builtin_clzll(before)) * step;
+            end = min(end, c + step);
+        }
+        c = __builtin_amdgcn_readfirstlane(c);
+        j = __builtin_amdgcn_readfirstlane(j - first_index(a, c));
+    }
+#endif
+    for (; c < end; c += 64) {
+        const Seq s = c == 0 || c + lane >= end ? first : sequence(a, c + lane);
+        const int blocks = c + lane < end ? blocks_of(a, s) : 0, pieces = SPLIT ? max(1, (tiles_of(s) + most - 1) / most) : 1;
         const int cut = pieces > 1 ? blocks * pieces : 0;      // states that the sequence leaves
         const int items = WHAT == ITEMS ? blocks * pieces : pieces > 1 ? blocks : 0;
         const int sum = WHAT == ROWS ? 0 : scan(items), sums = SPLIT ? scan(cut) : 0;
@@ -662,7 +682,11 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     // tiles of the block's last row, of the piece
     const int last_vis = s.vis((min(rows, r0 + BM) - 1) / a.G, a.causal);
     const int all = (max(last_vis + 1, 0) + BN - 1) / BN, share = (all + item.pieces - 1) / item.pieces;
-    const int kt0 = item.piece * share, n_kt = max(0, min(all, kt0 + share) - kt0);
+    int kt0 = item.piece * share;
+#if I8 && !SPLIT
+    asm volatile("" : "+s"(kt0));          // (where it is known to be 0, more is held than there are registers for)
+#endif
+    const int n_kt = max(0, min(all, kt0 + share) - kt0);
     const int n_it = (n_kt + HALVES - 1) / HALVES, n_loc = (n_kt + HALVES - 1 - sp) / HALVES;        // turns; tiles of this half
 
     // loads: lane's byte offsets within the wave's rows of a tile

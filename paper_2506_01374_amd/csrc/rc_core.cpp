@@ -471,6 +471,8 @@ static std::string check_seqs_desc(const rc_op_desc *d, bool *size) {
     if (s.T > most || s.TK > most || s.H > most || s.T * s.H > most || s.TK * s.Hkv > most) return "rows x heads exceed 2^30";
     if (s.Hkv > (1 << 20) / s.D) return fmt("Hkv x D = %lld x %lld exceeds 2^20", (long long)s.Hkv, (long long)s.D);
     if (s.B > (1 << 24)) return fmt("B = %lld exceeds 2^24", (long long)s.B);
+    const bool cache = d->kind == RC_OP_KV_WRITE || d->kind == RC_OP_KV_READ;
+    if (!cache && s.B * s.Hkv > (1 << 25)) return fmt("B x Hkv = %lld x %lld exceeds 2^25", (long long)s.B, (long long)s.Hkv);
     if (d->kind == RC_OP_ATTENTION_PACKED) return "";
     if (s.page != 16 && s.page != 32 && s.page != 64 && s.page != 128 && s.page != 256)
         return fmt("page = %lld: pages hold 16, 32, 64, 128 or 256 tokens", (long long)s.page);
@@ -615,7 +617,9 @@ static std::string check_kv_cache(const rc_op_desc *d, const rc_schedule *s) {
 
 int64_t seqs_items(const rc_op_desc *d, int bm, int splits) {
     const SeqDims q = seq_dims(d);
-    return q.Hkv * (q.T * (q.H / q.Hkv) / bm + std::min(q.B, q.T)) + 256 * splits;
+    // (indexes of blocks, of which a sequence without rows has one where there are
+    // many sequences)
+    return q.Hkv * (q.T * (q.H / q.Hkv) / bm + (q.B > 256 && !splits ? q.B : std::min(q.B, q.T))) + 256 * splits;
 }
 
 int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits) {
@@ -627,6 +631,7 @@ static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *
     const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
     if (redundant_tile(d, "block_m", bm, q.T * (q.H / q.Hkv)))
         return fmt("block_m %d: block_m %d already covers all rows of a K/V head", bm, bm / 2);
+    if (sp && q.B > 2048) return fmt("splits: every workgroup goes through the lengths of all sequences, %lld, more than 2048", (long long)q.B);
     if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     if (kv(d, s, "stages") == 3) {
         if ((w != 4 && w != 8) || kv(d, s, "occ") != 2) return "the ring (stages 3) takes 4 waves, or 8 in turns, two a SIMD (occ 2)";
@@ -1069,12 +1074,14 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
 // sequence has on average, and by the keys that it may have.
 // Few rows: keys go straight to registers, blocks of 16 or 32 rows; where there may
 // be more than 1024 keys (512 of D = 256: 16 sequences of 900 19 us, 24 uncut), cut
-// into pieces.  Four waves share a piece, eight with int8 and D = 256, whose registers
-// leave room for one workgroup of four a CU (64 sequences of up to 4096 keys 76 and
-// 90 us, 8 of 8000 34 and 35).  Sequences of 17 rows or more whose keys are cut, and
-// whose blocks of 32 rows leave no registers for two waves a SIMD, go through the ring
-// in blocks of 64 (us): 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4 in
-// blocks of 16; 20 rows and 8192 keys 25.8 and 28.2; 8 of D = 256, 24 rows and 3000
+// into pieces, but for many sequences, whose blocks fill the chip many times (1024 of
+// 64 to 4096 keys and 8 heads 776 cut, 730 not).  Four waves share a piece, eight with
+// int8 and D = 256, whose registers leave room for one workgroup of four a CU (64
+// sequences of up to 4096 keys 76 and 90 us, 8 of 8000 34 and 35).  Sequences of 17
+// rows or more with more than 1024 keys, whose blocks of 32 rows leave no registers for
+// two waves a SIMD, go through the ring in blocks of 64, cut where there are fewer than
+// 512 (us): 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4 in blocks of 16; 64
+// of up to 4096 66 (cut 72, in blocks of 16 77); 8 of D = 256, 24 rows and 3000
 // keys 29 and 32, of 40 rows and 6000 int8 keys 38 and 51 (one of 400 rows with 15 of
 // 4 rows 36 and 34; 10 of 31 rows and 31 to 3200 keys of 2 heads 20 and 13); with D =
 // 64, or of int8 otherwise, blocks of 32 take less: 16.2 and 19.3, 27.5 and 38.  Up to
@@ -1124,8 +1131,9 @@ static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
         if (set(bm, items >= four ? 4 : 8, 3, 2, 0)) return;
     }
     if (keys > 1024 && rows > 16 * q.B && (wide || (q.D > 64 && !i8)) && q.Hkv * q.B * keys >= (wide ? 1 << 16 : 1 << 18))
-        if (set(64, 8, 3, 2, 1)) return;
-    for (bool cut : {keys * (wide ? 2 : 1) > 1024, false})
+        if (set(64, 8, 3, 2, q.Hkv * q.B < 512 ? 1 : 0)) return;
+    const bool many = q.B > 1024 || q.Hkv * q.B >= 8192;
+    for (bool cut : {keys * (wide ? 2 : 1) > 1024 && !many, false})
         for (int occ : {2, 1})
             for (int bm : {rows > 16 * q.B ? 32 : 16, 16})
                 if (set(bm, wide && i8 ? 8 : 4, 1, occ, cut ? occ : 0)) return;

@@ -509,6 +509,31 @@ def test_thousands_of_sequences():
         check(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]), want, tol)
 
 
+@pytest.mark.parametrize("b", [64, 65, 256, 257, 4097])
+def test_sequences_on_either_side_of_what_is_scanned(b):
+    # up to 256 sequences are gone through, more are searched; rows of some, of
+    # the first and of the last alone, and offsets that make no sense
+    r = np.random.default_rng(b)
+    op = rc.Op(rc.RC_OP_ATTENTION_PACKED, (200, 200, b, 3, 1, 64), C)
+    ins = packed_inputs(([200], [200], 1, 3, 64), b)
+    some = np.zeros(b, np.int64)
+    np.add.at(some, r.integers(0, b, 150), 1)
+    some[b // 2] += 50
+    first, last = np.zeros(b, np.int64), np.zeros(b, np.int64)
+    first[0], last[-1] = 190, 200
+    for q in (some, first, last):
+        q = q.tolist()
+        at = starts(q)
+        keys = [[f64(x)[at[i]:at[i + 1]] for x in ins[1:]] for i in range(b)]
+        n = at[-1]
+        want, tol = reference(q, q, f64(ins[0])[:n], keys, True, 64 ** -0.5)
+        for text in S.legal(op, ["", "waves=4,splits=2", "block_m=64,waves=8,stages=3,occ=2", "block_m=128,waves=4,stages=3,occ=2"]):
+            check(run_packed(op, text, ins, at, at)[:n], want, tol)
+    for offsets in (r.integers(-2 ** 31, 2 ** 31, b + 1), r.integers(0, 200, b + 1), np.arange(b + 1)[::-1]):
+        for text in S.legal(op, ["", "waves=4,splits=2", "block_m=64,waves=8,stages=3,occ=2", "block_m=128,waves=4,stages=3,occ=2"]):
+            run_packed(op, text, ins, offsets.tolist(), offsets.tolist())
+
+
 def test_sequences_that_share_pages():
     # the same first pages in two tables, and one page twice in a table
     case = ([3, 40], [40, 75], 2, 4, 128, 16)

@@ -41,6 +41,7 @@ def test_descriptor_and_schedules(kind, dims, flags):
     (PG, (7, 3, 5, 2, 64, 16, 9, 5), 0, rc.RC_ERR_INVALID_ARGUMENT), (PG, (7, 3, 1, 2, 64, 16, 9, 5), 0, rc.RC_ERR_INVALID_ARGUMENT),
     (PG, (7, 3, 6, 2, 32, 16, 9, 5), 0, rc.RC_ERR_UNSUPPORTED), (PG, (2 ** 28, 3, 8, 2, 64, 16, 9, 5), 0, rc.RC_ERR_UNSUPPORTED),
     (PG, (7, 3, 6, 2, 64, 16, 9, 5), 2, rc.RC_ERR_INVALID_ARGUMENT), (PG, (7, 3, 6, 2, 64, 16, 0, 5), 0, rc.RC_ERR_INVALID_ARGUMENT),
+    (PG, (7, 2 ** 24, 8, 4, 64, 16, 9, 5), 0, rc.RC_ERR_UNSUPPORTED), (PK, (7, 7, 2 ** 24, 8, 4, 64), 0, rc.RC_ERR_UNSUPPORTED),
     (PK, (7, 30, 3, 6, 2, 64), I8, rc.RC_ERR_INVALID_ARGUMENT), (PK, (7, 30, 3, 6, 4, 64), 0, rc.RC_ERR_INVALID_ARGUMENT),
     (PK, (7, 0, 3, 6, 2, 64), 0, rc.RC_ERR_INVALID_ARGUMENT), (PK, (7, 2 ** 30, 3, 6, 2, 64), 0, rc.RC_ERR_UNSUPPORTED),
     (rc.RC_OP_GEMM_I8, (8, 8, 8), I8, rc.RC_ERR_INVALID_ARGUMENT), (rc.RC_OP_ATTENTION, (1, 1, 64, 64), I8, rc.RC_ERR_INVALID_ARGUMENT)])
@@ -83,6 +84,11 @@ def test_legality():
     huge = rc.Op(PG, (2 ** 26 - 64, 1, 16, 16, 64, 16, 9, 5))
     assert huge.default().validate() == "" and "2^32 - 1 threads" in huge.schedule(waves=2).validate()
     assert "already cover" in rc.Op(W, (1, 1, 1, 64, 16, 9, 5)).schedule(waves=2).validate()
+    many = rc.Op(PG, (4000, 2049, 16, 16, 64, 16, 9, 500))
+    assert many.suggest().as_dict()["splits"] == 0 and "2049, more than 2048" in many.schedule(splits=1).validate()
+    # a sequence without rows has an index where there are many
+    empty = rc.Op(PG, (1, 2 ** 22, 8, 8, 64, 16, 9, 5))
+    assert empty.suggest().validate() == "" and "2^32 - 1 threads" in empty.schedule(waves=4).validate()
 
 
 @pytest.mark.parametrize("kind,flags", [(W, 0), (W, I8), (RD, 0), (RD, I8), (PG, 0), (PG, C), (PG, I8), (PG, I8 | C), (PK, 0), (PK, C)])
