@@ -51,6 +51,27 @@ __device__ __forceinline__ float element(const Vec &x, int j) {
     return __builtin_bit_cast(float, j % 2 ? x[j / 2] & 0xFFFF0000u : x[j / 2] << 16);
 }
 
+// the larger of each half of two words
+__device__ __forceinline__ u32 larger(u32 a, u32 b) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(u32, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// the same over the lanes of a head, in rows of 16 without shared memory: lanes 1
+// and 2 away, then the mirror images in 8 and in 16 lanes, whose quads and halves
+// are alike by then
+__device__ __forceinline__ u32 over_head(u32 x) {
+#define WITH(how) x = larger(x, (u32)__builtin_amdgcn_update_dpp(0, (int)x, how, 0xF, 0xF, true))
+    WITH(0xB1);
+    WITH(0x4E);
+    WITH(0x141);
+    if (LANES > 8) WITH(0x140);
+#undef WITH
+#pragma unroll
+    for (int s = 16; s < LANES; s <<= 1) x = larger(x, (u32)__shfl_xor((int)x, s));
+    return x;
+}
+
 // (row of the cache's slots, or -1 if the token has none; whether the row is a
 // sequence's) of a packed row.  The wave narrows the sequences down 64-fold
 // with each load, and finds the row's among the last 64 of them.
@@ -155,12 +176,11 @@ extern "C" __global__ __launch_bounds__(64 * WAVES) void rc_kv_write(CacheArgs a
             const long long slot = p.slot + ((long long)h << a.shift);
 #if I8
             // magnitudes as bits: above all others a NaN
-            u32 bits = 0;
+            u32 most = 0;
 #pragma unroll
-            for (int e = 0; e < WORDS; ++e) bits = max(bits, max(x[j][e] & 0x7FFF0000u, x[j][e] << 16 & 0x7FFF0000u));
-#pragma unroll
-            for (int s = 1; s < LANES; s <<= 1) bits = max(bits, (u32)__shfl_xor((int)bits, s));
-            const float top = __builtin_bit_cast(float, bits);
+            for (int e = 0; e < WORDS; ++e) most = larger(most, x[j][e] & 0x7FFF7FFFu);
+            most = over_head(most);
+            const float top = __builtin_bit_cast(float, max(most & 0xFFFF0000u, most << 16));
             const bool bad = !(top < __builtin_inff());
             // brought near 1 by a power of two, exactly, so that 127 x and its
             // remainders stay in fp32's range

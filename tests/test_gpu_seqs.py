@@ -467,6 +467,25 @@ def test_extreme_scores():
         assert abs(got[2] - 36.5) <= 2 * 36.5 * BF16 + 0.2 and np.isnan(got[3])
 
 
+@pytest.mark.parametrize("flags", [0, C, I8 | C])
+def test_a_row_that_is_not_finite_spoils_no_other(flags):
+    case = ([70, 1, 3], [150, 40, 3], 2, 4, 128, 16)
+    q, lens, hkv, g, d, page = case
+    op = S.paged_op(case, flags)
+    rows, cache, table = paged_inputs(case, flags & I8, 9)
+    keys, _ = keys_of(cache, table, lens, page, flags & I8)
+    want, tol = reference(q, lens, f64(rows), keys, flags & C, d ** -0.5)
+    bad = [(0, 1), (17, 7), (69, 0), (70, 3), (73, 5)]
+    for i, (row, head) in enumerate(bad):
+        rows[row, head, 3 * i] = (float("nan"), float("inf"), -float("inf"))[i % 3]
+    keep = np.ones(want.shape[:2], bool)
+    keep[tuple(zip(*bad))] = False
+    for text in S.legal(op, S.ATTENTION_TEXTS):
+        got = f64(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]))
+        assert np.all(np.abs(got - want)[keep] <= tol[keep] + 1e-30)
+        assert np.isnan(got[0, 1]).all()
+
+
 def test_offsets_and_lengths_that_make_no_sense_stay_in_bounds():
     case = ([8, 8, 8], [20, 20, 20], 1, 2, 64, 16)
     op = S.paged_op(case, C)
