@@ -560,6 +560,12 @@ def _check_tensors(tensors, device: int, inputs, output, workspace, stream):
                 raise ValueError(f"{name} must be contiguous")
             if t.get_device() != device:
                 raise ValueError(f"{name} is on {t.device}, the plan on cuda:{device}")
+    _check_workspace(device, workspace, stream)
+    return inputs, output
+
+
+def _check_workspace(device: int, workspace, stream):
+    """The part of _check_tensors that is no operand's."""
     if workspace is not None and workspace.get_device() != device:
         raise ValueError(f"the workspace is on {workspace.device}, the plan on cuda:{device}")
     if workspace is not None and not workspace.is_contiguous():
@@ -567,7 +573,6 @@ def _check_tensors(tensors, device: int, inputs, output, workspace, stream):
         raise ValueError("the workspace must be contiguous")
     if stream is not None and stream.device.index != device:
         raise ValueError(f"the stream is of {stream.device}, the plan on cuda:{device}")
-    return inputs, output
 
 
 def _i8_packer(tensors, device: int):
@@ -589,8 +594,10 @@ def _i8_packer(tensors, device: int):
                     if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device]
         except AttributeError:                       # None among them
             ptrs = ()
-        if len(ptrs) != n or len(given) != n or len(output) != nout or workspace is not None or stream is not None:
+        if len(ptrs) != n or len(given) != n or len(output) != nout:
             _check_tensors(tensors, device, given[:len(given) - len(output)], output, workspace, stream)
+        if workspace is not None or stream is not None:
+            _check_workspace(device, workspace, stream)
         if stream is None and raw_stream is not None:
             return block.pack(block.size, *ptrs), raw_stream(device)
         return block.pack(block.size, *ptrs), _stream_ptr(stream)
