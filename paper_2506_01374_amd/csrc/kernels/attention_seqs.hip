@@ -125,9 +125,9 @@ __device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amd
 
 // A sequence's rows are cut into blocks of BM, and with SPLIT its keys into
 // pieces of at most `most` tiles, the same number for each block.  `most` is
-// the work of all sequences over the workgroups that it is cut for (a.slots), so
-// that pieces of blocks that are cut are at most 2 a.slots: each takes more than
-// half of it.  The pieces' states are in this order too: sequence by sequence,
+// the work of all sequences over the workgroups that it is cut for (a.slots), or
+// half of that, so that pieces of blocks that are cut are at most 2 a.slots, or 4:
+// each takes more than half of it.  The pieces' states are in this order too: sequence by sequence,
 // its last block (the one that sees most keys) first, piece by piece, head by
 // head.  Item `index` of that order (ITEMS), the first piece's of what row
 // `index` of Q is in (ROWS), or of the `index`-th block that is cut (BLOCKS).
@@ -155,10 +155,15 @@ template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int
     }
     work = (work * a.HKV + a.slots - 1) / a.slots;
     most = work < LEAST ? LEAST : work > (1 << 30) ? 1 << 30 : (int)work;
-#if STAGES == 3
-    // (a last piece more of many blocks can be a second round of workgroups: 25
-    // blocks of 8 heads in 3 pieces for 2, with 15 single rows, 157 us for 148)
-    for (int tries = 0; tries < 4; ++tries) {
+    // (a last piece more of many blocks can be a second round of workgroups: in the
+    // ring, 25 blocks of 8 heads in 3 pieces for 2, with 15 single rows, 157 us for
+    // 148.  Outside it, where pieces are long, a second round comes in smaller ones:
+    // 128 rows over int8 caches of 128 to 4096 tokens 92 us for 79, 64 over bf16 ones
+    // of 64 to 8192 88 for 85; where all are as long and fit one round, 64 of 1600
+    // int8 tokens, smaller ones take 56 for 47.  Of short pieces the count would take
+    // what it gains, and over int8 caches of 64 to 8192 tokens 64 rows 58 for 56.)
+    const int tries = STAGES == 3 ? 4 : most >= (I8 ? 64 : 32) ? 1 : 0;
+    for (int t = 0; t < tries; ++t) {
         long long items = 0;
         bool cut = false;
         for (int c = 0; c < a.B; c += 64) {
@@ -169,9 +174,8 @@ template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int
         }
         items *= a.HKV;
         if (!cut || items * 16 <= a.slots * 17ll) break;
-        most = (int)min((long long)(1 << 30), most * items / a.slots + 1);
+        most = STAGES == 3 ? (int)min((long long)(1 << 30), most * items / a.slots + 1) : max(LEAST, (most + 1) / 2);
     }
-#endif
 #endif
     int slot = 0, c = 0, end = a.B;
 #if !SPLIT

@@ -615,6 +615,8 @@ static std::string check_kv_cache(const rc_op_desc *d, const rc_schedule *s) {
     return "";
 }
 
+int seqs_pieces(const rc_op_desc *d, const rc_schedule *s) { return kv(d, s, "splits") * (kv(d, s, "stages") == 3 ? 1 : 2); }
+
 int64_t seqs_items(const rc_op_desc *d, int bm, int splits) {
     const SeqDims q = seq_dims(d);
     // (indexes of blocks, of which a sequence without rows has one where there are
@@ -632,7 +634,7 @@ static std::string check_attention_seqs(const rc_op_desc *d, const rc_schedule *
     if (redundant_tile(d, "block_m", bm, q.T * (q.H / q.Hkv)))
         return fmt("block_m %d: block_m %d already covers all rows of a K/V head", bm, bm / 2);
     if (sp && q.B > 2048) return fmt("splits: every workgroup goes through the lengths of all sequences, %lld, more than 2048", (long long)q.B);
-    if (seqs_items(d, bm, sp) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
+    if (seqs_items(d, bm, seqs_pieces(d, s)) * 64 * w > MAX_GRID_THREADS) return "the items exceed the grid's 2^32 - 1 threads";
     if (kv(d, s, "stages") == 3) {
         if ((w != 4 && w != 8) || kv(d, s, "occ") != 2) return "the ring (stages 3) takes 4 waves, or 8 in turns, two a SIMD (occ 2)";
         if (bm != 64 && !(bm == 128 && q.D < 256)) return fmt("the ring (stages 3) takes blocks of 64 rows, or 128 with D < 256 (%d, %lld)", bm, (long long)q.D);

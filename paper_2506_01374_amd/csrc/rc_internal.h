@@ -47,9 +47,12 @@ struct SeqDims {
 };
 SeqDims seq_dims(const rc_op_desc *d);
 int expected_dims(int32_t kind);
+// Workgroups a CU for which keys are cut: `splits`, or twice that (outside the ring,
+// where the pieces take more than a round).
+int seqs_pieces(const rc_op_desc *d, const rc_schedule *s);
 // Work items that an attention over sequences has at most, and blocks of rows
 // that it cuts: of two pieces at least, which are fewer than two a workgroup that
-// the keys are cut for.
+// the keys are cut for (`splits`: seqs_pieces).
 int64_t seqs_items(const rc_op_desc *d, int bm, int splits);
 int64_t seqs_cut_blocks(const rc_op_desc *d, int bm, int splits);
 

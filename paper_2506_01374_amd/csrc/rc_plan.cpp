@@ -970,10 +970,10 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             const SeqDims q = seq_dims(d);
             const bool paged = d->kind == RC_OP_ATTENTION_PAGED, i8 = d->flags & RC_FLAG_I8_CACHE;
             const int causal = (d->flags & RC_FLAG_CAUSAL) != 0;
-            const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits");
+            const int bm = kv(d, s, "block_m"), w = kv(d, s, "waves"), sp = kv(d, s, "splits"), cut = seqs_pieces(d, s);
             // states of the pieces of cut blocks: fewer than two a workgroup that
             // the keys are cut for
-            const size_t offP = sp ? ws.add((size_t)512 * sp * bm * (q.D + 2) * 4, "partials") : 0;
+            const size_t offP = sp ? ws.add((size_t)512 * cut * bm * (q.D + 2) * 4, "partials") : 0;
             // the join: by blocks, or by rows where there are few, which may have
             // many pieces.  us by rows and by blocks: 32 rows (a token's heads) of
             // 64 pieces 6.8 and 14.2, 256 rows of 16 pieces 6.4 and 10.3, 1280 rows
@@ -985,7 +985,7 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
             k.src = Source{SRC_attention_seqs, "rc_attention_seqs",
                            def("BM", bm) + def("NW", w) + def("STAGES", kv(d, s, "stages")) + def("OCC", kv(d, s, "occ")) + def("SPLIT", sp > 0) + def("HD", q.D) + def("PAGED", paged) +
                                def("I8", i8) + def("LEAST", 2 * w) + scale};
-            k.grid = dim3((unsigned)seqs_items(d, bm, sp), 1, 1);
+            k.grid = dim3((unsigned)seqs_items(d, bm, cut), 1, 1);
             k.block = dim3(64 * w, 1, 1);
             k.flops = rc_op_flops(d);
             k.bind = [=](const rc_args *a, char *wsp, ArgBlob &b) {
@@ -1000,7 +1000,7 @@ rc_status describe(const rc_op_desc *d, const rc_schedule *s, rc_plan &p) {
                 Kern kj = k;
                 kj.flops = 0;
                 kj.src.entry = "rc_attention_seqs_join";
-                kj.grid = dim3((unsigned)(by == 2 ? seqs_cut_blocks(d, bm, sp) * std::max<int64_t>(1, bm * q.D / 2048) : q.T * q.H), 1, 1);
+                kj.grid = dim3((unsigned)(by == 2 ? seqs_cut_blocks(d, bm, cut) * std::max<int64_t>(1, bm * q.D / 2048) : q.T * q.H), 1, 1);
                 kj.block = dim3(256, 1, 1);
                 p.kerns.push_back(kj);
             }
