@@ -514,6 +514,22 @@ def test_many_pieces(case, flags):
         check(run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)]), want, tol)
 
 
+@pytest.mark.parametrize("flags", [C, I8 | C])
+def test_long_pieces_of_uneven_sequences(flags):
+    # 25,000 tiles of 32 keys and heads over 256 workgroups: pieces of 98, which are
+    # more than a round, and halved
+    r = np.random.default_rng(22)
+    lens = r.integers(16, 2000, 90).tolist() + [6000, 5000]
+    case = ([1] * 92, lens, 8, 1, 64, 64)
+    assert 64 * 256 < sum(-(-n // 32) for n in lens) * 8 < 98 * 2 * 256
+    op = S.paged_op(case, flags)
+    rows, cache, table = paged_inputs(case, flags & I8, 23)
+    keys, _ = keys_of(cache, table, lens, 64, flags & I8)
+    want, tol = reference(case[0], lens, f64(rows), keys, True, 64 ** -0.5)
+    for text in ("waves=4,splits=1", "waves=1,splits=1", "waves=4,occ=2,splits=2"):
+        check(run_paged(op, text, rows, cache, [ints(range(93)), ints(lens), ints(table)]), want, tol)
+
+
 def test_thousands_of_sequences():
     r = np.random.default_rng(30)
     q = r.integers(0, 3, 5000).tolist()
@@ -604,6 +620,23 @@ def test_a_cache_past_32_bits(i8):
         plan.launch([rows.cuda()] + cache + [ints(starts(q)).cuda()] + where[1:], got, plan.workspace())
         torch.cuda.synchronize()
         check(got, want, tol)
+
+
+def test_packed_rows_past_32_bits():
+    # 140000 sequences of one token: each row of O, of 2^32 bytes and more, is V's
+    t, h, hkv, d = 140000, 128, 8, 128
+    assert t * h * d * 2 > 2 ** 32
+    op = rc.Op(rc.RC_OP_ATTENTION_PACKED, (t, t, t, h, hkv, d), C)
+    q, out = (torch.zeros(t, h, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v = (torch.randn(t, hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    at = torch.arange(t + 1, dtype=torch.int32, device="cuda")
+    for text in S.legal(op, ["waves=4"]):
+        print(f"[gpu] packed dims={op.dims} flags={op.flags} sched={text}", flush=True)
+        plan = rc.Plan(op, op.from_string(text))
+        plan.launch([q, k, v, at, at], out.zero_(), plan.workspace())
+        for i in range(0, t, 10000):
+            part = out[i:i + 10000].view(-1, hkv, h // hkv, d)
+            assert bool((part == v[i:i + 10000, :, None]).all())
 
 
 def test_one_plan_on_two_streams():
