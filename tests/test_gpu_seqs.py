@@ -499,6 +499,30 @@ def test_offsets_and_lengths_that_make_no_sense_stay_in_bounds():
             run_write(wr, str(wr.suggest()), [kv, kv], [ints(offsets), ints(lens), ints(table)], cache)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("kind,flags", [(rc.RC_OP_ATTENTION_PAGED, C), (rc.RC_OP_ATTENTION_PAGED, I8 | C), (rc.RC_OP_ATTENTION_PACKED, C)])
+def test_every_suggested_schedule(kind, flags, d):
+    case = ([70, 1, 0, 3], [150, 40, 9, 3], 2, 4, d, 16)
+    q, lens, hkv, g, _, page = case
+    if kind == rc.RC_OP_ATTENTION_PAGED:
+        op = S.paged_op(case, flags)
+        rows, cache, table = paged_inputs(case, flags & I8, 70)
+        keys, _ = keys_of(cache, table, lens, page, flags & I8)
+    else:
+        op = S.packed_op((q, lens, hkv, g, d), flags)
+        ins, at = packed_inputs((q, lens, hkv, g, d), 70), starts(lens)
+        rows, keys = ins[0], [[f64(x)[at[b]:at[b + 1]] for x in ins[1:]] for b in range(4)]
+    want, tol = reference(q, lens, f64(rows), keys, True, d ** -0.5)
+    texts = [str(s) for o, s in rc.suggestions(kind, flags) if o.dims[5 if kind == rc.RC_OP_ATTENTION_PACKED else 4] == d]
+    assert len(texts) >= 6
+    for text in texts:
+        if kind == rc.RC_OP_ATTENTION_PAGED:
+            got = run_paged(op, text, rows, cache, [ints(starts(q)), ints(lens), ints(table)])
+        else:
+            got = run_packed(op, text, ins, starts(q), at)
+        check(got, want, tol)
+
+
 @pytest.mark.parametrize("flags", [C, I8 | C])
 @pytest.mark.parametrize("case", [([1], [9000], 1, 4, 64, 16), ([1] * 40, [700 + 61 * i for i in range(40)], 2, 16, 64, 16),
                                   ([90, 1, 0, 1], [2500, 4000, 5, 31], 2, 8, 64, 64)])
