@@ -300,7 +300,10 @@ struct Tile {
     int held;          // of the two 16-key blocks
 };
 
-extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OCC, 8))) void rc_attention_seqs(SeqsArgs a) {
+// (At most three waves a SIMD where there are two at least: with four, pieces that are
+// cut for two crowd some of the CUs, 64 rows over int8 caches of 64 to 8192 tokens 58.6
+// us for 56.0, 100 rows of D = 64 over bf16 ones 100.3 for 98.6.)
+extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(OCC, OCC == 2 ? 3 : 8))) void rc_attention_seqs(SeqsArgs a) {
     __shared__ __attribute__((aligned(16))) float osum[NW][BM][HD + 4];
     __shared__ float om[NW][BM], ol[NW][BM];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -310,9 +313,10 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     const Seq s = item.s;
     const int rows = s.n * a.G, r0 = item.block * BM;
 
-    // queries, and the last key that each sees
+    // queries, and the last key that each sees (the first row the fewest)
     bf16x8 q[QB][NKS];
-    int vis[QB], least = 1 << 30;
+    int vis[QB];
+    const int least = __builtin_amdgcn_readfirstlane(s.vis(r0 / a.G, a.causal));
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = r0 + 16 * b + i, token = r / a.G;
@@ -321,16 +325,12 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         for (int ks = 0; ks < NKS; ++ks) q[b][ks] = bf16x8{};
         if (r < rows) {
             vis[b] = s.vis(token, a.causal);
-            least = min(least, vis[b]);
             const bf16_t *p = a.Q + ((size_t)(s.q0 + token) * a.HKV * a.G + item.h * a.G + r % a.G) * HD;
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
                 q[b][ks] = *(const bf16x8 *)(p + (I8 ? 64 * (ks / 2) + 16 * g + 8 * (ks % 2) : 32 * ks + 8 * g));
         }
     }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d));
-    least = __builtin_amdgcn_readfirstlane(least);
 
     // tiles of the block's last row, of the piece, of the wave
     const int last = s.vis((min(rows, r0 + BM) - 1) / a.G, a.causal);
@@ -600,7 +600,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // the other does its softmax (vector work); a barrier ends each turn.  Four waves
 // alternate the same turns, two workgroups a CU, which fall out of step by
 // themselves and fill each other's starts and ends, 17000 cycles a block (8
-// prompts of 8192 tokens in all, 32 heads of 128: 152 us, with eight waves 188);
+// prompts of 8192 tokens in all, 32 heads of 128: 147 us, with eight waves 188);
 // eight are for few blocks, each of them done sooner (64 rows, 8 sequences: 19 and
 // 22).
 // K and V go straight from memory to shared memory, into a ring of two tiles for
@@ -834,7 +834,11 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
     };
 
     bf16x8 qf[QB][NKS];
-    int vis[QB], least = 1 << 30, most = -1;
+    int vis[QB], least = 1 << 30, most = -1;           // (of the wave's first and last row)
+    if (r0w < rows) {
+        least = __builtin_amdgcn_readfirstlane(s.vis(r0w / a.G, a.causal));
+        most = __builtin_amdgcn_readfirstlane(s.vis((min(rows, r0w + 16 * QB) - 1) / a.G, a.causal));
+    }
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
         const int r = r0w + 16 * b + i, token = r / a.G;
@@ -843,20 +847,11 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         for (int ks = 0; ks < NKS; ++ks) qf[b][ks] = bf16x8{};
         if (r < rows) {
             vis[b] = s.vis(token, a.causal);
-            least = min(least, vis[b]);
-            most = max(most, vis[b]);
             const bf16_t *p = a.Q + ((size_t)(s.q0 + token) * a.HKV * a.G + item.h * a.G + r % a.G) * HD;
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks) qf[b][ks] = *(const bf16x8 *)(p + 32 * ks + 8 * g);
         }
     }
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) {
-        least = min(least, __shfl_xor(least, d));
-        most = max(most, __shfl_xor(most, d));
-    }
-    least = __builtin_amdgcn_readfirstlane(least);
-    most = __builtin_amdgcn_readfirstlane(most);
     // (their loads end before the loop, whose waits count the ring's alone)
 #pragma unroll
     for (int b = 0; b < QB; ++b)
