@@ -600,7 +600,8 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // the other does its softmax (vector work); a barrier ends each turn.  Four waves
 // alternate the same turns, two workgroups a CU, which fall out of step by
 // themselves and fill each other's starts and ends, 17000 cycles a block (8
-// prompts of 8192 tokens in all, 32 heads of 128: 146 us, with eight waves 188);
+// prompts of 8192 tokens in all, 32 heads of 128: 150 us, with eight waves 188; 142
+// with the stores below);
 // eight are for few blocks, each of them done sooner (64 rows, 8 sequences: 19 and
 // 22).
 // K and V go straight from memory to shared memory, into a ring of two tiles for
