@@ -155,26 +155,37 @@ template <Find WHAT> __device__ __forceinline__ bool find(const SeqsArgs &a, int
     }
     work = (work * a.HKV + a.slots - 1) / a.slots;
     most = work < LEAST ? LEAST : work > (1 << 30) ? 1 << 30 : (int)work;
-    // (a last piece more of many blocks can be a second round of workgroups: in the
+    // A last piece more of many blocks can be a second round of workgroups: in the
     // ring, 25 blocks of 8 heads in 3 pieces for 2, with 15 single rows, 157 us for
-    // 148.  Outside it, where pieces are long, a second round comes in smaller ones:
+    // 148.  There a piece counts as a workgroup, and a block that is not cut as the part
+    // of one that its tiles are of `most`, with START tiles more for the start and the
+    // end of each: with all blocks as workgroups, many short sequences leave a long one
+    // whole (62 of 256 tokens and 5 rows, one of 32768: 268 us for 55; 32 of 300 to 8192
+    // and 16 rows 74 for 65).  Cut blocks, each of more than `most` tiles, exceed what
+    // their tiles take of a round by one piece each, so that the next `most` is at most
+    // twice what all tiles and starts are over the workgroups.
+    // (Outside the ring, where pieces are long, a second round comes in smaller ones:
     // 128 rows over int8 caches of 128 to 4096 tokens 92 us for 79, 64 over bf16 ones
     // of 64 to 8192 88 for 85; where all are as long and fit one round, 64 of 1600
     // int8 tokens, smaller ones take 56 for 47.  Of short pieces the count would take
     // what it gains, and over int8 caches of 64 to 8192 tokens 64 rows 58 for 56.)
     const int tries = STAGES == 3 ? 4 : most >= (I8 ? 64 : 32) ? 1 : 0;
+    constexpr int PART = STAGES == 3 ? 32 : 1, START = 5;     // (a workgroup, in the units that are counted)
+#pragma nounroll
     for (int t = 0; t < tries; ++t) {
-        long long items = 0;
+        const float part = PART * __builtin_amdgcn_rcpf((float)(most + START));
+        long long load = 0;
         bool cut = false;
         for (int c = 0; c < a.B; c += 64) {
             const Seq s = c == 0 || c + lane >= a.B ? first : sequence(a, c + lane);
-            const int pieces = c + lane < a.B ? max(1, (tiles_of(s) + most - 1) / most) : 1;
-            items += from_lane(scan(c + lane < a.B ? (int)min((long long)blocks_of(a, s) * pieces, 1ll << 24) : 0), 63);
+            const int tiles = tiles_of(s), pieces = c + lane < a.B ? max(1, (tiles + most - 1) / most) : 1;
+            const int each = STAGES != 3 || pieces > 1 ? PART * pieces : (int)((float)(tiles + START) * part);
+            load += from_lane(scan(c + lane < a.B ? (int)min((long long)blocks_of(a, s) * each, 1ll << 24) : 0), 63);
             cut |= __builtin_amdgcn_ballot_w64(pieces > 1) != 0;
         }
-        items *= a.HKV;
-        if (!cut || items * 16 <= a.slots * 17ll) break;
-        most = STAGES == 3 ? (int)min((long long)(1 << 30), most * items / a.slots + 1) : max(LEAST, (most + 1) / 2);
+        load *= a.HKV;
+        if (!cut || load * 16 <= PART * a.slots * 17ll) break;
+        most = STAGES == 3 ? (int)min((long long)(1 << 30), most * load / (PART * a.slots) + 1) : max(LEAST, (most + 1) / 2);
     }
 #endif
     int slot = 0, c = 0, end = a.B;
