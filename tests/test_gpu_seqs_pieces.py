@@ -1,5 +1,5 @@
 """GPU tests of how attention in serving cuts keys into pieces: how long the pieces
-are, and many sequences of which few are cut.
+are, many sequences of which few are cut, and pieces in the library's own workspace.
 
 References and bounds are those of test_gpu_seqs, with a term more for the ring over
 bf16 (stages=3), where the sum of p is that of the rounded p too: with roundings d_j of
@@ -111,3 +111,28 @@ def test_few_of_many_sequences_are_cut(b, few):
             check_cut(got, op, text, want, tol)
             blocks = sum(-(-q[i] * 4 // op.from_string(text)["block_m"]) for i in long)
             assert made >= 2 * 2 * blocks
+
+
+def test_pieces_in_the_library_s_own_workspace():
+    case = ([1, 1, 30, 1, 1, 1], [3000, 1, 500, 64, 2000, 77], 2, 4, 128, 16)
+    q, lens = case[:2]
+    for flags in (C, I8 | C):
+        op = S.paged_op(case, flags)
+        rows, cache, table = paged_inputs(case, flags & I8, 95)
+        where = [ints(starts(q)), ints(lens), ints(table)]
+        ins = [x.cuda() for x in [rows] + cache + where]
+        for text in ("waves=4,splits=2", "block_m=64,waves=8,stages=3,occ=2,splits=1"):
+            want, made = run_cut(op, text, rows, cache, where)
+            plan = rc.Plan(op, op.from_string(text))
+            assert made > 0 and 0 < plan.workspace_bytes <= rc.lib().rc_static_scratch_bytes()
+            for _ in range(2):
+                got = torch.full_like(want, float("nan"))
+                plan.launch_static(ins, got)
+                torch.cuda.synchronize()
+                assert torch.equal(got, want)
+        # more than the library keeps
+        plan = rc.Plan(op, op.from_string("block_m=128,waves=4,stages=3,occ=2,splits=4"))
+        assert plan.workspace_bytes > rc.lib().rc_static_scratch_bytes()
+        with pytest.raises(rc.RCError) as e:
+            plan.launch_static(ins, got)
+        assert e.value.status == rc.RC_ERR_OUT_OF_MEMORY and "use rc_launch" in str(e.value)
