@@ -244,6 +244,13 @@ __device__ __forceinline__ float least_finite(float m) { return fmaxf(m, -0x1.ff
 __device__ __forceinline__ u32 pack2(float a, float b) {
     return __builtin_bit_cast(u32, __builtin_convertvector((f32x2){a, b}, bf16x2));
 }
+// four outputs of a row, sums of p V over the sum of p: 0 where nothing was seen, or at
+// -inf alone, whose values (0 times each) may be anything
+__device__ __forceinline__ u32x2 outputs(const f32x4 &o, float sum) {
+    const float inv = 1.f / sum;
+    const u32x2 x = {pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+    return sum == 0.f ? u32x2{} : x;
+}
 __device__ __forceinline__ f32x4 mfma(const bf16x8 &a, const bf16x8 &b, const f32x4 &c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -590,10 +597,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
             if (d == 0) state[r] = top, state[BM + r] = sum;
             *(f32x4 *)(state + 2 * BM + r * HD + d) = out;
         } else {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
             const int row = r0 + r;
             bf16_t *p = a.O + ((size_t)(s.q0 + row / a.G) * a.HKV * a.G + item.h * a.G + row % a.G) * HD + d;
-            *(u32x2 *)p = u32x2{pack2(out[0] * inv, out[1] * inv), pack2(out[2] * inv, out[3] * inv)};
+            *(u32x2 *)p = outputs(out, sum);
         }
     }
 }
@@ -1252,9 +1258,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 #if HALVES == 2
         const float mo = other[b * 32 + ie], lo = other[b * 32 + 16 + ie], top = fmaxf(m[b], mo);
         const float by = m[b] == top ? 1.f : pow2(m[b] - top), byo = mo == top ? 1.f : pow2(mo - top);
-        const float sum = SUM(b) * by + lo * byo, inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float sum = SUM(b) * by + lo * byo;
 #else
-        const float top = m[b], sum = SUM(b), inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float top = m[b], sum = SUM(b);
 #endif
         const int row = r0w + 16 * b + ie, r = row - r0;
         if (row >= rows) continue;
@@ -1277,9 +1283,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
         // with 8 bytes, 52.6 with 16)
 #pragma unroll
         for (int d = 0; d < DB; d += 2) {
-            const f32x4 x = sum_of(d), y = sum_of(d + 1);
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(pack2(x[0] * inv, x[1] * inv), pack2(y[0] * inv, y[1] * inv), false, false));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(pack2(x[2] * inv, x[3] * inv), pack2(y[2] * inv, y[3] * inv), false, false));
+            const u32x2 x = outputs(sum_of(d), sum), y = outputs(sum_of(d + 1), sum);
+            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false));
+            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false));
             *(u32x4 *)(p + 16 * (d + (ge & 1)) + 8 * (ge >> 1)) = u32x4{lo[0], hi[0], lo[1], hi[1]};
         }
     }
@@ -1337,9 +1343,8 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
                 for (int i = 0; i < ONCE; ++i)
                     if (p + i < item.pieces) add(mp[i], lp[i], op[i]);
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
             bf16_t *to = a.O + ((size_t)(item.s.q0 + row / a.G) * H + item.h * a.G + row % a.G) * HD + d;
-            *(u32x2 *)to = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+            *(u32x2 *)to = outputs(o, l);
         }
         return;
     }
@@ -1375,7 +1380,6 @@ extern "C" __global__ __launch_bounds__(256) void rc_attention_seqs_join(SeqsArg
     if (w) return;
 #pragma unroll
     for (int x = 1; x < 4; ++x) add(pm[x], pl[x], po[x][d / 4]);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (part == 0) *(u32x2 *)(a.O + (size_t)at * HD + d) = u32x2{pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv)};
+    if (part == 0) *(u32x2 *)(a.O + (size_t)at * HD + d) = outputs(o, l);
 }
 #endif
