@@ -298,7 +298,14 @@ rc_status rc_default_schedule(const rc_op_desc *d, rc_schedule *out);
  * rules on sizes: for a caller
  * that has not searched, whose sizes change from call to call (the kernels of
  * these kinds take sizes as arguments, so that plans of all sizes share the
- * code objects that rc_suggestions lists).  RC_ERR_UNSUPPORTED for the other kinds. */
+ * code objects that rc_suggestions lists).  RC_ERR_UNSUPPORTED for the other kinds.
+ * The lengths of attention in serving are not known here: the rules take B
+ * sequences that share the rows evenly, with as many keys each as the table's
+ * width holds, or TK / B.  A caller whose table is wider than its sequences are
+ * long takes the suggestion for a descriptor of the width that they need: a
+ * schedule that is legal at one width is legal at all, and its code object is the
+ * same.  (600 rows over 600 tokens, 32 heads over 8 of 128: 18 us, and 28 as
+ * suggested for a table of eight times the tokens.) */
 rc_status rc_suggest_schedule(const rc_op_desc *d, rc_schedule *out);
 
 /* All schedules that rc_suggest_schedule may return for a kind and flags,

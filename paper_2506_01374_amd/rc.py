@@ -292,7 +292,9 @@ class Op:
 
     def suggest(self) -> "Schedule":
         """A legal schedule by rules on the sizes (the 8-bit kinds and those of
-        attention in serving)."""
+        attention in serving; of the paged kinds, whose tables may be wider than
+        the sequences are long, ask one of the width that these need, and use it
+        with ``op.from_string(str(...))``)."""
         s = rc_schedule()
         _check(lib().rc_suggest_schedule(self.ref, ctypes.byref(s)), "rc_suggest_schedule")
         return Schedule(self, s)
