@@ -202,7 +202,9 @@ typedef enum rc_op_kind {
      * (H / Hkv).  Keys without a page are not seen.  A row that sees no key, or
      * whose scores all are -infinity, is 0; what a row does not see does not
      * count, a NaN there neither.  Probabilities are rounded to bf16 for the
-     * second product, int8 values with their scale multiplied in.
+     * second product, int8 values with their scale multiplied in; with a ring
+     * (the schedule's stages 3) over bf16 sum_j p_j is that of the rounded ones,
+     * else it is of those before rounding.
      * dim = {T, B, H, Hkv, D, page, pages, width}, H a multiple of Hkv.  in[0] =
      * Q [T][H][D] bf16; in[1] = K, in[2] = V, in[3] = Ks and in[4] = Vs
      * (RC_FLAG_I8_CACHE), then offsets, lens and table; out[0] = O [T][H][D]. */
