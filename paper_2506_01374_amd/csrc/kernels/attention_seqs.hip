@@ -24,6 +24,11 @@
 // r sees the keys 0 .. vis, with vis the token's position (causal) or the last
 // key's.  A row that sees none is 0.
 //
+// Scores, maxima and all sums are fp32.  Probabilities are rounded to bf16 for the
+// second product, with int8 after V's scale is multiplied in: half a step, 2^-8, of
+// each, which is what the output's own rounding may cost, where two terms of each
+// would double the second product's matrix instructions.
+//
 // What is in the offsets, lengths and the table is on the device, and so is the
 // division of work: every wave reads the lengths of all sequences and finds its
 // workgroup's item (see find), so that a launch, a captured one too, serves
@@ -617,10 +622,9 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // the other does its softmax (vector work); a barrier ends each turn.  Four waves
 // alternate the same turns, two workgroups a CU, which fall out of step by
 // themselves and fill each other's starts and ends, 17000 cycles a block (8
-// prompts of 8192 tokens in all, 32 heads of 128: 150 us, with eight waves 188; 142
-// with the stores below);
-// eight are for few blocks, each of them done sooner (64 rows, 8 sequences: 19 and
-// 22).
+// prompts of 8192 tokens in all, 32 heads of 128: 148 us, with eight waves 180);
+// eight are for few blocks, each of them done sooner (8 sequences of 64 new rows and
+// 1000 tokens: blocks of 64 rows 19 us, with four 23).
 // K and V go straight from memory to shared memory, into a ring of two tiles for
 // each operand and half of the waves; the softmax turn issues the loads between its
 // exponentials, K of the tile after the next and V of the next, into the places
@@ -634,14 +638,14 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
 // scores, V's into the probabilities.
 //
 // Bound by the issue of vector and matrix instructions together, at a clock that
-// the power limits: a prompt of 16384 tokens, 32 heads of 128, 1.84 ms (1.19
-// PFLOP/s), matrix cores busy 62 % of the time at 1.9 GHz.  Over an int8 cache by
-// vector instructions, more than a quarter of which widen (512 rows over 8192 tokens
-// 110 us, over bf16 74).  Slower were: loads issued by the matrix turn (1972 -> 2147
-// us), V read by 16 bytes and paired by permutes (7 % more), the matrix turn without
-// priority; no gain: none of the loads past a half's last tile, V and the second K
-// tile loaded behind the first's wait, priority for a block's start and end, V's rows
-// swizzled by their parity too.
+// the power limits: a prompt of 16384 tokens, 32 heads of 128, 1.78 to 1.88 ms
+// (1.23 to 1.17 PFLOP/s), matrix cores busy 62 % of the time at 1.9 GHz.  Over an
+// int8 cache by vector instructions, more than a quarter of which widen (512 rows
+// over 8192 tokens 110 us, over bf16 75 to 81).  Slower were: loads issued by the
+// matrix turn (1972 -> 2147 us), V read by 16 bytes and paired by permutes (7 %
+// more), the matrix turn without priority; no gain: none of the loads past a half's
+// last tile, V and the second K tile loaded behind the first's wait, priority for a
+// block's start and end, V's rows swizzled by their parity too.
 
 #if STAGES == 3
 #define ROWG 4                     // groups of rows
@@ -953,7 +957,7 @@ extern "C" __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per
             seq<0, QB>([&](auto bc) __attribute__((always_inline)) {
                 constexpr int b = decltype(bc)::value;
                 o[b][d] = mfma(x, pf[j][b], o[b][d]);
-                // the sums of the probabilities, a product with ones: two
+                // the sums of the rounded probabilities, a product with ones: two
                 // instructions of the matrix cores for 16 additions
 #if !I8
                 if constexpr (d == 0) l[b] = mfma(ones_row, pf[j][b], l[b]);

@@ -1072,43 +1072,54 @@ static void suggest_kv_cache(const rc_op_desc *d, rc_schedule *s) {
     set_knob(d, s, "waves", q.T > 4 ? 4 : q.T > 1 ? 2 : 1);
 }
 
-// Attention over sequences, whose lengths are on the device: by the rows that a
-// sequence has on average, and by the keys that it may have.
+// Attention over sequences, whose lengths are on the device: by the rows (tokens times
+// query heads of a K/V head) that a sequence has on average, and by the keys that it
+// may have.  Figures are us, over a paged cache in bf16 with 32 query heads over 8 K/V
+// heads of 128, or with 16 over 4 of 256 (D = 256), where nothing else is said; "600 /
+// 2300": a sequence of 600 new tokens and 2300 in all, "16 x 5 / 2000" 16 of 5.
 // Few rows: keys go straight to registers, blocks of 16 or 32 rows; where there may
-// be more than 1024 keys (512 of D = 256: 16 sequences of 900 19 us, 24 uncut), cut
-// into pieces, but for many sequences, whose blocks fill the chip many times (1024 of
-// 64 to 4096 keys and 8 heads 776 cut, 730 not).  Four waves share a piece, eight with
-// int8 and D = 256, whose registers leave room for one workgroup of four a CU (64
-// sequences of up to 4096 keys 76 and 90 us, 8 of 8000 34 and 35).  Sequences of 17
-// rows or more with more than 1024 keys, whose blocks of 32 rows leave no registers for
-// two waves a SIMD, go through the ring in blocks of 64, cut where there are fewer than
-// 512 (us): 16 sequences of 20 rows and up to 8192 keys 25.7, 32.4 in blocks of 16; 64
-// of up to 4096 66 (cut 72, in blocks of 16 77); 8 of D = 256, 24 rows and 3000
-// keys 29 and 32, of 40 rows and 6000 int8 keys 38 and 51 (one of 400 rows with 15 of
-// 4 rows 36 and 34; 10 of 31 rows and 31 to 3200 keys of 2 heads 20 and 13); with D =
-// 64, or of int8 otherwise, blocks of 32 take less: 16.2 and 19.3, 27.5 and 38.  Up to
-// 512 blocks of 16 rows with few keys stay as they are: 64 items of a prompt of 256
-// 8.8 (ring 9.8), 7 prompts of 100 6.6 (9.1), 600 tokens of one head 9.9 (12.3), but
-// 1000 with three shorter prompts 18 (16).
-// More rows: the ring.  `items` is the number of blocks of 128 rows.  Few of them with
-// keys enough are cut for two workgroups of four waves a CU: 64 and 8192 keys 77
-// (uncut, 8 waves, 82), 75 and 5000 of D = 64 37 (41); int8 keys, and D = 256, take
-// about twice as long, so that shorter ones are: 75 and 2048 of int8 44 (52), 150 and
-// 2300 56 (94), 225 and 3000 83 (90), but 300 and 2300 105 (97); 54 and 2038 of D =
-// 256 34 (48), 75 and 2300 48 (53), 112 58 (55), 112 and 5000 102 (115), 200 173
-// (166).  D = 128 without int8, 225 and 5000 take 87 (77), 450 139 (126).  Sequences
-// of up to 64 rows are cut in blocks of 64: 32 of 32 rows and up to 8192 keys 24 with
-// eight waves (27 in blocks of 128), over int8 keys with four, 16 of 64 rows and 5000
-// keys 67 (78 with eight, 76 in blocks of 128).
+// be more than 1024 keys (512 of D = 256: 16 x 1 / 900 20, uncut 24), cut into pieces,
+// but for many sequences, whose blocks fill the chip many times (1024 x 1 / 64 to 4096
+// 864 cut, 722 not).  Four waves share a piece, eight with int8 and D = 256, whose
+// registers leave room for one workgroup of four a CU (64 x 1 / 64 to 4096, 32 heads
+// over 8, 75 and 90; 8 x 1 / 8000 32 and 34).
+// Sequences of 17 rows or more with more than 1024 keys, whose blocks of 32 rows leave no
+// registers for two waves a SIMD, go through the ring in blocks of 64, cut where there
+// are fewer than 512 sequences times K/V heads: 16 x 5 / 64 to 8192 25 (in blocks of 16
+// straight to registers 32); 64 x 5 / 64 to 4096 65 (cut 68, blocks of 16 71); D = 256,
+// 8 x 6 / 3000 28 and 28, int8 8 x 5 / 6000 of 16 heads over 2 39 and 50; but 100 with
+// 15 x 1 / 200 to 8192 36 and 30.  With D = 64, or of int8 otherwise, blocks of 32 take
+// less: 16 x 5 / 300 to 4000 of 16 heads over 4 of 64 16.5 (ring 18.9), int8 16 x 8 /
+// 2000 27 (ring 38).
+// Up to 512 blocks of 16 rows with few keys stay as they are.  Packed prompts: one of 256
+// 8.9 (ring 9.3), 7 of 30 6.7 (7.7), 600 tokens of 4 heads over one 10.1 (11.8), but 1000,
+// 500, 200 and 300 of these 18.7 (15.0).
+// More rows: the ring.  `items` is the number of blocks of 128 rows of all K/V heads.
+// Few of them with keys enough are cut for two workgroups of four waves a CU (items; in
+// brackets the best uncut): 512 / 8192 81 (128; 87), 300 / 5000 of D = 64, 32 heads over
+// 8, 39 (75; 42).  int8 keys, and D = 256, take about twice as long, so that shorter ones
+// are: int8 300 / 2048 45 (75; 52), 600 / 2300 58 (150; 69), 900 / 3000 83 (225; 88), but
+// 1200 / 2300 105 (300; 94); D = 256 672 and 189 / 672 and 2038 of 8 heads over one 33
+// (54; 49), 600 / 2300 49 (75; 55), 900 / 2300 62 (112; 56), 900 / 5000 106 (112; 109),
+// 1600 / 5000 172 (200; 162).  bf16 with D = 128, 900 / 5000 takes 84 (225; 74) and 1800
+// / 5000 138 (450; 123).  Sequences of up to 64 rows are cut in blocks of 64: 32 x 2 / 64
+// to 8192 of 32 heads over 2 24 with eight waves (27 in blocks of 128), over int8 keys
+// with four, 16 x 16 / 5000 67 (78 with eight, 76 in blocks of 128).
 // Uncut blocks of 128 rows with four waves (two workgroups a CU), with eight, and of
-// 64 rows with four and with eight: 2048 items of prompts of 8192 tokens 150, 188,
-// 192 and 238; a prompt with 512 items 51, 47, 48 and 61, with 250 28, 23, 22 and 24,
-// with 128 17, 16, 13 and 12; 8 sequences of 64 new rows and 1000 keys 29, 24, 22
-// and 19; 4 prompts of 512 25, 32, 27 and 37, 64 of 128 60, 102, 73 and 129; 225 items
-// and 5000 keys 107, 77, 91 and 104; of int8, 300 and 2300 95, 97, 98 and 125, 450 and
-// 6000 238, 284, 342 and 446, 375 and 1500 65, 54, 53 and 78.  D = 256 has blocks of
-// 64 alone, four waves and eight: 112 items 80 and 57, 256 71 and 59, 512 164 and 195,
-// of int8 200 271 and 316.
+// 64 rows with four and with eight:
+//   packed prompts   8 of 8192 tokens (2048 items)     148  180  187  234
+//                    one of 2048 (512)                  51   46   47   60
+//                    one of 1000 (250)                  27   22   22   23
+//                    one of 512 (128)                   17   16   13   12
+//                    4 of 512 (512)                     22   30   26   36
+//                    64 of 128 (2048)                   53   94   67  123
+//   paged            8 x 64 / 1000 (128)                29   24   23   19
+//                    900 / 5000 (225)                  108   74   87   91
+//   int8             1200 / 2300 (300)                  94   95   99  126
+//                    1800 / 6000 (450)                 239  280  343  455
+//                    1500 / 1500 (375)                  64   52   52   78
+//   D = 256 (blocks of 64 alone): a packed prompt of 2048 (256) 69 and 61, of 4096 (512)
+//   160 and 203; 900 / 2300 (112) 78 and 56; int8 1600 / 5000 (200) 267 and 314
 static void suggest_attention_seqs(const rc_op_desc *d, rc_schedule *s) {
     const SeqDims q = seq_dims(d);
     const int64_t rows = q.T * (q.H / q.Hkv);         // of a K/V head
